@@ -306,6 +306,39 @@ int moe_set_gemm_config(moe_ctx* ctx, int config);
  * Not a stream call: do not make it while a stream is being captured. */
 int moe_set_expert_output_fp32(moe_ctx* ctx, int enable);
 
+/* ---- the 8-bit path -----------------------------------------------------------------------
+ * Activations and weights as 8-bit integers with an fp32 scale for each token (row of
+ * activations) and each output channel (row of a weight matrix): element k of row p stands for
+ * scale[p] * q[p,k]. */
+typedef int8_t moe_i8;
+
+/* Types of a residual stream. */
+enum { MOE_RESIDUAL_BF16 = 0, MOE_RESIDUAL_FP32 = 1 };
+
+/* Root-mean-square norm with the residual's addition, and its output in 8 bits with scales:
+ *   h = x + residual (x where residual is NULL),   residual_out = h rounded to its type,
+ *   v = h * weight / sqrt(mean_i h[i]^2 + eps),    y = v rounded to bf16,
+ *   q_scale[t] = max_i |v[t,i]| / 127,             q = v / q_scale[t] to the nearest integer
+ * (ties to even), -127..127; h, v and the sums are fp32, neither rounding enters the other
+ * outputs. A row of zeros has scale 0 and q 0. A row whose v holds a NaN or an infinity has scale
+ * NaN and q 0, so that what is computed from it is NaN, and other rows are what they are.
+ * x [T,d] bf16, rows x_stride elements apart (x_stride >= d; x may be part of a wider tensor);
+ * residual [T,d] of residual_type (MOE_RESIDUAL_*) or NULL; weight [d] bf16; residual_out [T,d] of
+ * residual_type out or NULL (it may be `residual` itself); y [T,d] bf16 out or NULL; q [T,d] and
+ * q_scale [T] out, or both NULL. At least one output. Any 1 <= d <= 65536 (larger:
+ * MOE_ERR_UNSUPPORTED_SHAPE); rows start at any element; eps > 0 and finite. No context and no
+ * workspace: the calling thread's current device is the one used. */
+int moe_rmsnorm_i8(const moe_bf16* x, int64_t x_stride, const void* residual, int residual_type,
+                   const moe_bf16* weight, float eps, int32_t T, int32_t d, void* residual_out,
+                   moe_bf16* y, moe_i8* q, float* q_scale, void* stream);
+
+/* Rows of bf16 in 8 bits with a scale each: q_scale[t] = max_i |x[t,i]| / 127, q = x / q_scale[t] to
+ * the nearest integer (ties to even); zeros, NaN and infinities as for moe_rmsnorm_i8. Tokens, or the
+ * rows (output channels) of a weight matrix: T = E * N rows of K for E matrices [N,K].
+ * x [T,d], rows x_stride >= d elements apart; q [T,d]; q_scale [T]. 1 <= d <= 65536. No context. */
+int moe_quantize_i8(const moe_bf16* x, int64_t x_stride, int32_t T, int32_t d, moe_i8* q,
+                    float* q_scale, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -24,7 +24,7 @@ EXPORTS = (
     "moe_layer_forward_microbatched", "moe_last_routing", "moe_profile_begin", "moe_profile_end",
     "moe_set_gemm_config", "moe_estimate_expert_stage", "moe_layer_forward_streamed",
     "moe_estimate_streamed_stage", "moe_permute_static", "moe_set_expert_output_fp32",
-    "moe_profile_end_per_call",
+    "moe_profile_end_per_call", "moe_rmsnorm_i8", "moe_quantize_i8",
 )
 
 
@@ -297,3 +297,48 @@ def moe_set_gemm_config(ctx: MoeContext, config: int):
 def moe_set_expert_output_fp32(ctx: MoeContext, enable: bool):
     _check(lib().moe_set_expert_output_fp32(ctx._h, C.c_int(1 if enable else 0)),
            "moe_set_expert_output_fp32")
+
+
+def _rows_ptr(t: torch.Tensor, what: str):
+    """-> (pointer, row stride) of a 2-D bf16 cuda tensor whose rows are contiguous and do not overlap."""
+    if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise MoeError(f"{what}: expected a 2-D cuda tensor of {torch.bfloat16} with contiguous rows, got "
+                       f"{t.dtype} on {t.device}, shape={tuple(t.shape)}, strides={t.stride()}")
+    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return C.c_void_p(t.data_ptr()), C.c_int64(stride)
+
+
+def _sized(t: Optional[torch.Tensor], shape, what: str) -> None:
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise MoeError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def moe_rmsnorm_i8(x, residual, weight, eps, residual_out=None, y=None, q=None, q_scale=None, stream=None):
+    """x [T,d] bf16 (rows may be strided), residual [T,d] bf16 or fp32 or None, weight [d] bf16 ->
+    residual_out = x + residual, y = norm in bf16, q and q_scale = norm in 8 bits; outputs that are None
+    are not written."""
+    ptr, stride = _rows_ptr(x, "x")
+    T, d = x.shape
+    stream_type = (residual if residual is not None else residual_out)
+    stream_type = torch.bfloat16 if stream_type is None else stream_type.dtype
+    if stream_type not in (torch.bfloat16, torch.float32):
+        raise MoeError(f"residual: expected bfloat16 or float32, got {stream_type}")
+    for t, shape, what in ((residual, (T, d), "residual"), (weight, (d,), "weight"), (residual_out, (T, d), "residual_out"),
+                           (y, (T, d), "y"), (q, (T, d), "q"), (q_scale, (T,), "q_scale")):
+        _sized(t, shape, what)
+    _check(lib().moe_rmsnorm_i8(ptr, stride, _ptr(residual, stream_type, "residual"),
+                                C.c_int(1 if stream_type == torch.float32 else 0),
+                                _ptr(weight, torch.bfloat16, "weight"), C.c_float(eps), C.c_int32(T), C.c_int32(d),
+                                _ptr(residual_out, stream_type, "residual_out"), _ptr(y, torch.bfloat16, "y"),
+                                _ptr(q, torch.int8, "q"), _ptr(q_scale, torch.float32, "q_scale"), _stream(stream)),
+           "moe_rmsnorm_i8")
+
+
+def moe_quantize_i8(x, q, q_scale, stream=None):
+    """x [T,d] bf16 (rows may be strided) -> q [T,d] int8, q_scale [T] fp32. Weights: x = W.view(-1, K)."""
+    ptr, stride = _rows_ptr(x, "x")
+    T, d = x.shape
+    _sized(q, (T, d), "q")
+    _sized(q_scale, (T,), "q_scale")
+    _check(lib().moe_quantize_i8(ptr, stride, C.c_int32(T), C.c_int32(d), _ptr(q, torch.int8, "q"),
+                                 _ptr(q_scale, torch.float32, "q_scale"), _stream(stream)), "moe_quantize_i8")

@@ -9,6 +9,7 @@ namespace moe {
 
 constexpr int kWave = 64;        // CDNA wavefront width
 constexpr int kMaxExperts = 256; // four experts per lane in the permutation and routing kernels
+constexpr int kMaxRowI8 = 65536; // a row in the registers of a workgroup (norm.hip)
 constexpr int kXcds = 8;         // workgroups are dealt round-robin to the 8 XCDs (own L2 each)
 
 __device__ __forceinline__ float bf16_to_f32(uint16_t b) {
@@ -88,5 +89,10 @@ int launch_down(const GemmEnv& env, const moe_bf16* H, const int32_t* offsets, i
                 int d, int f, int E, const moe_bf16* W2, void* y_perm, bool y_f32, hipStream_t s);
 int launch_combine(const void* y_perm, bool y_f32, const int32_t* inv_perm, const float* topk_w, int T,
                    int d, int k, moe_bf16* y, hipStream_t s);
+// Rows in 8 bits, of up to kMaxRowI8 elements: the norm in front of an 8-bit product, and bf16 rows as they are.
+int launch_rmsnorm_i8(const moe_bf16* x, long long x_stride, const void* residual, bool residual_f32,
+                      const moe_bf16* weight, float eps, int T, int d, void* residual_out, moe_bf16* y, moe_i8* q,
+                      float* q_scale, hipStream_t s);
+int launch_quantize_i8(const moe_bf16* x, long long x_stride, int T, int d, moe_i8* q, float* q_scale, hipStream_t s);
 
 }  // namespace moe

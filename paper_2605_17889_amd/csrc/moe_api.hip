@@ -1,5 +1,6 @@
 // C-ABI entry points of libmoe: argument validation, workspace, stage sequencing and the
 // optional per-stage event timing. All arithmetic lives in the kernels of the other files.
+#include <cmath>
 #include <new>
 #include <vector>
 
@@ -624,6 +625,29 @@ int moe_set_expert_output_fp32(moe_ctx* c, int enable) {
         if (err != hipSuccess) return MOE_ERR_HIP;
     }
     return MOE_OK;
+}
+
+// Outputs in 8 bits come with their scales, and an eps that is not positive would divide by zero on a row of zeros.
+int moe_rmsnorm_i8(const moe_bf16* x, int64_t x_stride, const void* residual, int residual_type,
+                   const moe_bf16* weight, float eps, int32_t T, int32_t d, void* residual_out, moe_bf16* y,
+                   moe_i8* q, float* q_scale, void* stream) {
+    if (T < 0 || d < 1 || x_stride < d || !(eps > 0.f) || !(eps < INFINITY)) return MOE_ERR_INVALID_ARG;
+    if (residual_type != MOE_RESIDUAL_BF16 && residual_type != MOE_RESIDUAL_FP32) return MOE_ERR_INVALID_ARG;
+    if (d > kMaxRowI8) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (T == 0) return MOE_OK;
+    if (!x || !weight || (q == nullptr) != (q_scale == nullptr)) return MOE_ERR_INVALID_ARG;
+    if (!residual_out && !y && !q) return MOE_ERR_INVALID_ARG;
+    return launch_rmsnorm_i8(x, x_stride, residual, residual_type == MOE_RESIDUAL_FP32, weight, eps, T, d,
+                             residual_out, y, q, q_scale, static_cast<hipStream_t>(stream));
+}
+
+int moe_quantize_i8(const moe_bf16* x, int64_t x_stride, int32_t T, int32_t d, moe_i8* q, float* q_scale,
+                    void* stream) {
+    if (T < 0 || d < 1 || x_stride < d) return MOE_ERR_INVALID_ARG;
+    if (d > kMaxRowI8) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (T == 0) return MOE_OK;
+    if (!x || !q || !q_scale) return MOE_ERR_INVALID_ARG;
+    return launch_quantize_i8(x, x_stride, T, d, q, q_scale, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

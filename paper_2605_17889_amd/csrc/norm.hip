@@ -1,0 +1,289 @@
+// Rows in 8-bit integers with a scale each: the root-mean-square norm with the residual's addition in front of an 8-bit
+// product, and the plain conversion of bf16 rows (the experts' intermediate, a matrix's output channels).
+//
+//   h = x + residual,  r = 1 / sqrt(mean(h^2) + eps),  y = h * w * r,  scale = max|y| / 127,  q = rint(y / scale)
+//
+// One pass over the data: a row stays in registers between its loads and its stores. With u = h * w the largest |y| is
+// the largest |u| times r and y / scale is u * 127 / max|u|, so the sum of squares and the maximum are reduced
+// together, once per row, and q does not wait for r. All of it is fp32; the sum's order is fixed by d and T.
+#include "common.h"
+
+namespace moe {
+namespace {
+
+constexpr int kVec = 8;             // consecutive elements that a thread holds per chunk
+
+// Addresses need not be multiples of anything: rows of odd lengths and rows cut out of wider tensors start anywhere.
+// The compiler makes one wide load or store of these (the hardware takes any address).
+struct Raw16 { uint32_t w[4]; };
+struct Raw8 { uint32_t w[2]; };
+template <class T> __device__ __forceinline__ T load_any(const void* p) {
+    T v;
+    __builtin_memcpy(&v, p, sizeof(T));
+    return v;
+}
+template <class T> __device__ __forceinline__ void store_any(void* p, const T& v) { __builtin_memcpy(p, &v, sizeof(T)); }
+
+// Elements [at, at + n) of a row, n <= 8; those past n are zero. bf16 ones stay packed, two to a register.
+__device__ __forceinline__ Raw16 load_packed(const uint16_t* row, int at, int n) {
+    if (n == kVec) return load_any<Raw16>(row + at);
+    Raw16 r{};
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+        if (i < n) r.w[i >> 1] |= static_cast<uint32_t>(row[at + i]) << (16 * (i & 1));
+    return r;
+}
+__device__ __forceinline__ float unpack(const Raw16& r, int i) {
+    return __uint_as_float((i & 1) ? (r.w[i >> 1] & 0xffff0000u) : (r.w[i >> 1] << 16));
+}
+__device__ __forceinline__ void load_row(const uint16_t* row, int at, int n, float (&v)[kVec]) {
+    const Raw16 r = load_packed(row, at, n);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = unpack(r, i);
+}
+__device__ __forceinline__ void load_row(const float* row, int at, int n, float (&v)[kVec]) {
+    if (n == kVec) {
+        const Raw16 a = load_any<Raw16>(row + at), b = load_any<Raw16>(row + at + 4);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = __uint_as_float(i < 4 ? a.w[i & 3] : b.w[i & 3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) v[i] = i < n ? row[at + i] : 0.f;
+    }
+}
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {      // round to nearest even
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+}
+__device__ __forceinline__ void store_row(uint16_t* row, int at, int n, const float (&v)[kVec]) {
+    if (n == kVec) {
+        Raw16 r;
+#pragma unroll
+        for (int i = 0; i < kVec; i += 2) r.w[i >> 1] = bf16_pair(v[i], v[i + 1]);
+        store_any(row + at, r);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (i < n) row[at + i] = f32_to_bf16(v[i]);
+    }
+}
+__device__ __forceinline__ void store_row(float* row, int at, int n, const float (&v)[kVec]) {
+    if (n == kVec) {
+        Raw16 a, b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a.w[i] = __float_as_uint(v[i]);
+            b.w[i] = __float_as_uint(v[i + 4]);
+        }
+        store_any(row + at, a);
+        store_any(row + at + 4, b);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (i < n) row[at + i] = v[i];
+    }
+}
+
+// q = rint(u * k), |u * k| <= 127 up to rounding: in fma(u, k, 1.5 * 2^23) the sum's unit is 1, so that the one rounding
+// of the fused operation is the one to the nearest integer (ties to even), whose two's complement is the low byte.
+__device__ __forceinline__ void store_q(int8_t* row, int at, int n, const float (&u)[kVec], float k, bool fine) {
+    uint32_t b[kVec];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) b[i] = __float_as_uint(fmaf(u[i], k, 12582912.f));
+    Raw8 r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t lo = __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u);
+        const uint32_t hi = __builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x04000c0cu);
+        r.w[i] = fine ? lo | hi : 0u;
+    }
+    if (n == kVec) {
+        store_any(row + at, r);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (i < n) row[at + i] = static_cast<int8_t>(r.w[i >> 2] >> (8 * (i & 3)));
+    }
+}
+
+// Sum and maximum over the threads of a row, the same bits in all of them: butterflies inside a wavefront, then the
+// wavefronts' results in their order. |values| as integers: a NaN counts as more than infinity and stays.
+template <int WAVES>
+__device__ __forceinline__ void reduce_row(float& sum, uint32_t& peak, float* sums, uint32_t* peaks) {
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) {
+        sum += __shfl_xor(sum, s);
+        peak = max(peak, static_cast<uint32_t>(__shfl_xor(static_cast<int>(peak), s)));
+    }
+    if constexpr (WAVES > 1) {
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) {
+            sums[wave] = sum;
+            peaks[wave] = peak;
+        }
+        __syncthreads();
+        sum = sums[0];
+        peak = peaks[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) {
+            sum += sums[w];
+            peak = max(peak, peaks[w]);
+        }
+    }
+}
+
+struct RowArgs {
+    const uint16_t* x;               // [T, d], rows x_stride elements apart
+    long long x_stride;
+    const void* residual;            // [T, d] of Residual, or null
+    const uint16_t* weight;          // [d], with NORM
+    float eps;
+    int T, d;
+    void* residual_out;              // [T, d] of Residual, or null; may be `residual` itself
+    uint16_t* y;                     // [T, d], or null
+    moe_i8* q;                       // [T, d], or null
+    float* scale;                    // [T]
+};
+
+// TPR threads per row, each with CHUNKS chunks of 8 elements: chunk c of thread t is elements 8 * (c * TPR + t) to + 7.
+// A workgroup holds one row, or with TPR = 64 a row per wavefront.
+template <int TPR, int CHUNKS, bool NORM, class Residual>
+__global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_i8_kernel(RowArgs a) {
+    constexpr int WAVES = TPR / kWave;
+    __shared__ float sums[2][WAVES];
+    __shared__ uint32_t peaks[2][WAVES];
+    const int t = TPR == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    if (TPR == 64 && t >= a.T) return;               // the whole wavefront; no barrier follows with TPR = 64
+    const int lane = TPR == 64 ? threadIdx.x & 63 : threadIdx.x;
+    const size_t row = static_cast<size_t>(t) * a.d;
+    const uint16_t* x = a.x + static_cast<long long>(t) * a.x_stride;
+    const Residual* res = a.residual ? static_cast<const Residual*>(a.residual) + row : nullptr;
+    auto at = [&](int c) { return (c * TPR + lane) * kVec; };
+    auto count = [&](int c) { return min(kVec, a.d - at(c)); };      // 0 or less: nothing of this chunk is in the row
+
+    float h[CHUNKS][kVec];
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) h[c][i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+        if (count(c) > 0) load_row(x, at(c), count(c), h[c]);
+    if (NORM && res) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+            if (count(c) > 0) {
+                float v[kVec];
+                load_row(res, at(c), count(c), v);
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) h[c][i] += v[i];
+            }
+    }
+    Raw16 w[NORM ? CHUNKS : 1] = {};
+    if constexpr (NORM) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+            if (count(c) > 0) w[c] = load_packed(a.weight, at(c), count(c));
+    }
+    auto weighted = [&](int c, int i) { return NORM ? h[c][i] * unpack(w[NORM ? c : 0], i) : h[c][i]; };
+    auto reduce = [&](float& sum, uint32_t& peak, int which) {
+        sum = 0.f;
+        peak = 0;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                if constexpr (NORM) sum = fmaf(h[c][i], h[c][i], sum);
+                peak = max(peak, __float_as_uint(weighted(c, i)) & 0x7fffffffu);
+            }
+        reduce_row<WAVES>(sum, peak, sums[which], peaks[which]);
+    };
+    float sum;
+    uint32_t peak;
+    reduce(sum, peak, 0);
+    if (NORM && a.residual_out) {
+        Residual* out = static_cast<Residual*>(a.residual_out) + row;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+            if (count(c) > 0) store_row(out, at(c), count(c), h[c]);
+    }
+    float r = 1.f;
+    if constexpr (NORM) {
+        float down = 1.f;
+        // values past 2^63 or so, whose squares leave the range of fp32: again with the row scaled by 2^-64 (the same
+        // decision in all threads of the row; a row that holds an infinity or a NaN stays one that does)
+        if (!(sum < __builtin_inff())) {
+            down = 0x1p-64f;
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) h[c][i] *= down;
+            reduce(sum, peak, 1);
+        }
+        r = 1.f / sqrtf(sum / static_cast<float>(a.d) + a.eps * down * down);
+    }
+    const float top = __uint_as_float(peak) * r;     // the largest |y|
+    if (NORM && a.y) {
+        uint16_t* out = a.y + row;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+            if (count(c) > 0) {
+                float v[kVec];
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) v[i] = weighted(c, i) * r;
+                store_row(out, at(c), count(c), v);
+            }
+    }
+    if (a.q) {
+        const bool fine = peak < 0x7f800000u && top < __builtin_inff();
+        // 127 / max|u| leaves the range of fp32 for the smallest maxima: both factors are then moved by 2^100
+        const float up = peak < 0x0d800000u ? 0x1p100f : 1.f;        // below 2^-100
+        const float k = peak == 0 ? 0.f : 127.f / (__uint_as_float(peak) * up);
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+            if (count(c) > 0) {
+                float u[kVec];
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) u[i] = weighted(c, i) * up;
+                store_q(a.q + row, at(c), count(c), u, k, fine);
+            }
+        if (lane == 0) a.scale[t] = fine ? top / 127.f : __builtin_nanf("");
+    }
+}
+
+template <int TPR, int CHUNKS, bool NORM, class Residual>
+int launch_rows(const RowArgs& a, hipStream_t s) {
+    const int rows = TPR == 64 ? 4 : 1;
+    hipLaunchKernelGGL((rows_i8_kernel<TPR, CHUNKS, NORM, Residual>), dim3((a.T + rows - 1) / rows),
+                       dim3(TPR == 64 ? 256 : TPR), 0, s, a);
+    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
+template <bool NORM, class Residual>
+int launch_rows_of(const RowArgs& a, hipStream_t s) {
+    if (a.T == 0) return MOE_OK;
+    const int chunks = (a.d + kVec - 1) / kVec;
+    if (chunks <= 64) return launch_rows<64, 1, NORM, Residual>(a, s);
+    if (chunks <= 256) return launch_rows<256, 1, NORM, Residual>(a, s);
+    if (chunks <= 512) return launch_rows<256, 2, NORM, Residual>(a, s);
+    if (chunks <= 768) return launch_rows<256, 3, NORM, Residual>(a, s);
+    if (chunks <= 1024) return launch_rows<256, 4, NORM, Residual>(a, s);
+    if (chunks <= 2048) return launch_rows<256, 8, NORM, Residual>(a, s);
+    return launch_rows<1024, 8, NORM, Residual>(a, s);
+}
+
+}  // namespace
+
+int launch_rmsnorm_i8(const moe_bf16* x, long long x_stride, const void* residual, bool residual_f32,
+                      const moe_bf16* weight, float eps, int T, int d, void* residual_out, moe_bf16* y, moe_i8* q,
+                      float* q_scale, hipStream_t s) {
+    const RowArgs a{x, x_stride, residual, weight, eps, T, d, residual_out, y, q, q_scale};
+    return residual_f32 ? launch_rows_of<true, float>(a, s) : launch_rows_of<true, uint16_t>(a, s);
+}
+
+int launch_quantize_i8(const moe_bf16* x, long long x_stride, int T, int d, moe_i8* q, float* q_scale, hipStream_t s) {
+    const RowArgs a{x, x_stride, nullptr, nullptr, 0.f, T, d, nullptr, nullptr, q, q_scale};
+    return launch_rows_of<false, uint16_t>(a, s);
+}
+
+}  // namespace moe
