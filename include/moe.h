@@ -339,6 +339,37 @@ int moe_rmsnorm_i8(const moe_bf16* x, int64_t x_stride, const void* residual, in
 int moe_quantize_i8(const moe_bf16* x, int64_t x_stride, int32_t T, int32_t d, moe_i8* q,
                     float* q_scale, void* stream);
 
+/* Types of a product's output. */
+enum { MOE_OUT_BF16 = 0, MOE_OUT_FP32 = 1 };
+
+/* Matrix product in 8-bit integers with a scale for each token and each output channel: for
+ * offsets[e] <= p < offsets[e+1],
+ *   out[p,n] = x_scale[p] * w_scale[e,n] * sum_k x[p,k] * W[e,n,k],
+ * the sum exact (int32), rounded to fp32, multiplied by x_scale[p], then by w_scale[e,n] in fp32, and
+ * rounded to out's type. offsets [E+1] int32 (device), or NULL with E == 1: all R rows are one group
+ * (one matrix for all tokens). x [R,K]; x_scale [R]; W [E,N,K]; w_scale [E,N]; out [R,N] of out_type.
+ * x, W and out start at multiples of 16 bytes (not checked). R <= T_max * k of the context, whose
+ * d_model, d_ff and E play no part here. E <= 256; K a multiple of 128 up to 130944 (the sums
+ * fit 32 bits); N a multiple of 16, 32 <= N <= 2^23; else MOE_ERR_UNSUPPORTED_SHAPE. */
+int moe_gemm_i8(moe_ctx* ctx, const moe_i8* x, const float* x_scale, const int32_t* offsets,
+                int32_t R, int32_t E, int32_t N, int32_t K, const moe_i8* W, const float* w_scale,
+                void* out, int out_type, void* stream);
+
+/* moe_expert_ffn in 8 bits: rows grouped by expert in 8 bits with their scales, weights in 8 bits with
+ * a scale for each output channel, for offsets[e] <= p < offsets[e+1]
+ *   H[p,:]      = bf16( SiLU(g) (.) u ),  g and u the products (as in moe_gemm_i8) with W1 and W3,
+ *   q, s        = H's rows in 8 bits (as in moe_quantize_i8),
+ *   y_perm[p,:] = bf16 product of q, s with W2.
+ * x_perm [R,d_model]; x_scale [R]; W1, W3 [E,d_ff,d_model], their scales [E,d_ff]; W2
+ * [E,d_model,d_ff], w2_scale [E,d_model]; y_perm [R,d_model] bf16 out; R <= T_max * k; x_perm, the
+ * weights and y_perm start at multiples of 16 bytes (not checked). d_ff <= 65536. The first call allocates
+ * T_max * k * (d_ff + 4) bytes, kept until moe_destroy (MOE_ERR_WORKSPACE if that fails): make one
+ * before recording such calls into a HIP graph. */
+int moe_expert_ffn_i8(moe_ctx* ctx, const moe_i8* x_perm, const float* x_scale,
+                      const int32_t* offsets, int32_t R, const moe_i8* W1, const float* w1_scale,
+                      const moe_i8* W3, const float* w3_scale, const moe_i8* W2,
+                      const float* w2_scale, moe_bf16* y_perm, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

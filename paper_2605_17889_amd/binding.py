@@ -24,7 +24,7 @@ EXPORTS = (
     "moe_layer_forward_microbatched", "moe_last_routing", "moe_profile_begin", "moe_profile_end",
     "moe_set_gemm_config", "moe_estimate_expert_stage", "moe_layer_forward_streamed",
     "moe_estimate_streamed_stage", "moe_permute_static", "moe_set_expert_output_fp32",
-    "moe_profile_end_per_call", "moe_rmsnorm_i8", "moe_quantize_i8",
+    "moe_profile_end_per_call", "moe_rmsnorm_i8", "moe_quantize_i8", "moe_gemm_i8", "moe_expert_ffn_i8",
 )
 
 
@@ -342,3 +342,41 @@ def moe_quantize_i8(x, q, q_scale, stream=None):
     _sized(q_scale, (T,), "q_scale")
     _check(lib().moe_quantize_i8(ptr, stride, C.c_int32(T), C.c_int32(d), _ptr(q, torch.int8, "q"),
                                  _ptr(q_scale, torch.float32, "q_scale"), _stream(stream)), "moe_quantize_i8")
+
+
+def _i8_matrices(shape, W, scale, what: str):
+    """Pointers of matrices [E,N,K] (or [N,K]) in 8 bits and their scales [E,N] (or [N]); E * N * K elements in all."""
+    E, N, K = shape
+    for t, full in ((W, (E, N, K)), (scale, (E, N))):
+        if t is not None and tuple(t.shape) != full and not (E == 1 and tuple(t.shape) == full[1:]):
+            raise MoeError(f"{what}: expected shape {full}, got {tuple(t.shape)}")
+    return _ptr(W, torch.int8, what), _ptr(scale, torch.float32, what + "_scale")
+
+
+def moe_gemm_i8(ctx: MoeContext, x, x_scale, offsets, R, E, N, K, W, w_scale, out, stream=None):
+    """out[p,n] = x_scale[p] * w_scale[e,n] * sum_k x[p,k] W[e,n,k] for the rows p of expert e; offsets None: one
+    matrix for all rows. x [R,K] int8, W [E,N,K] int8, scales fp32, out [R,N] bf16 or fp32."""
+    for t, shape, what in ((x, (R, K), "x"), (x_scale, (R,), "x_scale"), (offsets, (E + 1,), "offsets"), (out, (R, N), "out")):
+        _sized(t, shape, what)
+    w, ws = _i8_matrices((E, N, K), W, w_scale, "W")
+    f32 = out is not None and out.dtype == torch.float32
+    _check(lib().moe_gemm_i8(ctx._h, _ptr(x, torch.int8, "x"), _ptr(x_scale, torch.float32, "x_scale"),
+                             _ptr(offsets, torch.int32, "offsets"), C.c_int32(R), C.c_int32(E), C.c_int32(N), C.c_int32(K),
+                             w, ws, _ptr(out, torch.float32 if f32 else torch.bfloat16, "out"), C.c_int(1 if f32 else 0),
+                             _stream(stream)), "moe_gemm_i8")
+
+
+def moe_expert_ffn_i8(ctx: MoeContext, x_perm, x_scale, offsets, R, W1, w1_scale, W3, w3_scale, W2, w2_scale, y_perm,
+                      stream=None):
+    """moe_expert_ffn over rows and weights in 8 bits: x_perm [R,d] int8, W1, W3 [E,f,d] and W2 [E,d,f] int8, scales fp32
+    for each row and each output channel, y_perm [R,d] bf16."""
+    d, f, E = ctx.d_model, ctx.d_ff, ctx.E
+    for t, shape, what in ((x_perm, (R, d), "x_perm"), (x_scale, (R,), "x_scale"), (offsets, (E + 1,), "offsets"),
+                           (y_perm, (R, d), "y_perm")):
+        _sized(t, shape, what)
+    w1, s1 = _i8_matrices((E, f, d), W1, w1_scale, "W1")
+    w3, s3 = _i8_matrices((E, f, d), W3, w3_scale, "W3")
+    w2, s2 = _i8_matrices((E, d, f), W2, w2_scale, "W2")
+    _check(lib().moe_expert_ffn_i8(ctx._h, _ptr(x_perm, torch.int8, "x_perm"), _ptr(x_scale, torch.float32, "x_scale"),
+                                   _ptr(offsets, torch.int32, "offsets"), C.c_int32(R), w1, s1, w3, s3, w2, s2,
+                                   _ptr(y_perm, torch.bfloat16, "y_perm"), _stream(stream)), "moe_expert_ffn_i8")

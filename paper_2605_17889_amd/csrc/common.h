@@ -10,6 +10,8 @@ namespace moe {
 constexpr int kWave = 64;        // CDNA wavefront width
 constexpr int kMaxExperts = 256; // four experts per lane in the permutation and routing kernels
 constexpr int kMaxRowI8 = 65536; // a row in the registers of a workgroup (norm.hip)
+constexpr int kMaxSumI8 = 130944; // products of -128 .. 127 whose sum stays below 2^31, a multiple of 128
+constexpr int kMaxDimI8 = 1 << 23; // widths of outputs, for 32-bit offsets inside a tile
 constexpr int kXcds = 8;         // workgroups are dealt round-robin to the 8 XCDs (own L2 each)
 
 __device__ __forceinline__ float bf16_to_f32(uint16_t b) {
@@ -94,5 +96,11 @@ int launch_rmsnorm_i8(const moe_bf16* x, long long x_stride, const void* residua
                       const moe_bf16* weight, float eps, int T, int d, void* residual_out, moe_bf16* y, moe_i8* q,
                       float* q_scale, hipStream_t s);
 int launch_quantize_i8(const moe_bf16* x, long long x_stride, int T, int d, moe_i8* q, float* q_scale, hipStream_t s);
+// Products of 8-bit integers with scales (expert_gemm_i8.hip). R rows in E groups; without offsets they are one group.
+int launch_gateup_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, int d, int f,
+                     int E, const moe_i8* W1, const float* w1_scale, const moe_i8* W3, const float* w3_scale, moe_bf16* H,
+                     hipStream_t s);
+int launch_product_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, int N, int K,
+                      int E, const moe_i8* W, const float* w_scale, void* out, bool out_f32, hipStream_t s);
 
 }  // namespace moe

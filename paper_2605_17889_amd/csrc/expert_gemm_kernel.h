@@ -27,6 +27,12 @@
 //                           the direct-to-LDS loads are spread between the MFMAs.
 // In the last two the workgroup barrier sits in the middle of a k-step, so that MFMAs are ready on
 // both sides of it, and the two operands have LDS rings of different depth.
+//
+// Operands of 8-bit integers (OperandsI8) run through the same kernels: 16 bytes of a row are a lane's operand of
+// v_mfma_i32_16x16x64_i8 as they are one of v_mfma_f32_16x16x32_bf16, in the same cycles, so a row of K integers is loaded,
+// staged and read as K / 2 units of 16 bits, which is what K, BK and offsets along k count here. The sums are exact
+// (int32, |q| <= 127: up to 133000 products), so they are the same in every tile and order; the epilogue turns them into
+// fp32 and multiplies by the row's scale, then by the column's.
 #pragma once
 #include <type_traits>
 
@@ -40,6 +46,7 @@ namespace gemm {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kGroupM = 8;   // at most this many m-tiles that sweep the n-tiles together (share weight tiles)
@@ -285,6 +292,13 @@ struct TileTable {
         for (int w = 0; w <= EPL; ++w) off[w] += before;
         init_tiles(NT, 0, xcd);
     }
+    // one group of `rows` rows
+    __device__ __forceinline__ void init_one(int rows, int NT, int split_cus, int xcd, int lane) {
+        off[0] = lane == 0 ? 0 : rows;
+#pragma unroll
+        for (int w = 1; w <= EPL; ++w) off[w] = rows;
+        init_tiles(NT, split_cus, xcd);
+    }
     __device__ __forceinline__ int first_row(int expert) const {
         int v = off[0];
 #pragma unroll
@@ -360,6 +374,17 @@ __device__ __forceinline__ TileCoord locate_tile(const int32_t* __restrict__ off
     return uniform_tile(table.find(NT, cut, slot, division_magic(threadIdx.x & (kWave - 1))));
 }
 
+// The same for one group that is all of `rows` rows, without offsets in memory.
+template <int BM>
+__device__ __forceinline__ TileCoord locate_tile_of_one(int rows, int NT, int split_cus = 0, Cut cut = Cut::kNever) {
+    SlotRange range;
+    range.init((rows + BM - 1) / BM * NT, split_cus, blockIdx.x % kXcds);
+    int half;
+    const int L = range.tile(blockIdx.x / kXcds, half);
+    if (L < 0) return TileCoord{kNoTile, 0, 0, 0, 0};
+    return uniform_tile(tile_in_expert<BM>(0, 0, rows, L, NT, half, cut));
+}
+
 // LDS tile layout: rows of BK bf16 in 16-byte chunks; logical chunk c of row r is stored at
 // chunk position c ^ swz(r). LDS has 64 four-byte banks and a 16-byte read is served 16 lanes
 // at a time; the 16 lanes of a fragment read the same logical chunk of 16 consecutive rows,
@@ -431,6 +456,11 @@ struct F32Out : Cfg {
     static constexpr bool OUT_F32 = true;
     static_assert(!Cfg::DUAL, "the gate/up intermediate stays bf16");
 };
+// The same tiling over operands of 8-bit integers; accumulators hold int32 bits.
+template <class Cfg>
+struct OperandsI8 : Cfg {
+    static constexpr bool OPERANDS_I8 = true;
+};
 // The same tile with H rows.
 template <class Cfg, int H> struct WithHeight;
 template <int BM, int BN, int BK, int WM, int WN, int NSTAGE, bool DUAL, bool STREAM_B, int H>
@@ -439,13 +469,30 @@ struct WithHeight<Config<BM, BN, BK, WM, WN, NSTAGE, DUAL, STREAM_B>, H> {
 };
 template <class Cfg, int H>
 struct WithHeight<F32Out<Cfg>, H> { using type = F32Out<typename WithHeight<Cfg, H>::type>; };
+template <class Cfg, int H>
+struct WithHeight<OperandsI8<Cfg>, H> { using type = OperandsI8<typename WithHeight<Cfg, H>::type>; };
 template <class Cfg, int H> using AtHeight = typename WithHeight<Cfg, H>::type;
 template <class Cfg, class = void>
 struct out_is_f32 : std::false_type {};
 template <class Cfg>
 struct out_is_f32<Cfg, std::void_t<decltype(Cfg::OUT_F32)>> : std::bool_constant<Cfg::OUT_F32> {};
+template <class Cfg, class = void>
+struct operands_i8 : std::false_type {};
+template <class Cfg>
+struct operands_i8<Cfg, std::void_t<decltype(Cfg::OPERANDS_I8)>> : std::bool_constant<Cfg::OPERANDS_I8> {};
 
 // ---- pieces shared by the kernels ---------------------------------------------------------
+
+// The n-tiles of N output columns. With 8-bit operands N need not be a multiple of a tile's columns (it has to hold one): the
+// last tile then starts further left, and the columns that two tiles share get the same bits from both.
+template <class Cfg>
+__host__ __device__ __forceinline__ int n_tiles(int N) {
+    return operands_i8<Cfg>::value ? (N + Cfg::BN_OUT - 1) / Cfg::BN_OUT : N / Cfg::BN_OUT;
+}
+template <class Cfg>
+__device__ __forceinline__ int first_column(const TileCoord& tc, int N) {
+    return operands_i8<Cfg>::value ? min(tc.nt * Cfg::BN_OUT, N - Cfg::BN_OUT) : tc.nt * Cfg::BN_OUT;
+}
 
 // MFMA 16x16x32 operand fragment: lane l supplies 8 consecutive k (k-group l >> 4) of operand
 // row l & 15. Per-lane LDS byte offsets inside a stage of the fragment of this wavefront's
@@ -473,8 +520,14 @@ __device__ __forceinline__ bf16x8 lds16(const unsigned char* p) {
 }
 
 // acc (16x16, transposed: rows = weight rows, columns = activation rows) += W_frag * X_frag
+template <bool I8 = false>
 __device__ __forceinline__ f32x4 mma16(const bf16x8& w, const bf16x8& x, const f32x4& acc) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, acc, 0, 0, 0);
+    if constexpr (I8)
+        return __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_i32_16x16x64_i8(
+                                             __builtin_bit_cast(i32x4, w), __builtin_bit_cast(i32x4, x),
+                                             __builtin_bit_cast(i32x4, acc), 0, 0, 0));
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, acc, 0, 0, 0);
 }
 
 // The same instruction with the accumulator pinned to the accumulation registers (AGPRs). The
@@ -483,8 +536,10 @@ __device__ __forceinline__ f32x4 mma16(const bf16x8& w, const bf16x8& x, const f
 // two register classes inside the k-loop). The compiler does not know that this is an MFMA:
 // it still waits for the LDS reads that feed it, but the kernel must pad by hand before
 // anything other than an MFMA touches the accumulators (see mfma_drain()).
+template <bool I8 = false>
 __device__ __forceinline__ void mma16_agpr(const bf16x8& w, const bf16x8& x, f32x4& acc) {
-    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(w), "v"(x));
+    if constexpr (I8) asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(w), "v"(x));
+    else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(w), "v"(x));
 }
 // Wait states between the last MFMA and the first ordinary read of its result. `last` are the
 // accumulators of the last MFMAs: the empty statements keep the compiler from reading them ahead of
@@ -496,21 +551,106 @@ __device__ __forceinline__ void mfma_drain(f32x4 (&last)[N]) {
     for (int j = 0; j < N; ++j) asm volatile("" : "+a"(last[j]));
 }
 
+// Scales of operands in 8 bits: of the rows of the grouped A matrix, and of the rows of the weight matrices [E, N].
+struct ScalesI8 {
+    const float *x, *w0, *w1;
+    int rows;            // where there are no offsets: the rows of the one group
+};
+struct NoScales {};
+template <class Cfg> using ScalesOf = std::conditional_t<operands_i8<Cfg>::value, ScalesI8, NoScales>;
+
+// The scales of one wavefront's outputs, spread over its lanes: one load per 64 of them at the start of a tile, two to four
+// registers through the k-loop, a permute across lanes (no LDS memory) where an accumulator needs its own. Rows past the end of
+// the group take its last one's.
+template <class Cfg>
+struct TileScales {
+    static constexpr int GROUP = Cfg::DUAL ? 2 : 1;        // columns of W1, then the same ones of W3
+    static constexpr int COLS = Cfg::WTN / GROUP;          // output columns of the wavefront
+    static constexpr int NX = (Cfg::WTM + 63) / 64, NC = (COLS + 63) / 64;
+    float x[NX], w[GROUP][NC];
+    __device__ __forceinline__ void load(const ScalesI8& sc, const TileCoord& tc, int wm, int wn, int lane, int N) {
+        const float* xs = sc.x + tc.row0;
+#pragma unroll
+        for (int i = 0; i < NX; ++i) x[i] = xs[min(wm * Cfg::WTM + i * 64 + lane, tc.rows - 1)];
+        const size_t first = static_cast<size_t>(tc.expert) * N + first_column<Cfg>(tc, N) + wn * COLS;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int col = c * 64 + min(lane, COLS - 1);
+            w[0][c] = sc.w0[first + col];
+            if constexpr (Cfg::DUAL) w[1][c] = sc.w1[first + col];
+        }
+    }
+    // The row scale of fragment row i.
+    __device__ __forceinline__ float of_row(int i, int frag_row) const {
+        return of_lane(x[i / 4], (i & 3) * 16 + frag_row);
+    }
+    // The scales of the four columns of B fragment j that a lane's accumulators hold.
+    __device__ __forceinline__ f32x4 of_columns(int j, int frag_kg) const {
+        constexpr int P = Cfg::DB / 16;
+        const int up = Cfg::DUAL && (j & P) ? 1 : 0;
+        const int col = Cfg::DUAL ? j / (2 * P) * Cfg::DB + j % P * 16 : j * 16;
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = of_lane(w[up][col / 64], (col & 63) + 4 * frag_kg + r);
+        return v;
+    }
+    static __device__ __forceinline__ float of_lane(float v, int from) {
+        return __uint_as_float(__builtin_amdgcn_ds_bpermute(from * 4, __float_as_uint(v)));
+    }
+};
+template <> struct TileScales<void> {};
+// The tile of this workgroup where every workgroup has one.
+template <class Cfg>
+__device__ __forceinline__ TileCoord tile_of_workgroup(const int32_t* __restrict__ offsets, const ScalesOf<Cfg>& sc, int E,
+                                                       int N, int split_cus, Cut cut) {
+    if constexpr (operands_i8<Cfg>::value)
+        if (offsets == nullptr) return locate_tile_of_one<Cfg::BM>(sc.rows, n_tiles<Cfg>(N), split_cus, cut);
+    return locate_tile<Cfg::BM>(offsets, E, n_tiles<Cfg>(N), split_cus, cut);
+}
+
+// What a kernel keeps of them: nothing for bf16 operands.
+template <class Cfg> using KeptScales = TileScales<std::conditional_t<operands_i8<Cfg>::value, Cfg, void>>;
+template <class Cfg>
+__device__ __forceinline__ KeptScales<Cfg> load_scales(const ScalesOf<Cfg>& sc, const TileCoord& tc, int wm, int wn,
+                                                       int lane, int N) {
+    KeptScales<Cfg> kept;
+    if constexpr (operands_i8<Cfg>::value) kept.load(sc, tc, wm, wn, lane, N);
+    return kept;
+}
+
+// An int32 sum (its bits) as the number it stands for: one rounding to fp32, then one for each scale.
+__device__ __forceinline__ float scaled(float bits, float row, float col) {
+    return static_cast<float>(static_cast<int>(__float_as_uint(bits))) * row * col;
+}
+
 // Epilogue. Result layout of the transposed 16x16 tile: lane holds activation row (lane & 15)
 // and the four output columns 4 * (lane >> 4) + r in registers r = 0..3. With DUAL, B-tile rows
 // come in blocks of DB W1 rows followed by the DB W3 rows of the same output columns, so accumulator
 // tiles j and j + P (P = DB / 16, j & P == 0) are gate and up of the same columns.
 template <class Cfg>
-__device__ __forceinline__ void store_tile(const f32x4 (&acc)[Cfg::TM][Cfg::TN], const TileCoord& tc,
+__device__ __forceinline__ void store_tile(f32x4 (&acc)[Cfg::TM][Cfg::TN], const TileCoord& tc,
                                            const FragPlan<Cfg>& fp, int wm, int wn,
-                                           uint16_t* __restrict__ C, int ldc) {
+                                           uint16_t* __restrict__ C, int ldc, const KeptScales<Cfg>& sc) {
     constexpr bool DUAL = Cfg::DUAL;
     constexpr int DB = Cfg::DB, P = DB / 16;
+    if constexpr (operands_i8<Cfg>::value) {
+        f32x4 cols[Cfg::TN];
+#pragma unroll
+        for (int j = 0; j < Cfg::TN; ++j) cols[j] = sc.of_columns(j, fp.frag_kg);
+#pragma unroll
+        for (int i = 0; i < Cfg::TM; ++i) {
+            const float row = sc.of_row(i, fp.frag_row);
+#pragma unroll
+            for (int j = 0; j < Cfg::TN; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[i][j][r] = scaled(acc[i][j][r], row, cols[j][r]);
+        }
+    }
 #pragma unroll
     for (int i = 0; i < Cfg::TM; ++i) {
         const int row = wm * Cfg::WTM + i * 16 + fp.frag_row;
         if (row >= tc.rows) continue;
-        uint16_t* crow = C + static_cast<size_t>(tc.row0 + row) * ldc + tc.nt * Cfg::BN_OUT + 4 * fp.frag_kg;
+        uint16_t* crow = C + static_cast<size_t>(tc.row0 + row) * ldc + first_column<Cfg>(tc, ldc) + 4 * fp.frag_kg;
 #pragma unroll
         for (int j = 0; j < Cfg::TN; ++j) {
             if (DUAL && (j & P)) continue;
@@ -518,7 +658,7 @@ __device__ __forceinline__ void store_tile(const f32x4 (&acc)[Cfg::TM][Cfg::TN],
             const int col = DUAL ? r0 / (2 * DB) * DB + r0 % DB : r0;
             if constexpr (out_is_f32<Cfg>::value) {
                 float* frow = reinterpret_cast<float*>(C) + static_cast<size_t>(tc.row0 + row) * ldc +
-                              tc.nt * Cfg::BN_OUT + 4 * fp.frag_kg;
+                              first_column<Cfg>(tc, ldc) + 4 * fp.frag_kg;
                 *reinterpret_cast<f32x4*>(frow + col) = acc[i][j];
                 continue;
             }
@@ -639,7 +779,7 @@ struct LoadPlan {
     }
     __device__ __forceinline__ void init_b(const TileCoord& tc, int wave, const uint16_t* B0, const uint16_t* B1,
                                            int N, int K) {
-        const size_t first = (static_cast<size_t>(tc.expert) * N + static_cast<size_t>(tc.nt) * Cfg::BN_OUT) * K;
+        const size_t first = (static_cast<size_t>(tc.expert) * N + first_column<Cfg>(tc, N)) * K;
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b)
             b_base[b] = (Cfg::DUAL && ((wave * LB * Cfg::RPI / Cfg::DB + b) & 1) ? B1 : B0) + first;
@@ -694,7 +834,8 @@ template <class Cfg, class InitA>
 __device__ __forceinline__ void ring_of_stages(const TileCoord& tc, LoadPlan<Cfg>& lp, InitA&& init_a, unsigned char* smem,
                                                int wave, int lane, const uint16_t* __restrict__ B0,
                                                const uint16_t* __restrict__ B1, uint16_t* __restrict__ C, int N,
-                                               int K) {
+                                               int K, const ScalesOf<Cfg>& scales) {
+    constexpr bool I8 = operands_i8<Cfg>::value;
     constexpr int BK = Cfg::BK, TM = Cfg::TM, TN = Cfg::TN, LPW = Cfg::LPW, NSTAGE = Cfg::NSTAGE;
     static_assert(Cfg::KSUB == 2, "two k-substeps a stage");
     const int wm = wave / Cfg::WN, wn = wave % Cfg::WN;
@@ -703,6 +844,8 @@ __device__ __forceinline__ void ring_of_stages(const TileCoord& tc, LoadPlan<Cfg
     const int KT = K / BK;
     lp.init_fixed(wave, lane, K);
     lp.init_b(tc, wave, B0, B1, N, K);
+    // ahead of the others: loads complete in order, and these are counted with none of the stages that are waited for
+    const KeptScales<Cfg> sc = load_scales<Cfg>(scales, tc, wm, wn, lane, N);
     lp.issue_b_all(0, 0);
     init_a();
     lp.issue_a_all(0, 0);
@@ -747,14 +890,14 @@ __device__ __forceinline__ void ring_of_stages(const TileCoord& tc, LoadPlan<Cfg
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = mma16(bfr[0][j], af[0][i], acc[i][j]);
+            for (int j = 0; j < TN; ++j) acc[i][j] = mma16<I8>(bfr[0][j], af[0][i], acc[i][j]);
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = mma16(bfr[1][j], af[1][i], acc[i][j]);
+            for (int j = 0; j < TN; ++j) acc[i][j] = mma16<I8>(bfr[1][j], af[1][i], acc[i][j]);
         stage = (stage + 1 == NSTAGE) ? 0 : stage + 1;
     }
-    store_tile<Cfg>(acc, tc, fp, wm, wn, C, N);
+    store_tile<Cfg>(acc, tc, fp, wm, wn, C, N, sc);
 }
 
 template <class Cfg>
@@ -762,16 +905,16 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_kernel(
     const uint16_t* __restrict__ A, const uint16_t* __restrict__ B0,
     const uint16_t* __restrict__ B1, uint16_t* __restrict__ C,
     const int32_t* __restrict__ offsets, const int32_t* __restrict__ row_index, RowDiv index_div,
-    int E, int N, int K, int spread) {
+    int E, int N, int K, int spread, ScalesOf<Cfg> scales) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    const TileCoord tc = locate_tile<Cfg::BM>(offsets, E, N / Cfg::BN_OUT);
+    const TileCoord tc = tile_of_workgroup<Cfg>(offsets, scales, E, N, 0, Cut::kNever);
     if (tc.expert < 0) return;
     spread_start(spread);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     LoadPlan<Cfg> lp;
     ring_of_stages<Cfg>(tc, lp, [&] { lp.init_a(tc, wave, lane, A, row_index, index_div, K); }, smem, wave, lane, B0, B1,
-                        C, N, K);
+                        C, N, K, scales);
 }
 
 // ---- kernel 1, few tokens: tiles straight from the selected experts ---------------------------
@@ -864,7 +1007,7 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_routed_kernel(
             const int id = list[row];
             return index_div.mul == 0 ? id : static_cast<int>(__umulhi(static_cast<uint32_t>(id), index_div.mul) >> index_div.shift);
         });
-    }, smem, wave, lane, B0, B1, C, N, K);
+    }, smem, wave, lane, B0, B1, C, N, K, NoScales{});
 }
 
 // ---- kernel 2: operand rings of different depth, hand-placed software pipeline ---------------
@@ -1066,7 +1209,7 @@ __device__ __forceinline__ void ring_tile(const TileCoord& tc, unsigned char* sm
         return;
     }
     mfma_drain(acc[TM - 1]);
-    store_tile<Cfg>(acc, tc, fp, wm, wn, C, N);
+    store_tile<Cfg>(acc, tc, fp, wm, wn, C, N, KeptScales<Cfg>{});
 }
 
 // Epilogue of the one-wavefront-per-SIMD tile: the outputs go through LDS so that global memory
@@ -1101,8 +1244,8 @@ template <class Cfg, class Before>
 __device__ __forceinline__ void store_tile_via_lds(const f32x4 (&acc)[Cfg::TM][8], const TileCoord& tc,
                                                    const FragPlan<Cfg>& fp, int wave, int lane,
                                                    unsigned char* stage, uint16_t* __restrict__ C,
-                                                   int ldc, Before&& before_stores) {
-    constexpr bool DUAL = Cfg::DUAL, F32 = out_is_f32<Cfg>::value;
+                                                   int ldc, const KeptScales<Cfg>& sc, Before&& before_stores) {
+    constexpr bool DUAL = Cfg::DUAL, F32 = out_is_f32<Cfg>::value, I8 = operands_i8<Cfg>::value;
     constexpr int WN = Cfg::WN;
     constexpr int PASSES = F32 ? 2 : 1;              // pieces that a fragment row is staged in
     constexpr int COLS = DUAL ? 64 : 128;            // output columns of this wavefront
@@ -1129,14 +1272,30 @@ __device__ __forceinline__ void store_tile_via_lds(const f32x4 (&acc)[Cfg::TM][8
     const __amdgpu_buffer_rsrc_t out = __builtin_amdgcn_make_buffer_rsrc(
         reinterpret_cast<unsigned char*>(C) + static_cast<size_t>(tc.row0 + wm * Cfg::WTM) * row_bytes, 0,
         static_cast<int>(bytes), 0x00027000);
-    const uint32_t ccol = static_cast<uint32_t>(tc.nt * Cfg::BN_OUT + wn * COLS) * ESZ + rchunk * 16;
+    const uint32_t ccol = static_cast<uint32_t>(first_column<Cfg>(tc, ldc) + wn * COLS) * ESZ + rchunk * 16;
     uint32_t coff[16 / RPI];
 #pragma unroll
     for (int q = 0; q < 16 / RPI; ++q) coff[q] = (q * RPI + rrow) * row_bytes + ccol;
+    f32x4 cols[8];                                   // the columns' scales, the same for all rows
+    if constexpr (I8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) cols[j] = sc.of_columns(j, fp.frag_kg);
+    }
     auto write_piece = [&](int u) {
         const int i = u / PASSES, j0 = (u % PASSES) * NJ;
         auto frag = [&](int jj) { return j0 + (DUAL ? (jj & 1) + (jj >> 1) * 4 : jj); };   // gate; up = + 2
-        if constexpr (F32) {
+        float row = 0.f;
+        if constexpr (I8) row = sc.of_row(i, fp.frag_row);
+        if constexpr (F32 && I8) {
+#pragma unroll
+            for (int jj = 0; jj < NJ; ++jj) {
+                f32x4 v;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = scaled(read_acc(acc[i][frag(jj)], r), row, cols[frag(jj)][r]);
+                const uint32_t chunk = (static_cast<uint32_t>(jj * 4 + fp.frag_kg) ^ wswz) * 16;
+                *reinterpret_cast<f32x4*>(wbase + chunk) = v;
+            }
+        } else if constexpr (F32) {
 #pragma unroll
             for (int jj = 0; jj < NJ; ++jj) {
                 const uint32_t chunk = (static_cast<uint32_t>(jj * 4 + fp.frag_kg) ^ wswz) * 16;
@@ -1150,6 +1309,8 @@ __device__ __forceinline__ void store_tile_via_lds(const f32x4 (&acc)[Cfg::TM][8
                 for (int r = 0; r < 4; ++r) {
                     v[jj][r] = read_acc(acc[i][frag(jj)], r);
                     if constexpr (DUAL) up[jj][r] = read_acc(acc[i][frag(jj) + 2], r);
+                    if constexpr (I8) v[jj][r] = scaled(v[jj][r], row, cols[frag(jj)][r]);
+                    if constexpr (I8 && DUAL) up[jj][r] = scaled(up[jj][r], row, cols[frag(jj) + 2][r]);
                 }
 #pragma unroll
             for (int jj = 0; jj < NJ; ++jj) {
@@ -1272,7 +1433,7 @@ __device__ __forceinline__ void start_loads_1w(LoadPlan1W& lp, const TileCoord& 
     }
     row_off *= static_cast<uint32_t>(K) * 2u;
     lp.a_ptr = a_origin(A, tc, row_index, K);
-    const size_t first = (static_cast<size_t>(tc.expert) * N + static_cast<size_t>(tc.nt) * Full::BN_OUT) * K;
+    const size_t first = (static_cast<size_t>(tc.expert) * N + first_column<Full>(tc, N)) * K;
     lp.b_ptr[0] = B0 + first;
     lp.b_ptr[1] = Full::DUAL ? B1 + first : lp.b_ptr[0];
     const uint32_t chunk = static_cast<uint32_t>((lane & 7) ^ swz<64>(wave * 8 + (lane >> 3))) * 16u;
@@ -1293,10 +1454,17 @@ __device__ __forceinline__ void init_b_offsets(LoadPlan1W& lp, int wave, int lan
 
 // acc += W_frag * X_frag with the accumulator pinned to AGPRs; then one direct-to-LDS load whose
 // LDS address (lds_base + LDS_OFF) was put into M0 before the MFMA.
-template <int LDS_OFF>
+template <bool I8, int LDS_OFF>
 __device__ __forceinline__ void mma16_then_dma(const bf16x8& w, const bf16x8& x, f32x4& acc,
                                                uint32_t lds_base, uint32_t voff, const void* sbase) {
-    asm volatile("s_add_u32 m0, %3, %4\n\t"
+    if constexpr (I8)
+        asm volatile("s_add_u32 m0, %3, %4\n\t"
+                     "v_mfma_i32_16x16x64_i8 %0, %1, %2, %0\n\t"
+                     "global_load_lds_dwordx4 %5, %6"
+                     : "+a"(acc)
+                     : "v"(w), "v"(x), "s"(lds_base), "n"(LDS_OFF), "v"(voff), "s"(sbase)
+                     : "memory", "m0", "scc");
+    else asm volatile("s_add_u32 m0, %3, %4\n\t"
                  "v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0\n\t"
                  "global_load_lds_dwordx4 %5, %6"
                  : "+a"(acc)
@@ -1323,14 +1491,14 @@ struct RingState1W {
 
 // MFMA number m of a half-step with its load, if it has one: load n = m / STRIDE goes out behind
 // MFMA m when m % STRIDE == 3 and n < NLOADS; it lands LDS_STEP bytes behind load n - 1.
-template <int M, int STRIDE, int NLOADS, int LDS_STEP>
+template <bool I8, int M, int STRIDE, int NLOADS, int LDS_STEP>
 __device__ __forceinline__ void mma16_slot(const bf16x8& w, const bf16x8& x, f32x4& acc,
                                            uint32_t lds_base, const uint32_t* voff,
                                            const void* sbase) {
     if constexpr (M % STRIDE == 3 && M / STRIDE < NLOADS)
-        mma16_then_dma<(M / STRIDE) * LDS_STEP>(w, x, acc, lds_base, voff[M / STRIDE], sbase);
+        mma16_then_dma<I8, (M / STRIDE) * LDS_STEP>(w, x, acc, lds_base, voff[M / STRIDE], sbase);
     else
-        mma16_agpr(w, x, acc);
+        mma16_agpr<I8>(w, x, acc);
 }
 
 template <class Cfg, class R>
@@ -1340,6 +1508,7 @@ __device__ __forceinline__ void kstep_1w(f32x4 (&acc)[Cfg::TM][8], bf16x8 (&fa)[
                                          const unsigned char* pb0, const unsigned char* pb1) {
     constexpr int TM = Cfg::TM, NM = TM * 8, NR = TM + 8;      // MFMAs and fragment reads per half
     constexpr int LA = TM, LB = R::LB;
+    constexpr bool I8 = operands_i8<Cfg>::value;
     constexpr uint32_t AB = R::AB, BB = R::BB;
     static_assert(TM >= 4 && TM <= 8 && Cfg::TN == 8, "64 to 128 rows x 128 columns per wavefront");
     const uint32_t a_region = rs.a_region, b_region = rs.b_region;
@@ -1365,7 +1534,7 @@ __device__ __forceinline__ void kstep_1w(f32x4 (&acc)[Cfg::TM][8], bf16x8 (&fa)[
     auto first = [&](auto mtag) {
         constexpr int m = decltype(mtag)::value, i = m >> 3, j = m & 7, n = m / (NM / 8);
         const void* src = lp.b_ptr[Cfg::DUAL ? (n >> 2) & 1 : 0];
-        mma16_slot<m, NM / 8, 8, 1024>(fb[0][j], fa[0][i], acc[i][j], b_region, lp.b_voff, src);
+        mma16_slot<I8, m, NM / 8, 8, 1024>(fb[0][j], fa[0][i], acc[i][j], b_region, lp.b_voff, src);
         MOE_FENCE();
         read_behind(mtag, std::integral_constant<int, SPAN1>{}, fb[1], fa[1], pb_h1, pa_h1);
         // the B pointers move on behind the last B load (MFMA 7 * NM / 8 + 3)
@@ -1382,7 +1551,7 @@ __device__ __forceinline__ void kstep_1w(f32x4 (&acc)[Cfg::TM][8], bf16x8 (&fa)[
     RingState1W nx;
     auto second = [&](auto mtag) {
         constexpr int m = decltype(mtag)::value, i = m >> 3, j = m & 7;
-        mma16_slot<m, 8, LA, 4096>(fb[1][j], fa[1][i], acc[i][j], a_region, lp.a_voff, lp.a_ptr);
+        mma16_slot<I8, m, 8, LA, 4096>(fb[1][j], fa[1][i], acc[i][j], a_region, lp.a_voff, lp.a_ptr);
         MOE_FENCE();
         read_behind(mtag, std::integral_constant<int, NM>{}, fb[0], fa[0], pb_n0, pa_n0);
         if constexpr (m == 1) { sb1 = rs.sb + BB; MOE_FENCE(); }
@@ -1408,20 +1577,21 @@ __device__ __forceinline__ void kstep_1w(f32x4 (&acc)[Cfg::TM][8], bf16x8 (&fa)[
     rs = nx;
 }
 
-// One tile of a persistent workgroup. On entry its first two k-steps are in the rings (stages 0 and 1 of
-// A, sb and the one behind it of B) and every wavefront knows it; on return those of the next tile are
-// in the rings or on their way, sb is its B stage, and the stores of this one are on their way.
+// One tile of a persistent workgroup. On entry its first two k-steps are in the rings (stages sa and the other one
+// of A, sb and the one behind it of B) and every wavefront knows it; on return those of the next tile are
+// in the rings or on their way, sa and sb are its stages, and the stores of this one are on their way.
+//   ODD       the reduction has an odd number of k-steps (sa is 0 for every tile where it has not)
 //   lp        loads of this tile at k-step 2, then of the next one
 //   nxt       the next tile, id as for start_loads_1w; this one if it is the last
 //   draw      called once in each wavefront two k-steps before the end; drawn() before the first store, when
 //             all loads of the wavefront have landed
-template <class Cfg, class Full, class Draw, class Drawn>
+template <class Cfg, class Full, bool ODD, class Draw, class Drawn>
 __device__ __forceinline__ void ring_tile_1w(const TileCoord& tc, const TileCoord& nxt, LoadPlan1W& lp,
-                                             int id, bool last, uint32_t& sb, unsigned char* smem, int wave, int lane,
+                                             int id, bool last, uint32_t& sa, uint32_t& sb, unsigned char* smem, int wave, int lane,
                                              const uint16_t* __restrict__ A, const uint16_t* __restrict__ B0,
                                              const uint16_t* __restrict__ B1, uint16_t* __restrict__ C,
                                              const int32_t* __restrict__ row_index, RowDiv index_div, int N, int K,
-                                             Draw&& draw, Drawn&& drawn) {
+                                             const ScalesOf<Full>& scales, Draw&& draw, Drawn&& drawn) {
     using R = Ring1W<Full>;
     constexpr int TM = Cfg::TM, TN = Cfg::TN;
     constexpr uint32_t AB = R::AB, BB = R::BB;
@@ -1431,11 +1601,12 @@ __device__ __forceinline__ void ring_tile_1w(const TileCoord& tc, const TileCoor
     const unsigned char* pa[2] = {smem + fp.a_off[0], smem + fp.a_off[1]};
     const unsigned char* pb[2] = {smem + R::A_RING + (fp.b_off[0] - Cfg::A_BYTES),
                                   smem + R::A_RING + (fp.b_off[1] - Cfg::A_BYTES)};
+    const KeptScales<Cfg> sc = load_scales<Cfg>(scales, tc, wave / Cfg::WN, wave % Cfg::WN, lane, N);
     bf16x8 fa[2][TM], fb[2][TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) fb[0][j] = lds16(pb[0] + sb + j * Cfg::TILE_STEP);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) fa[0][i] = lds16(pa[0] + i * Cfg::TILE_STEP);
+    for (int i = 0; i < TM; ++i) fa[0][i] = lds16(pa[0] + sa + i * Cfg::TILE_STEP);
     MOE_FENCE();
     // The accumulators start as the result of an MFMA, 0 * 0 + 0, not as ordinary register
     // writes: the compiler may sink those to just in front of the k-loop, where it cannot
@@ -1452,11 +1623,15 @@ __device__ __forceinline__ void ring_tile_1w(const TileCoord& tc, const TileCoor
                 asm volatile("v_mfma_f32_4x4x4_16b_bf16 %0, %1, %1, 0" : "=a"(acc[i][j]) : "v"(zero));
     }
     const uint32_t sb_next = sb + BB == R::NB * BB ? 0u : sb + BB;
-    RingState1W rs{pa[1], pb[1] + sb, pa[0] + AB, pb[0] + sb_next, wave * 1024u,
-                   R::A_RING + (sb == 0 ? (R::NB - 1) * BB : sb - BB) + wave * (R::LB * 1024u), 0u, sb};
-    // two k-steps per trip (K is a multiple of 128 for every supported shape): the loop's own
+    RingState1W rs{pa[1] + sa, pb[1] + sb, pa[0] + (sa ^ AB), pb[0] + sb_next, sa + wave * 1024u,
+                   R::A_RING + (sb == 0 ? (R::NB - 1) * BB : sb - BB) + wave * (R::LB * 1024u), sa, sb};
+    // two k-steps per trip (K is a multiple of 128, or one more k-step goes ahead of the loop): the loop's own
     // compare-and-branch then falls between MFMAs half as often
     int left = K / Cfg::BK - 2;                      // k-steps whose loads are this tile's
+    if constexpr (ODD) {
+        kstep_1w<Cfg, R>(acc, fa, fb, rs, lp, wave, pa[0], pa[1], pb[0], pb[1]);
+        --left;
+    }
     for (;; left -= 2) {
         if (left == 0) {                             // from here on the loads are the next tile's
             if (last) {                              // or the last two k-steps again, from L2 and to no use
@@ -1473,14 +1648,15 @@ __device__ __forceinline__ void ring_tile_1w(const TileCoord& tc, const TileCoor
         if (left == 0) break;
     }
     mfma_drain(acc[TM - 1]);                         // before anything else touches the accumulators
+    if constexpr (ODD) sa = rs.sa;                   // A stage of the next tile's first k-step
     sb = rs.sb;                                      // B stage of the next tile's first k-step
     // rows of a higher next tile that this one's loads did not reach, of both its k-steps
     if constexpr (TM < 8) {
         if (!last && nxt.height > Cfg::BM) {
 #pragma unroll
             for (int i = TM; i < 8; ++i) {
-                dma16(lp.a_ptr - 2 * Cfg::BK, lp.a_voff[i], wave * 1024 + i * 4096);
-                dma16(lp.a_ptr - Cfg::BK, lp.a_voff[i], AB + wave * 1024 + i * 4096);
+                dma16(lp.a_ptr - 2 * Cfg::BK, lp.a_voff[i], sa + wave * 1024 + i * 4096);
+                dma16(lp.a_ptr - Cfg::BK, lp.a_voff[i], (sa ^ AB) + wave * 1024 + i * 4096);
             }
         }
     }
@@ -1488,7 +1664,7 @@ __device__ __forceinline__ void ring_tile_1w(const TileCoord& tc, const TileCoor
     // next load into it is the next tile's first. A wavefront stages its outputs in the 8 KB that it will
     // then fill by itself.
     unsigned char* idle = smem + R::A_RING + (sb == 0 ? (R::NB - 1) * BB : sb - BB);
-    store_tile_via_lds<Cfg>(acc, tc, fp, wave, lane, idle + wave * (R::LB * 1024), C, N, [&] {
+    store_tile_via_lds<Cfg>(acc, tc, fp, wave, lane, idle + wave * (R::LB * 1024), C, N, sc, [&] {
         __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): the next tile's first loads, and what draw() asked for
         drawn(idle);
     });
@@ -1506,28 +1682,33 @@ constexpr int kCounterInts = 32;                     // a counter per XCD, on a 
 // range. Draws: of a range of S slots, S - 2 P are drawn, and every workgroup that has a second tile, min(P, S - P) of
 // them, draws until it is past the end: S - P draws in all, whose last one sets the counter back to zero for
 // the next launch.
-template <class Cfg, bool PERSISTENT>
+template <class Cfg, bool PERSISTENT, bool ODD = false>
 __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_1w_kernel(
     const uint16_t* __restrict__ A, const uint16_t* __restrict__ B0,
     const uint16_t* __restrict__ B1, uint16_t* __restrict__ C,
     const int32_t* __restrict__ offsets, const int32_t* __restrict__ row_index, RowDiv index_div,
-    int E, int N, int K, int split_cus, int32_t* __restrict__ counters) {
+    int E, int N, int K, int split_cus, int32_t* __restrict__ counters, ScalesOf<Cfg> scales) {
     using R = Ring1W<Cfg>;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int xcd = blockIdx.x % kXcds, workgroups = gridDim.x / kXcds;
     int32_t* counter = counters + xcd * kCounterInts;
-    const int NT = N / Cfg::BN_OUT;
+    const int NT = n_tiles<Cfg>(N);
     const Cut cut = K < kLongK ? Cut::kAlways : Cut::kLong;
     TileTable<Cfg::BM> table;                        // kept over the tiles: a lookup then reads no memory
     TileCoord tc;
     const uint32_t magic = division_magic(lane);
     if constexpr (PERSISTENT) {
-        table.init(offsets, E, NT, split_cus, xcd, lane);
+        bool one = false;
+        if constexpr (operands_i8<Cfg>::value) {
+            one = offsets == nullptr;
+            if (one) table.init_one(scales.rows, NT, split_cus, xcd, lane);
+        }
+        if (!one) table.init(offsets, E, NT, split_cus, xcd, lane);
         tc = uniform_tile(table.find(NT, cut, blockIdx.x / kXcds, magic));
     } else {
-        tc = locate_tile<Cfg::BM>(offsets, E, NT, split_cus, cut);
+        tc = tile_of_workgroup<Cfg>(offsets, scales, E, N, split_cus, cut);
     }
     if (PERSISTENT ? tc.expert == kNoTile : tc.expert < 0) return;     // uniform for the whole workgroup
     // to a persistent one an empty slot is a tile without rows and without k-steps: it has to go on to its next one
@@ -1555,8 +1736,8 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_1w_kernel(
         return row_index != nullptr ? row_index[t.row0 + a_row_1w(t, wave, lane)] : offsets[0];
     };
     LoadPlan1W lp;
-    uint32_t sb = 0;
-    // the first two k-steps of tile t into the rings: stages 0 and 1 of A, sb and the one behind it of B
+    uint32_t sa = 0, sb = 0;
+    // the first two k-steps of tile t into the rings: stages sa and the other one of A, sb and the one behind it of B
     auto first_loads = [&](const TileCoord& t, int id) {
         start_loads_1w<Cfg>(lp, t, id, wave, lane, A, B0, B1, row_index, index_div, N, K);
 #pragma unroll
@@ -1564,7 +1745,7 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_1w_kernel(
             const uint32_t b_stage = s == 0 ? sb : sb + R::BB == R::NB * R::BB ? 0u : sb + R::BB;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (i < 4 || i * 32 < t.height) dma16(lp.a_ptr, lp.a_voff[i], s * R::AB + wave * 1024 + i * 4096);
+                if (i < 4 || i * 32 < t.height) dma16(lp.a_ptr, lp.a_voff[i], (s == 0 ? sa : sa ^ R::AB) + wave * 1024 + i * 4096);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 dma16(lp.b_ptr[Cfg::DUAL ? i >> 2 : 0], lp.b_voff[i], R::A_RING + b_stage + wave * (R::LB * 1024) + i * 1024);
@@ -1601,8 +1782,8 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_1w_kernel(
         const int id = row_id(nxt);
         auto run = [&](auto cfg_tag) {
             using TileCfg = typename decltype(cfg_tag)::type;
-            ring_tile_1w<TileCfg, Cfg>(tc, nxt, lp, id, last, sb, smem, wave, lane, A, B0, B1, C, row_index, index_div,
-                                       N, K, draw, drawn);
+            ring_tile_1w<TileCfg, Cfg, ODD>(tc, nxt, lp, id, last, sa, sb, smem, wave, lane, A, B0, B1, C, row_index, index_div,
+                                       N, K, scales, draw, drawn);
         };
         if (PERSISTENT && tc.rows == 0) {            // nothing to compute: the next tile's first loads, as at the start
             wait_vmcnt<0>();                         // this one's have landed where they go

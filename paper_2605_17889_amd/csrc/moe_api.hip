@@ -26,6 +26,9 @@ struct moe_ctx {
     moe_bf16* H;         // [R_max, f]
     moe_bf16* y_perm;    // [R_max, d]
     float* y_perm_f32;   // [R_max, d], allocated by moe_set_expert_output_fp32; null = keep bf16
+    // 8-bit experts (created by the first call of them, kept until destroy): H in 8 bits [R_max, f] and its scales [R_max]
+    moe_i8* h_i8;
+    float* h_scale;
     // profiling
     bool prof_armed;
     int prof_max_calls, prof_calls;
@@ -183,6 +186,19 @@ int forward_chunk(moe_ctx* c, const moe_bf16* x, const float* w_router, const fl
     });
 }
 
+int ensure_i8(moe_ctx* c) {
+    if (c->h_i8) return MOE_OK;
+    const size_t rows = static_cast<size_t>(c->shape.T_max) * c->shape.k, bytes = align_up(rows * c->shape.d_ff);
+    void* p = nullptr;
+    if (hipMalloc(&p, bytes + rows * sizeof(float)) != hipSuccess) {
+        (void)hipGetLastError();
+        return MOE_ERR_WORKSPACE;
+    }
+    c->h_i8 = static_cast<moe_i8*>(p);
+    c->h_scale = reinterpret_cast<float*>(c->h_i8 + bytes);
+    return MOE_OK;
+}
+
 int ensure_streaming(moe_ctx* c) {
     if (c->copy_stream) return MOE_OK;
     const size_t bytes = static_cast<size_t>(3) * c->shape.d_model * c->shape.d_ff * sizeof(moe_bf16);
@@ -287,6 +303,8 @@ int moe_create(moe_ctx** out, const moe_shape* shape, int device_id) {
     c->H = reinterpret_cast<moe_bf16*>(c->base + L.H);
     c->y_perm = reinterpret_cast<moe_bf16*>(c->base + L.y_perm);
     c->y_perm_f32 = nullptr;
+    c->h_i8 = nullptr;
+    c->h_scale = nullptr;
     c->gemm.tile_counters = counters;
     c->prof_armed = false;
     c->prof_max_calls = c->prof_calls = 0;
@@ -313,6 +331,7 @@ int moe_destroy(moe_ctx* c) {
     }
     if (c->slot[0] && hipFree(c->slot[0]) != hipSuccess) rc = MOE_ERR_HIP;
     if (c->y_perm_f32 && hipFree(c->y_perm_f32) != hipSuccess) rc = MOE_ERR_HIP;
+    if (c->h_i8 && hipFree(c->h_i8) != hipSuccess) rc = MOE_ERR_HIP;
     if (c->base && hipFree(c->base) != hipSuccess) rc = MOE_ERR_HIP;
     give_tile_counters(c->device, c->counter_set);
     delete c;
@@ -648,6 +667,40 @@ int moe_quantize_i8(const moe_bf16* x, int64_t x_stride, int32_t T, int32_t d, m
     if (T == 0) return MOE_OK;
     if (!x || !q || !q_scale) return MOE_ERR_INVALID_ARG;
     return launch_quantize_i8(x, x_stride, T, d, q, q_scale, static_cast<hipStream_t>(stream));
+}
+
+int moe_gemm_i8(moe_ctx* c, const moe_i8* x, const float* x_scale, const int32_t* offsets, int32_t R, int32_t E, int32_t N,
+                int32_t K, const moe_i8* W, const float* w_scale, void* out, int out_type, void* stream) {
+    if (!c || R < 0 || static_cast<long long>(R) > static_cast<long long>(c->shape.T_max) * c->shape.k)
+        return MOE_ERR_INVALID_ARG;
+    if (!on_own_device(c) || E < 1 || N < 1 || K < 1 || (!offsets && E != 1)) return MOE_ERR_INVALID_ARG;
+    if (out_type != MOE_OUT_BF16 && out_type != MOE_OUT_FP32) return MOE_ERR_INVALID_ARG;
+    if (E > kMaxExperts || N % 16 != 0 || N < 32 || N > kMaxDimI8 || K % 128 != 0 || K > kMaxSumI8) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (R == 0) return MOE_OK;
+    if (!x || !x_scale || !W || !w_scale || !out) return MOE_ERR_INVALID_ARG;
+    return launch_product_i8(c->gemm, x, x_scale, offsets, R, N, K, E, W, w_scale, out, out_type == MOE_OUT_FP32,
+                             static_cast<hipStream_t>(stream));
+}
+
+int moe_expert_ffn_i8(moe_ctx* c, const moe_i8* x_perm, const float* x_scale, const int32_t* offsets, int32_t R,
+                      const moe_i8* W1, const float* w1_scale, const moe_i8* W3, const float* w3_scale, const moe_i8* W2,
+                      const float* w2_scale, moe_bf16* y_perm, void* stream) {
+    if (!c || R < 0 || static_cast<long long>(R) > static_cast<long long>(c->shape.T_max) * c->shape.k)
+        return MOE_ERR_INVALID_ARG;
+    if (!on_own_device(c)) return MOE_ERR_INVALID_ARG;
+    const moe_shape& sh = c->shape;
+    if (sh.d_model > kMaxSumI8 || sh.d_ff > kMaxRowI8) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (R == 0) return MOE_OK;
+    if (!x_perm || !x_scale || !offsets || !W1 || !w1_scale || !W3 || !w3_scale || !W2 || !w2_scale || !y_perm)
+        return MOE_ERR_INVALID_ARG;
+    int rc = ensure_i8(c);
+    if (rc != MOE_OK) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    rc = launch_gateup_i8(c->gemm, x_perm, x_scale, offsets, R, sh.d_model, sh.d_ff, sh.E, W1, w1_scale, W3, w3_scale, c->H, s);
+    if (rc != MOE_OK) return rc;
+    rc = launch_quantize_i8(c->H, sh.d_ff, R, sh.d_ff, c->h_i8, c->h_scale, s);
+    if (rc != MOE_OK) return rc;
+    return launch_product_i8(c->gemm, c->h_i8, c->h_scale, offsets, R, sh.d_model, sh.d_ff, sh.E, W2, w2_scale, y_perm, false, s);
 }
 
 }  // extern "C"

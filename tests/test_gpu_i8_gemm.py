@@ -1,0 +1,382 @@
+"""Products in 8-bit integers with scales, moe_gemm_i8 and moe_expert_ffn_i8, against their definitions in 64 bits.
+
+Tolerances, counted in roundings (half a step: 2^-24 in fp32, 2^-8 in bf16, relative to the value):
+  product   the sum is exact; its conversion to fp32 and the two scales are three roundings (THREE), then the output's own
+  H         gate and up carry THREE each; SiLU's exponential turns a relative error of g into one of |g| times as much and
+            adds that of its own argument (g times log2 e: 2 roundings, again times |g|); exponential, sum, reciprocal (1 step
+            each, 2 roundings) and two products: at most 3 + 3 + 8 + 5 |g| roundings, rounded up to 16 + 6 |g|. H and the
+            8-bit rows are rounded values: an element that lies within that of a border may land on either side, all others
+            are what 64 bits give. near_borders() adds up what the former can do to an output.
+"""
+import pytest
+import torch
+
+from paper_2605_17889_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+HALF32, HALF16 = 2.0 ** -24, 2.0 ** -8
+THREE = 3 * HALF32 * (1 + HALF32) ** 2
+TINY = 2.0 ** -126
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def whole(g, *shape):
+    return torch.randint(-127, 128, shape, generator=g, device="cuda", dtype=torch.int8)
+
+
+def positive(g, *shape):
+    return torch.rand(shape, generator=g, device="cuda") * 0.02 + 1e-4
+
+
+def groups(counts):
+    offsets = torch.zeros(len(counts) + 1, dtype=torch.int32)
+    offsets[1:] = torch.tensor(counts).cumsum(0)
+    return offsets.cuda()
+
+
+def product64(x, xs, w, ws):
+    return (x.double() @ w.double().t()) * xs.double()[:, None] * ws.double()[None, :]
+
+
+def assert_near(got, want, half, extra=0.0):
+    off = (got.double() - want).abs() - (want.abs() * (THREE + half) * (1 + half) + TINY + extra)
+    assert off.numel() == 0 or off.max().item() <= 0, f"off by {off.max().item():.3g} more than allowed"
+
+
+def half_of(dtype):
+    return HALF32 * 0 if dtype == torch.float32 else HALF16
+
+
+def gemm_case(counts, N, K, dtype, seed=0, dense=False, config=None):
+    g = gen(seed)
+    R, E = sum(counts), len(counts)
+    x, xs, w, ws = whole(g, R, K), positive(g, R), whole(g, E, N, K), positive(g, E, N)
+    out = torch.full((R + 3, N), 7.0, dtype=dtype, device="cuda")
+    ctx = B.MoeContext(R, 512, 128, 1, 1)
+    if config is not None:
+        B.moe_set_gemm_config(ctx, config)
+    say(f"gemm_i8 rows={counts} N={N} K={K} {dtype} config={config} dense={dense}")
+    B.moe_gemm_i8(ctx, x, xs, None if dense else groups(counts), R, E, N, K, w, ws, out[:R])
+    torch.cuda.synchronize()
+    at = 0
+    for e, n in enumerate(counts):
+        assert_near(out[at:at + n], product64(x[at:at + n], xs[at:at + n], w[e], ws[e]), half_of(dtype))
+        at += n
+    assert (out[R:] == 7).all(), "rows past the last group were written"
+    ctx.close()
+    return out[:R]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 31, 33, 64, 65, 100, 127, 128, 129, 300, 513])
+def test_one_matrix(T, dtype):
+    gemm_case([T], 384, 640, dtype, seed=T, dense=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,K", [(32, 128), (48, 128), (112, 256), (128, 384), (144, 1408), (256, 2048), (272, 128),
+                                 (496, 512), (768, 896), (2064, 1152), (32000, 256)])
+@pytest.mark.parametrize("T", [1, 7, 40, 90, 260, 700])
+def test_widths_and_reductions(T, N, K, dtype):
+    gemm_case([T], N, K, dtype, seed=N + K, dense=True)
+
+
+def test_one_group_with_offsets_is_the_matrix_without():
+    for T in (1, 40, 600, 3000):
+        a = gemm_case([T], 528, 1280, torch.bfloat16, seed=T, dense=True)
+        b = gemm_case([T], 528, 1280, torch.bfloat16, seed=T)
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("counts", [[0, 1, 0], [3, 0, 0, 9, 1], [16, 17, 0, 200, 1, 31, 64, 5], [0] * 40 + [2] + [0] * 87,
+                                    [257, 0, 255, 512, 1, 700], [33] * 20, [0] * 255 + [600]])
+def test_groups_of_experts(counts, dtype):
+    for N, K in ((176, 384), (512, 1408)):
+        gemm_case(counts, N, K, dtype, seed=len(counts))
+
+
+@pytest.mark.parametrize("config", [0, 1, 2, 3, 4, 16, 17, 18, 19, 20, 33, 34, 35, 36, 128, 256, 512])
+def test_every_tile_gives_the_same_bits(config):
+    """Sums of whole numbers: no tile and no order of them changes a bit."""
+    for counts, N, K in (([5, 0, 300, 40], 640, 896), ([700], 1024, 1024)):
+        for dtype in (torch.bfloat16, torch.float32):
+            want = gemm_case(counts, N, K, dtype, seed=5)
+            got = gemm_case(counts, N, K, dtype, seed=5, config=config)
+            assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("T,N,K", [(2100, 4096, 512), (4096, 2304, 640), (9000, 1040, 1408), (5000, 2048, 8192), (1300, 5120, 4224)])
+def test_large_tiles(T, N, K):
+    """Several rounds of tiles, persistent workgroups with an even and an odd number of k-steps, and long reductions."""
+    for dtype in (torch.bfloat16, torch.float32):
+        gemm_case([T], N, K, dtype, seed=T, dense=True)
+        gemm_case([T // 3, 0, T // 2, T - T // 3 - T // 2], N, K, dtype, seed=T)
+
+
+def test_sums_at_the_ends_of_the_range():
+    """The longest reduction, all products alike: sums of 2^31 - 2^21 and -2^31 + 2^24 or so, exactly."""
+    K, N = 130944, 32
+    for a, b in ((-128, -128), (-128, 127), (127, 127)):
+        x = torch.full((3, K), a, dtype=torch.int8, device="cuda")
+        w = torch.full((N, K), b, dtype=torch.int8, device="cuda")
+        out = torch.empty((3, N), device="cuda")
+        ctx = B.MoeContext(3, 512, 128, 1, 1)
+        B.moe_gemm_i8(ctx, x, torch.ones(3, device="cuda"), None, 3, 1, N, K, w, torch.ones(N, device="cuda"), out)
+        assert (out == float(torch.tensor(a * b * K, dtype=torch.float32))).all()
+        ctx.close()
+
+
+def test_scales_of_any_size_and_bad_rows():
+    """Scales multiply one after the other: no product of two scales that leaves the range on its way. NaN stays in its row."""
+    g = gen(3)
+    R, N, K = 70, 64, 256
+    x, w = whole(g, R, K), whole(g, N, K)
+    xs, ws = positive(g, R), positive(g, N)
+    xs[3], xs[5], xs[9], xs[11] = 0.0, float("nan"), 1e-36, 1e30
+    x[5] = 0
+    ws[7], ws[8] = 1e-38, 0.0
+    out = torch.empty((R, N), device="cuda")
+    ctx = B.MoeContext(R, 512, 128, 1, 1)
+    B.moe_gemm_i8(ctx, x, xs, None, R, 1, N, K, w, ws, out)
+    assert out[5].isnan().all() and (out[3] == 0).all()
+    ok = [r for r in range(R) if r != 5]
+    want = product64(x[ok], xs[ok], w, ws)
+    off = (out[ok].double() - want).abs() - (want.abs() * THREE + 2.0 ** -125)
+    assert off.max().item() <= 0
+    ctx.close()
+
+
+# ------------------------------------------------------------------------------- experts
+
+def rows8(h):
+    peak = h.abs().amax(1)
+    return torch.where(peak[:, None] > 0, (h * 127 / peak[:, None].clamp(min=1e-300)).round(), 0.0), peak / 127
+
+
+def near_borders(g, u, h, w2, s2):
+    """What elements of H and of its rows in 8 bits that lie next to a border can move an output by: [rows, d]."""
+    delta = (16 + 6 * g.abs()) * HALF32
+    exact = g * torch.sigmoid(g) * u
+    lo, hi = ((exact * (1 + s * delta)).to(torch.bfloat16).double() for s in (-1, 1))
+    moved = torch.maximum((lo - h).abs(), (hi - h).abs())
+    peak = h.abs().amax(1, keepdim=True)
+    sure = torch.where(h.abs() == peak, moved, 0.0).amax(1) == 0      # the row's scale is what 64 bits give
+    sure &= ((h.abs() + moved) <= peak).all(1)
+    t = h * 127 / peak.clamp(min=1e-300)
+    tie = ((t - t.floor()) - 0.5).abs() <= 127 * 4 * HALF32
+    step = peak / 127
+    each = torch.where((moved > 0) | tie, moved + step, 0.0)
+    each = torch.where(sure[:, None], each, moved + 1.02 * step)      # another scale: every element may round otherwise
+    return each @ w2.double().abs().t() * s2.double()[None, :] * 1.01
+
+
+def ffn_case(counts, d, f, k=1, seed=0, config=None, ctx=None, check=True, spread=1.0):
+    g = gen(seed)
+    E, R = len(counts), sum(counts)
+    x, xs = whole(g, R, d), positive(g, R) * spread
+    w = {n: (whole(g, E, *s), positive(g, E, s[0]) * (0.5 / (d if n != "w2" else f) ** 0.5))
+         for n, s in (("w1", (f, d)), ("w3", (f, d)), ("w2", (d, f)))}
+    y = torch.full((R + 2, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    own = ctx is None
+    if own:
+        ctx = B.MoeContext((R + k - 1) // k, d, f, E, k)
+    if config is not None:
+        B.moe_set_gemm_config(ctx, config)
+    say(f"expert_ffn_i8 rows={counts if E < 20 else (E, R)} d={d} f={f} config={config}")
+    B.moe_expert_ffn_i8(ctx, x, xs, groups(counts), R, *w["w1"], *w["w3"], *w["w2"], y[:R])
+    torch.cuda.synchronize()
+    assert (y[R:] == 7).all()
+    at = 0
+    for e, n in enumerate(counts if check else []):
+        if n:
+            rows = slice(at, at + n)
+            gate = product64(x[rows], xs[rows], w["w1"][0][e], w["w1"][1][e])
+            up = product64(x[rows], xs[rows], w["w3"][0][e], w["w3"][1][e])
+            h = (gate * torch.sigmoid(gate) * up).to(torch.bfloat16).double()
+            q, s = rows8(h)
+            want = (q @ w["w2"][0][e].double().t()) * s[:, None] * w["w2"][1][e].double()[None, :]
+            extra = near_borders(gate, up, h, w["w2"][0][e], w["w2"][1][e]) + 3 * HALF32 * want.abs()
+            assert_near(y[rows], want, HALF16, extra)
+        at += n
+    if own:
+        ctx.close()
+    return y[:R]
+
+
+@pytest.mark.parametrize("counts,d,f", [
+    ([1], 512, 128), ([0, 1, 0, 0], 512, 256), ([2, 0, 17, 40], 512, 1408), ([16] * 8, 1024, 384), ([33, 1, 64, 5], 1024, 896),
+    ([100, 0, 70], 512, 640), ([300, 200], 1024, 1024), ([1000, 3], 512, 2048), ([0, 2500, 700], 1536, 768),
+    ([1, 0] * 64, 2048, 768), ([9] * 64, 2048, 1408), ([120] * 16, 512, 128)])
+def test_experts(counts, d, f):
+    ffn_case(counts, d, f, seed=sum(counts))
+
+
+def test_experts_with_large_gates():
+    """|g| of some tens: SiLU between nothing and g itself."""
+    ffn_case([40, 3], 512, 256, seed=9, spread=40.0)
+
+
+@pytest.mark.parametrize("config", [0, 1, 2, 3, 4, 17, 18, 19, 20, 33, 34, 35, 36])
+def test_experts_in_every_tile(config):
+    want = ffn_case([5, 0, 300, 40], 1024, 640, seed=5)
+    got = ffn_case([5, 0, 300, 40], 1024, 640, seed=5, config=config, check=False)
+    assert torch.equal(got, want)
+
+
+def test_rows_of_nothing_and_rows_of_nan():
+    """A row of zeros gives zeros, a row whose scale is NaN gives NaN, and the others are what they are without them."""
+    g = gen(4)
+    d, f, E, R = 512, 256, 2, 40
+    x, xs = whole(g, R, d), positive(g, R)
+    w1, w3, w2 = whole(g, E, f, d), whole(g, E, f, d), whole(g, E, d, f)
+    s1, s3, s2 = positive(g, E, f) / 20, positive(g, E, f) / 20, positive(g, E, d) / 20
+    offsets = groups([25, 15])
+    ctx = B.MoeContext(R, d, f, E, 1)
+    clean, y = (torch.empty((R, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    B.moe_expert_ffn_i8(ctx, x, xs, offsets, R, w1, s1, w3, s3, w2, s2, clean)
+    x, xs = x.clone(), xs.clone()
+    x[3] = 0
+    xs[30] = 0
+    x[7], xs[7] = 0, float("nan")
+    B.moe_expert_ffn_i8(ctx, x, xs, offsets, R, w1, s1, w3, s3, w2, s2, y)
+    assert not y[3].any() and not y[30].any() and y[7].isnan().all()
+    keep = [r for r in range(R) if r not in (3, 7, 30)]
+    assert torch.equal(y[keep], clean[keep])
+    ctx.close()
+
+
+def test_same_context_other_calls_and_streams():
+    """Calls of other sizes in turn on one context, on a stream of their own: each gives what it gives alone."""
+    alone = [ffn_case(c, 1024, 384, seed=i) for i, c in enumerate(([40, 0, 9], [1, 1, 1], [900, 30, 200]))]
+    ctx = B.MoeContext(2000, 1024, 384, 3, 1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            for i, c in enumerate(([40, 0, 9], [1, 1, 1], [900, 30, 200])):
+                assert torch.equal(ffn_case(c, 1024, 384, seed=i, ctx=ctx, check=False), alone[i])
+    ctx.close()
+
+
+@pytest.mark.parametrize("counts", [[1, 0, 3], [200, 0, 900]])
+def test_graph_replays(counts):
+    d, f = 512, 640
+    g = gen(11)
+    E, R = len(counts), sum(counts)
+    x, xs = whole(g, R, d), positive(g, R)
+    w1, w3, w2 = whole(g, E, f, d), whole(g, E, f, d), whole(g, E, d, f)
+    s1, s3, s2 = positive(g, E, f) / 20, positive(g, E, f) / 20, positive(g, E, d) / 20
+    offsets = groups(counts)
+    ctx = B.MoeContext(R, d, f, E, 1)
+    y, logits = torch.empty((R, d), dtype=torch.bfloat16, device="cuda"), torch.empty((R, f), device="cuda")
+
+    def call():
+        B.moe_expert_ffn_i8(ctx, x, xs, offsets, R, w1, s1, w3, s3, w2, s2, y)
+        B.moe_gemm_i8(ctx, x, xs, None, R, 1, f, d, w1[:1], s1[:1], logits)
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(4):
+        x.copy_(whole(g, R, d))
+        call()
+        want = y.clone(), logits.clone()
+        y.zero_()
+        logits.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(logits, want[1])
+    ctx.close()
+
+
+def test_offsets_past_32_bits():
+    """Weights and outputs of more than 2^32 bytes: the last rows and columns are what a call of them alone gives."""
+    K, N, E = 2048, 16384, 160                           # 5.4e9 elements of weights
+    w = torch.empty((E, N, K), dtype=torch.int8, device="cuda")
+    for e in range(E):
+        w[e] = whole(gen(e % 3), N, K)
+    ws = positive(gen(1), E, N)
+    counts = [0] * E
+    counts[0], counts[79], counts[E - 1] = 5, 3, 20
+    R = sum(counts)
+    x, xs = whole(gen(2), R, K), positive(gen(3), R)
+    out = torch.empty((R, N), dtype=torch.bfloat16, device="cuda")
+    ctx = B.MoeContext(R, 512, 128, 1, 1)
+    B.moe_gemm_i8(ctx, x, xs, groups(counts), R, E, N, K, w, ws, out)
+    at = 0
+    for e, n in enumerate(counts):
+        if n:
+            assert_near(out[at:at + n], product64(x[at:at + n], xs[at:at + n], w[e], ws[e]), HALF16)
+        at += n
+    ctx.close()
+    del w
+    T, N, K = 70000, 32768, 512                          # 2.3e9 outputs, 9.2e9 bytes
+    x, xs, w, ws = whole(gen(4), T, K), positive(gen(5), T), whole(gen(6), N, K), positive(gen(7), N)
+    out = torch.empty((T, N), device="cuda")
+    ctx = B.MoeContext(T, 512, 128, 1, 1)
+    B.moe_gemm_i8(ctx, x, xs, None, T, 1, N, K, w, ws, out)
+    for rows in (slice(0, 40), slice(32760, 32790), slice(T - 40, T)):
+        assert_near(out[rows], product64(x[rows], xs[rows], w, ws), 0.0)
+    ctx.close()
+
+
+def test_no_rows():
+    ctx = B.MoeContext(4, 512, 128, 2, 1)
+    empty = lambda *s, dtype=torch.int8: torch.empty(s, dtype=dtype, device="cuda")
+    f32 = torch.float32
+    offsets = torch.zeros(3, dtype=torch.int32, device="cuda")
+    B.moe_gemm_i8(ctx, empty(0, 256), empty(0, dtype=f32), None, 0, 1, 64, 256, empty(64, 256), empty(64, dtype=f32),
+                  empty(0, 64, dtype=f32))
+    B.moe_expert_ffn_i8(ctx, empty(0, 512), empty(0, dtype=f32), offsets, 0, empty(2, 128, 512), empty(2, 128, dtype=f32),
+                        empty(2, 128, 512), empty(2, 128, dtype=f32), empty(2, 512, 128), empty(2, 512, dtype=f32),
+                        empty(0, 512, dtype=torch.bfloat16))
+    torch.cuda.synchronize()
+    ctx.close()
+
+
+def test_refusals():
+    ctx = B.MoeContext(8, 512, 128, 2, 1)
+    g = gen(0)
+
+    def gemm(R=8, E=1, N=64, K=256, offsets=None, **other):
+        a = dict(x=whole(g, R, K), x_scale=positive(g, R), W=whole(g, E, N, K), w_scale=positive(g, E, N),
+                 out=torch.empty((R, N), device="cuda"))
+        a.update(other)
+        B.moe_gemm_i8(ctx, a["x"], a["x_scale"], offsets, R, E, N, K, a["W"], a["w_scale"], a["out"])
+
+    gemm()
+    for bad in (dict(R=9), dict(E=2), dict(N=40), dict(N=16), dict(K=192), dict(K=64), dict(K=131072, N=32), dict(x=None),
+                dict(W=None), dict(x_scale=None), dict(w_scale=None), dict(out=None), dict(out=torch.empty((8, 64), device="cuda").half()),
+                dict(x=whole(g, 8, 128)), dict(W=whole(g, 1, 64, 128)), dict(out=torch.empty((8, 32), device="cuda")),
+                dict(x=whole(g, 8, 256).float()), dict(w_scale=positive(g, 1, 64).double()), dict(x=whole(g, 256, 8).t()),
+                dict(x=whole(g, 8, 256).cpu()), dict(offsets=groups([8, 0]))):
+        with pytest.raises(B.MoeError):
+            gemm(**bad)
+
+    def experts(R=8, **other):
+        a = dict(x=whole(g, R, 512), xs=positive(g, R), offsets=groups([5, R - 5]), w1=whole(g, 2, 128, 512),
+                 s1=positive(g, 2, 128), w3=whole(g, 2, 128, 512), s3=positive(g, 2, 128), w2=whole(g, 2, 512, 128),
+                 s2=positive(g, 2, 512), y=torch.empty((R, 512), dtype=torch.bfloat16, device="cuda"))
+        a.update(other)
+        B.moe_expert_ffn_i8(ctx, a["x"], a["xs"], a["offsets"], R, a["w1"], a["s1"], a["w3"], a["s3"], a["w2"], a["s2"], a["y"])
+
+    experts()
+    for name in ("x", "xs", "offsets", "w1", "s1", "w3", "s3", "w2", "s2", "y"):
+        with pytest.raises(B.MoeError):
+            experts(**{name: None})
+    for bad in (dict(R=9), dict(w1=whole(g, 2, 512, 128)), dict(s2=positive(g, 2, 128)), dict(x=whole(g, 8, 512).float()),
+                dict(y=torch.empty((8, 512), device="cuda")), dict(offsets=groups([8]))):
+        with pytest.raises(B.MoeError):
+            experts(**bad)
+    ctx.close()

@@ -51,3 +51,13 @@ def test_quantize_refuses(lib, change):
 def test_quantize_refuses_rows_too_long(lib):
     assert quantize(lib, d=65537, stride=70000) == UNSUPPORTED
     assert quantize(lib, T=0, x=NULL, q=NULL, scale=NULL) == 0
+
+
+def gemm(lib, ctx=NULL, x=P, xs=P, offsets=NULL, R=4, E=1, N=64, K=256, w=P, ws=P, out=P, kind=0):
+    return lib.moe_gemm_i8(ctx, x, xs, offsets, C.c_int32(R), C.c_int32(E), C.c_int32(N), C.c_int32(K), w, ws, out,
+                           C.c_int(kind), NULL)
+
+
+def test_products_without_a_context_are_refused(lib):
+    assert gemm(lib) == INVALID
+    assert lib.moe_expert_ffn_i8(NULL, P, P, P, C.c_int32(4), P, P, P, P, P, P, P, NULL) == INVALID
