@@ -42,6 +42,148 @@ using PlainTinyS       = I8<Config<32, 64, 64, 2, 2, 4, false, true>>;
 using PlainFew         = I8<Config<16, 32, 64, 1, 2, 6, false>>;
 using PlainFewS        = I8<Config<16, 32, 64, 1, 2, 6, false, true>>;
 
+// ---- a few rows and few tiles: weights straight to registers, the reduction shared by wavefronts and workgroups ------
+// A tile is 16 rows and 16 output columns (with DUAL of both matrices). Its eight wavefronts take contiguous parts of the
+// reduction, so that a projection of a few thousand columns has a workgroup for every compute unit, which streams from eight
+// places of its weight rows; the int32 parts are added in LDS. Where even so there are few tiles and the reduction is long, it
+// is split over `splits` workgroups as well, whose parts are added in memory. Weights and rows go from memory to the lanes that
+// multiply them, the next 128 bytes of a row while those before are multiplied. The sums are whole numbers: how they are split
+// changes no bit.
+//
+// Bound by the latency of its loads and launch, not by bandwidth: one token, weights from memory, tiles of
+// 32 columns with the reduction in one workgroup (16 x 32) -> so: 14336 x 4096 19.1 -> 13.7 us (58.7 MB, of which 8.6 at
+// 6.8 TB/s), 4096 x 4096 7.5 -> 5.5, 2048 x 2048 4.8 -> 3.8; 16 tokens 20.1 -> 18.4, 7.9 -> 6.8, 4.7 -> 4.5. Past one tile per compute
+// unit the 32-column tiles win: 6144 x 6144 10.1 against 12.0, 4096 x 14336 columns 12.6 against 14.2. Four wavefronts, 32 columns
+// and two or four pieces in flight per wavefront are all within 5 % or slower.
+constexpr int kFewWaves = 8, kFewRows = 16;
+
+template <bool STREAM>
+__device__ __forceinline__ gemm::i32x4 load_frag(const int8_t* p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const gemm::i32x4*>(p));
+    else return *reinterpret_cast<const gemm::i32x4*>(p);
+}
+
+template <bool DUAL, bool F32>
+__global__ __launch_bounds__(kFewWaves * kWave) void few_rows_i8_kernel(
+    const int8_t* __restrict__ A, const int8_t* __restrict__ B0, const int8_t* __restrict__ B1, void* __restrict__ C,
+    const int32_t* __restrict__ offsets, int E, int N, int K, gemm::ScalesI8 sc, int splits, int32_t* __restrict__ sums) {
+    using gemm::i32x4;
+    constexpr int NB = DUAL ? 2 : 1;                 // weight fragments
+    __shared__ i32x4 part[kFewWaves][NB][kWave];
+    // the parts of a split reduction are mapped as the n-tiles of a matrix `splits` times as wide
+    const int NT = N / 16 * splits;
+    const gemm::TileCoord tc =
+        offsets ? gemm::locate_tile<kFewRows>(offsets, E, NT) : gemm::locate_tile_of_one<kFewRows>(sc.rows, NT);
+    if (tc.expert < 0) return;
+    int split;
+    const int nt = gemm::div_small(tc.nt, splits, split);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int frag_row = lane & 15, kg = lane >> 4;
+    const size_t wrow = static_cast<size_t>(tc.expert) * N + nt * 16;
+    const int row = tc.row0 + min(frag_row, tc.rows - 1);
+
+    float xs = 0.f;                                  // the scales of the outputs that the first wavefront will write
+    gemm::f32x4 ws[NB] = {};
+    if (wave == 0) {
+        xs = sc.x[row];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            ws[0][r] = sc.w0[wrow + 4 * kg + r];
+            if constexpr (DUAL) ws[1][r] = sc.w1[wrow + 4 * kg + r];
+        }
+    }
+    const int pieces = K / 128;                      // of 128 bytes, two k-steps of the instruction
+    const int part_of = split * kFewWaves + wave, parts = splits * kFewWaves;
+    const int first = part_of * pieces / parts, last = (part_of + 1) * pieces / parts;
+    const int8_t* a = A + static_cast<size_t>(row) * K + kg * 16;
+    const int8_t* b[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) b[j] = (j == 0 ? B0 : B1) + (wrow + frag_row) * K + kg * 16;
+
+    i32x4 acc[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[j] = i32x4{0, 0, 0, 0};
+    if (first < last) {
+        i32x4 fa[2][2], fb[2][2][NB];
+        auto load = [&](auto tag, int p) {
+            constexpr int S = decltype(tag)::value;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const size_t k = static_cast<size_t>(p) * 128 + h * 64;
+#pragma unroll
+                for (int j = 0; j < NB; ++j) fb[S][h][j] = load_frag<true>(b[j] + k);
+                fa[S][h] = load_frag<false>(a + k);
+            }
+        };
+        auto multiply = [&](auto tag) {
+            constexpr int S = decltype(tag)::value;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+                    acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[S][h][j], fa[S][h], acc[j], 0, 0, 0);
+        };
+        using Even = std::integral_constant<int, 0>;
+        using Odd = std::integral_constant<int, 1>;
+        load(Even{}, first);
+        for (int p = first; p < last; p += 2) {
+            if (p + 1 < last) load(Odd{}, p + 1);
+            multiply(Even{});
+            if (p + 1 >= last) break;
+            if (p + 2 < last) load(Even{}, p + 2);
+            multiply(Odd{});
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j) part[wave][j][lane] = acc[j];
+    __syncthreads();
+    if (wave != 0) return;
+    i32x4 sum[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        sum[j] = part[0][j][lane];
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) sum[j] += part[w][j][lane];
+    }
+    if constexpr (!DUAL) {
+        if (splits > 1) {
+            // Memory that is zero between launches: 256 sums of each tile, then a counter each. Every access is an atomic
+            // operation, performed in one place for all compute units, and its returned value says that it has been: the
+            // counter moves on behind this part's sums. Who moves it last takes the sums and leaves zeros.
+            int32_t *mine = sums + nt * 256 + lane, *arrived = sums + N / 16 * 256 + nt;
+            int old[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                old[r] = __hip_atomic_fetch_add(mine + r * kWave, sum[0][r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            asm volatile("" :: "v"(old[0]), "v"(old[1]), "v"(old[2]), "v"(old[3]) : "memory");
+            int before = 0;
+            if (lane == 0) before = __hip_atomic_fetch_add(arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (__builtin_amdgcn_readfirstlane(before) != splits - 1) return;
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                sum[0][r] = __hip_atomic_exchange(mine + r * kWave, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (lane == 0) __hip_atomic_store(arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    if (frag_row >= tc.rows) return;
+    const size_t at = static_cast<size_t>(row) * N + nt * 16 + 4 * kg;
+    gemm::f32x4 v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        v[r] = static_cast<float>(sum[0][r]) * xs * ws[0][r];
+        if constexpr (DUAL) v[r] = gemm::silu(v[r]) * (static_cast<float>(sum[1][r]) * xs * ws[1][r]);
+    }
+    if constexpr (F32) {
+        *reinterpret_cast<gemm::f32x4*>(static_cast<float*>(C) + at) = v;
+    } else {
+        gemm::bf16x4 o;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] = static_cast<__bf16>(v[r]);
+        *reinterpret_cast<gemm::bf16x4*>(static_cast<uint16_t*>(C) + at) = o;
+    }
+}
+
 // A product's operands: matrices as 16-bit units, K of them per row.
 struct Call {
     const GemmEnv& env;
@@ -71,9 +213,39 @@ int large(const Call& c) {
         return launch_1w<Cfg, false>(c.env, c.A, c.B0, c.B1, out, c.offsets, nullptr, 1, c.R, c.E, c.N, c.K, c.s, c.scales);
     return launch_1w<Cfg, true>(c.env, c.A, c.B0, c.B1, out, c.offsets, nullptr, 1, c.R, c.E, c.N, c.K, c.s, c.scales);
 }
+// Experts that the call is expected to touch.
+double touched(const Call& c) { return c.E == 1 ? 1.0 : touched_experts(c.R, c.E); }
+
+// Whether the tiles of 16 rows and columns find a compute unit each.
+bool few_rows_fits(const Call& c) {
+    if (c.env.forced_config >= 0) return false;
+    const bool few = c.E == 1 ? c.R <= kFewRows : single_m_tile(c.env, c.R, c.E, kFewRows);
+    return few && touched(c) * (c.N / 16) <= compute_units(c.env.device);
+}
+// Workgroups that share the reduction of a tile, 2048 elements of it each, up to one workgroup per compute unit. One token, split
+// by 1 -> as here: 16384 x 256 12.3 -> 6.1 us (8), 8192 x 1024 7.7 -> 5.9 (4), 8192 x 2048 7.9 -> 6.9 (2); joining costs about 1 us,
+// 4096 x 512 4.9 -> 5.1 (2), 2048 x 1024 3.8 -> 4.6, and more with more parts (16384 x 256 in 16 7.0).
+int few_rows_splits(const Call& c) {
+    if (c.E != 1 || c.K < 3 * 1024) return 1;        // K counts pairs of elements
+    const int tiles = c.N / 16;
+    if (tiles > kSplitTiles) return 1;
+    return std::max(1, std::min(compute_units(c.env.device) / tiles, c.K / 1024));
+}
+template <bool DUAL, bool F32>
+int few_rows(const Call& c) {
+    const int splits = DUAL ? 1 : few_rows_splits(c);
+    const long long grid = (most_row_tiles(c.R, c.E, kFewRows) * (c.N / 16) * splits + kXcds - 1) / kXcds * kXcds;
+    if (grid > 0x7fffffffLL) return MOE_ERR_UNSUPPORTED_SHAPE;
+    hipLaunchKernelGGL((few_rows_i8_kernel<DUAL, F32>), dim3(static_cast<unsigned>(grid)), dim3(kFewWaves * kWave), 0, c.s,
+                       reinterpret_cast<const int8_t*>(c.A), reinterpret_cast<const int8_t*>(c.B0),
+                       reinterpret_cast<const int8_t*>(c.B1), c.C, c.offsets, c.E, c.N, 2 * c.K, c.scales, splits,
+                       c.env.split_sums);
+    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
 bool large_takes(int N, int K) { return gemm::offsets_fit_1w(N, K) && K >= 256; }
 
 int gateup(const Call& c) {
+    if (few_rows_fits(c)) return few_rows<true, false>(c);
     int config = pick_config(c.env, c.R, c.E, gateup_tiles(c.E, c.K, c.N));
     if (config == 0 && !large_takes(c.N, c.K)) config = 1;
     switch (config) {
@@ -82,7 +254,7 @@ int gateup(const Call& c) {
         case 4: return grouped<GateUpMid96, GateUpMid96S>(c);
         case 3: {
             if (!single_m_tile(c.env, c.R, c.E, 32)) return grouped<GateUpTiny>(c);
-            const double nt = touched_experts(c.R, c.E) * (c.N / 64);
+            const double nt = touched(c) * (c.N / 64);
             const int cus = compute_units(c.env.device);
             if (narrow_gateup_tiles(c.R, c.E, c.N, cus) || narrow_short_gateup_tiles(c.R, c.E, c.K, c.N, cus))
                 return one_tile_per_cu(c.R, c.E, c.N, cus) ? grouped<GateUpFewDeepS>(c) : grouped<GateUpFewS>(c);
@@ -95,6 +267,7 @@ int gateup(const Call& c) {
 
 template <bool F32>
 int product(const Call& c) {
+    if (few_rows_fits(c)) return few_rows<false, F32>(c);
     const int d = c.N;
     const bool wide_mid = static_cast<long long>(c.E) * (d / 256) >= 160;
     const int cus = compute_units(c.env.device);
@@ -112,14 +285,14 @@ int product(const Call& c) {
             if (wide_mid) return grouped<Out<F32, PlainMid96Wide>, Out<F32, PlainMid96WideS>>(c);
             return grouped<Out<F32, PlainMid96>, Out<F32, PlainMid96S>>(c);
         case 3:
-            if (touched_experts(c.R, c.E) * (d / 64) < cus) {
+            if (touched(c) * (d / 64) < cus) {
                 if (single_m_tile(c.env, c.R, c.E, 16)) return grouped<Out<F32, PlainFewS>>(c);
                 if (d < 64 || row_tiles(c.R, c.E, 16) * (d / 32) <= cus) return grouped<Out<F32, PlainFew>>(c);
             }
             return grouped<Out<F32, PlainTiny>, Out<F32, PlainTinyS>>(c);
         default:
             if (row_tiles(c.R, c.E, 64) * (d / 64) <= 0.5 * cus) return grouped<Out<F32, PlainTiny>>(c);
-            if (touched_experts(c.R, c.E) * (d / 128) >= 3.5 * cus)
+            if (touched(c) * (d / 128) >= 3.5 * cus)
                 return grouped<Out<F32, PlainSmallWide>, Out<F32, PlainSmallWideS>>(c);
             return grouped<Out<F32, PlainSmall>, Out<F32, PlainSmallS>>(c);
     }

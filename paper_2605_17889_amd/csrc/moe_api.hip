@@ -68,7 +68,7 @@ bool on_own_device(const moe_ctx* c) {
 }
 
 struct Layout {
-    size_t topk_idx, topk_w, counts, offsets, perm, inv_perm, scratch, logits, x_perm, H, y_perm, counters, total;
+    size_t topk_idx, topk_w, counts, offsets, perm, inv_perm, scratch, logits, x_perm, H, y_perm, counters, split_sums, total;
 };
 
 Layout layout_for(const moe_shape* s) {
@@ -88,6 +88,7 @@ Layout layout_for(const moe_shape* s) {
     L.H = take(R * s->d_ff * 2);
     L.y_perm = take(R * s->d_model * 2);
     L.counters = take(kTileCounterBytes);
+    L.split_sums = take(kSplitSumBytes);
     L.total = off ? off : 256;
     return L;
 }
@@ -282,6 +283,10 @@ int moe_create(moe_ctx** out, const moe_shape* shape, int device_id) {
         counters = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(p) + L.counters);
         err = hipMemcpy(counters, zeros, sizeof(zeros), hipMemcpyHostToDevice);
     }
+    if (err == hipSuccess) {
+        static const unsigned char zeros[kSplitSumBytes] = {};
+        err = hipMemcpy(static_cast<unsigned char*>(p) + L.split_sums, zeros, sizeof(zeros), hipMemcpyHostToDevice);
+    }
     const hipError_t back = hipSetDevice(caller_device);
     if (err != hipSuccess || back != hipSuccess) {
         (void)hipGetLastError();
@@ -306,6 +311,7 @@ int moe_create(moe_ctx** out, const moe_shape* shape, int device_id) {
     c->h_i8 = nullptr;
     c->h_scale = nullptr;
     c->gemm.tile_counters = counters;
+    c->gemm.split_sums = reinterpret_cast<int32_t*>(c->base + L.split_sums);
     c->prof_armed = false;
     c->prof_max_calls = c->prof_calls = 0;
     for (auto& v : c->prof_launches) v = 0;

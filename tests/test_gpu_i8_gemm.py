@@ -122,6 +122,29 @@ def test_large_tiles(T, N, K):
         gemm_case([T // 3, 0, T // 2, T - T // 3 - T // 2], N, K, dtype, seed=T)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_few_rows_with_a_split_reduction(dtype):
+    """One context, calls of other widths and splits in turn: every call leaves the sums in memory as it found them."""
+    ctx = B.MoeContext(16, 512, 128, 1, 1)
+    shapes = [(1, 256, 16384), (16, 32, 130944), (3, 1024, 8192), (9, 2048, 6144), (16, 2032, 6144), (1, 4096, 14336), (2, 112, 6272)]
+    for seed in range(3):
+        for T, N, K in shapes:
+            g = gen(seed * 100 + T)
+            x, xs, w, ws = whole(g, T, K), positive(g, T), whole(g, N, K), positive(g, N)
+            out = torch.empty((T, N), dtype=dtype, device="cuda")
+            for _ in range(2):
+                out.fill_(7)
+                B.moe_gemm_i8(ctx, x, xs, None, T, 1, N, K, w, ws, out)
+                assert_near(out, product64(x, xs, w, ws), half_of(dtype))
+    ctx.close()
+
+
+@pytest.mark.parametrize("counts,d,f", [([1, 0], 512, 1024), ([5, 9, 0, 40], 1024, 512), ([0, 0, 16], 2048, 1152), ([3], 4096, 256)])
+def test_few_rows_and_few_tiles(counts, d, f):
+    ffn_case(counts, d, f, seed=len(counts))
+    gemm_case(counts, f, d, torch.float32, seed=d)
+
+
 def test_sums_at_the_ends_of_the_range():
     """The longest reduction, all products alike: sums of 2^31 - 2^21 and -2^31 + 2^24 or so, exactly."""
     K, N = 130944, 32
