@@ -65,6 +65,7 @@ int launch_gather(const moe_bf16* x, const int32_t* perm, const int32_t* offsets
 // device's 64 and gives it back; set -1: there is none left (the caller then zeroes memory of its own). The
 // calling thread's current device must be `device`.
 constexpr size_t kTileCounterBytes = kXcds * 128;
+constexpr int kPartSums = 6 << 18;        // 6 MB of them
 constexpr int kSplitTiles = 128;
 constexpr size_t kSplitSumBytes = kSplitTiles * (256 + 1) * sizeof(int32_t);   // of 256 sums and a counter each
 int32_t* take_tile_counters(int device, int* set);
@@ -79,7 +80,8 @@ struct GemmEnv {
     bool split_last_round = true;     // large tiles: halve the tiles of a last round under half full
     int large_tile_waves = 0;         // 0: automatic; 4 / 8: wavefronts of the 256 x 256 tile
     int32_t* tile_counters = nullptr; // kTileCounterBytes, zero between launches
-    int32_t* split_sums = nullptr;    // kSplitSumBytes, zero between launches: 8-bit products with a split reduction
+    int32_t* split_sums = nullptr;    // kSplitSumBytes, zero between launches: 8-bit products of few rows, split reductions
+    int32_t* part_sums = nullptr;     // kPartSums: the same of more rows, parts that a second launch joins
 };
 int launch_gateup(const GemmEnv& env, const moe_bf16* a, const int32_t* row_index, int index_div,
                   const int32_t* offsets, int R, int R_hint, int d, int f, int E,

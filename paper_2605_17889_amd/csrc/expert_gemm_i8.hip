@@ -184,6 +184,11 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_rows_i8_kernel(
     }
 }
 
+using Piped32x64       = I8<Config<32, 64, 64, 2, 2, 4, false>>;
+using Piped64x64       = I8<Config<64, 64, 64, 2, 2, 5, false>>;
+using Piped64x128      = I8<Config<64, 128, 64, 2, 2, 6, false>>;
+using Piped128x128     = I8<Config<128, 128, 64, 2, 2, 5, false>>;
+
 // A product's operands: matrices as 16-bit units, K of them per row.
 struct Call {
     const GemmEnv& env;
@@ -200,6 +205,46 @@ template <class Cfg>
 int grouped(const Call& c) {
     return launch_grouped<Cfg>(c.env, c.A, c.B0, c.B1, static_cast<uint16_t*>(c.C), c.offsets, nullptr, 1, c.R, c.E, c.N,
                                c.K, c.s, c.scales);
+}
+template <class Cfg>
+int piped(const Call& c) {
+    return launch_pipelined<Cfg>(c.env, c.A, c.B0, c.B1, static_cast<uint16_t*>(c.C), c.offsets, c.R, c.E, c.N, c.K, c.s,
+                                 c.scales);
+}
+// Sums of `splits` parts of a reduction, part by part [R, N], as outputs.
+template <bool F32>
+__global__ __launch_bounds__(256) void join_parts_kernel(const gemm::i32x4* __restrict__ parts, int splits, long long quads, int N,
+                                                         gemm::ScalesI8 sc, void* __restrict__ C) {
+    const long long q = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    if (q >= quads) return;
+    gemm::i32x4 sum = parts[q];
+    for (int p = 1; p < splits; ++p) sum += parts[p * quads + q];
+    const int row = static_cast<int>(q * 4 / N), col = static_cast<int>(q * 4 - static_cast<long long>(row) * N);
+    const float xs = sc.x[row];
+    gemm::f32x4 v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = static_cast<float>(sum[r]) * xs * sc.w0[col + r];
+    if constexpr (F32) {
+        static_cast<gemm::f32x4*>(C)[q] = v;
+    } else {
+        gemm::bf16x4 o;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] = static_cast<__bf16>(v[r]);
+        static_cast<gemm::bf16x4*>(C)[q] = o;
+    }
+}
+template <bool F32, class Cfg>
+int split(const Call& c, int splits) {
+    int32_t* parts = c.env.part_sums;
+    Call d = c;
+    d.scales.splits = splits;
+    d.C = parts;
+    const int rc = piped<gemm::RawSums<Cfg>>(d);
+    if (rc != MOE_OK) return rc;
+    const long long quads = static_cast<long long>(c.R) * c.N / 4;
+    hipLaunchKernelGGL((join_parts_kernel<F32>), dim3(static_cast<unsigned>((quads + 255) / 256)), dim3(256), 0, c.s,
+                       reinterpret_cast<const gemm::i32x4*>(parts), splits, quads, c.N, c.scales, c.C);
+    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 // Weights that a single row tile reads are loaded as non-temporal.
 template <class Cached, class Streamed>
@@ -265,9 +310,85 @@ int gateup(const Call& c) {
     }
 }
 
+// ---- one matrix: its tiles are known, so the tile and the split of the reduction are priced ------------------------------
+// A compute unit takes in 50 GB/s of rows and weights that come from memory (85 from L2), whatever the tile, so that a k-step
+// costs by the bytes of its stage; small tiles load each byte more often, large ones leave compute units without any. Where
+// both hurt (few rows, narrow outputs, long reductions) the reduction is split over workgroups, whose int32 sums go to memory
+// and are joined by a second launch. us of a k-step of 128 elements, weights from memory; `pair`: of two workgroups on a
+// compute unit. Priced -> the tile that the grouped rules take, in us: 64 rows, 14336 x 4096 columns 30.8 -> 17.7; 128 rows there
+// 36.0 -> 22.9; 512 rows 93 -> 51; 1003 92 -> 68; 256 rows, 8192 x 1024 17.8 -> 11.9; 2048 rows there 50.7 -> 28.8; 128 rows,
+// 16384 x 256 24.6 -> 9.2; 1003 rows, 2048 x 2048 13.6 -> 9.2; 512 rows, 8192 x 8192 53 -> 41.
+enum class OneTile { t32x64, t64x64, t64x128, t128x128, large };
+struct OneTilePrice {
+    OneTile tile;
+    int rows, cols, stages;
+    double step, pair, fixed;        // us; without a pair one workgroup fills a compute unit
+};
+constexpr OneTilePrice kOneTiles[] = {
+    {OneTile::t32x64, 32, 64, 4, 0.28, 0.46, 1.5},    {OneTile::t64x64, 64, 64, 5, 0.32, 0.57, 1.5},
+    {OneTile::t64x128, 64, 128, 6, 0.47, 0.0, 1.5},   {OneTile::t128x128, 128, 128, 5, 0.62, 0.0, 1.5},
+    {OneTile::large, 256, 256, 4, 1.45, 0.0, 4.0},
+};
+struct OnePlan {
+    OneTile tile;
+    int splits;
+    double us;
+};
+OnePlan plan_one(const Call& c) {
+    const int cus = compute_units(c.env.device);
+    const double bytes = 2.0 * c.N * c.K, ksteps = c.K / 64.0;
+    OnePlan best{OneTile::t32x64, 1, 1e30};
+    for (const OneTilePrice& t : kOneTiles) {
+        if (c.N < t.cols || c.K / 64 < t.stages || (t.tile == OneTile::large && !large_takes(c.N, c.K))) continue;
+        const double tiles = std::ceil(c.R / static_cast<double>(t.rows)) * ((c.N + t.cols - 1) / t.cols);
+        const bool can_split = c.offsets == nullptr && t.tile <= OneTile::t64x128;
+        for (int s = 1; s <= (can_split ? 16 : 1); ++s) {
+            if (c.K / 64 / s < t.stages || (s > 1 && static_cast<double>(s) * c.R * c.N > kPartSums)) break;
+            const double n = tiles * s, each = std::ceil(n / cus);           // workgroups of a compute unit
+            double step = each * t.step, rounds = each;
+            if (t.pair > 0.0) {
+                rounds = std::ceil(each / 2);
+                step = std::floor(each / 2) * t.pair + (each - 2 * std::floor(each / 2)) * t.step;
+            }
+            if (t.tile == OneTile::large) {          // the tiles of a last round that is less than half full are run as two halves
+                const double rem = n - std::floor(n / cus) * cus;
+                if (rem > 0 && 2 * rem <= cus) step += 0.88 - t.step;
+            }
+            // joining: a launch, every sum written and read, and a tenth as the margin that a split has to win by
+            const double us = std::max(ksteps / s * step, bytes / 6e6) + rounds * t.fixed +
+                              (s > 1 ? 3.0 + 8e-6 / 4 * s * c.R * c.N : 0.0);
+            const double price = s > 1 ? us / 0.9 : us;
+            if (price < best.us) best = OnePlan{t.tile, s, price};
+        }
+    }
+    return best;
+}
+template <bool F32, class Cfg>
+int one_tile(const Call& c, int splits) {
+    if constexpr (Cfg::BN <= 128 && Cfg::BM <= 64)
+        if (splits > 1) return split<F32, Cfg>(c, splits);
+    return piped<Out<F32, Cfg>>(c);
+}
+template <bool F32>
+int product_of_one(const Call& c) {
+    const OnePlan plan = plan_one(c);
+    switch (plan.tile) {
+        case OneTile::t64x64: return one_tile<F32, Piped64x64>(c, plan.splits);
+        case OneTile::t64x128: return one_tile<F32, Piped64x128>(c, plan.splits);
+        case OneTile::t128x128: return one_tile<F32, Piped128x128>(c, 1);
+        case OneTile::large: return large<Out<F32, Plain1W>>(c);
+        default: break;
+    }
+    // narrower or shorter than every tile of the table (or a reduction of less than four k-steps): the grouped forms
+    if (c.N < 64) return grouped<Out<F32, PlainFew>>(c);
+    if (c.K / 64 < Piped32x64::NSTAGE) return grouped<Out<F32, PlainTiny>>(c);
+    return one_tile<F32, Piped32x64>(c, plan.splits);
+}
+
 template <bool F32>
 int product(const Call& c) {
     if (few_rows_fits(c)) return few_rows<false, F32>(c);
+    if (c.E == 1 && c.R > kFewRows && c.env.forced_config < 0) return product_of_one<F32>(c);
     const int d = c.N;
     const bool wide_mid = static_cast<long long>(c.E) * (d / 256) >= 160;
     const int cus = compute_units(c.env.device);
@@ -304,13 +425,13 @@ int launch_gateup_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, 
                      int E, const moe_i8* W1, const float* w1_scale, const moe_i8* W3, const float* w3_scale, moe_bf16* H,
                      hipStream_t s) {
     if (R == 0) return MOE_OK;
-    return gateup(Call{env, units(x), units(W1), units(W3), H, offsets, {x_scale, w1_scale, w3_scale, R}, R, E, f, d / 2, s});
+    return gateup(Call{env, units(x), units(W1), units(W3), H, offsets, {x_scale, w1_scale, w3_scale, R, 1}, R, E, f, d / 2, s});
 }
 
 int launch_product_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, int N, int K,
                       int E, const moe_i8* W, const float* w_scale, void* out, bool out_f32, hipStream_t s) {
     if (R == 0) return MOE_OK;
-    const Call c{env, units(x), units(W), nullptr, out, offsets, {x_scale, w_scale, nullptr, R}, R, E, N, K / 2, s};
+    const Call c{env, units(x), units(W), nullptr, out, offsets, {x_scale, w_scale, nullptr, R, 1}, R, E, N, K / 2, s};
     return out_f32 ? product<true>(c) : product<false>(c);
 }
 

@@ -461,6 +461,12 @@ template <class Cfg>
 struct OperandsI8 : Cfg {
     static constexpr bool OPERANDS_I8 = true;
 };
+// The same with the int32 sums themselves as outputs (four bytes each): parts of a split reduction.
+template <class Cfg>
+struct RawSums : Cfg {
+    static constexpr bool OUT_F32 = true, RAW_SUMS = true;
+    static_assert(!Cfg::DUAL && Cfg::OPERANDS_I8, "sums of one product");
+};
 // The same tile with H rows.
 template <class Cfg, int H> struct WithHeight;
 template <int BM, int BN, int BK, int WM, int WN, int NSTAGE, bool DUAL, bool STREAM_B, int H>
@@ -477,11 +483,25 @@ struct out_is_f32 : std::false_type {};
 template <class Cfg>
 struct out_is_f32<Cfg, std::void_t<decltype(Cfg::OUT_F32)>> : std::bool_constant<Cfg::OUT_F32> {};
 template <class Cfg, class = void>
+struct raw_sums : std::false_type {};
+template <class Cfg>
+struct raw_sums<Cfg, std::void_t<decltype(Cfg::RAW_SUMS)>> : std::bool_constant<Cfg::RAW_SUMS> {};
+template <class Cfg, class = void>
 struct operands_i8 : std::false_type {};
 template <class Cfg>
 struct operands_i8<Cfg, std::void_t<decltype(Cfg::OPERANDS_I8)>> : std::bool_constant<Cfg::OPERANDS_I8> {};
 
 // ---- pieces shared by the kernels ---------------------------------------------------------
+#define MOE_FENCE() __builtin_amdgcn_sched_barrier(0)
+
+// f(integral_constant<int, 0>) ... f(integral_constant<int, N - 1>) in order
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        static_for<N, I + 1>(f);
+    }
+}
 
 // The n-tiles of N output columns. With 8-bit operands N need not be a multiple of a tile's columns (it has to hold one): the
 // last tile then starts further left, and the columns that two tiles share get the same bits from both.
@@ -541,6 +561,20 @@ __device__ __forceinline__ void mma16_agpr(const bf16x8& w, const bf16x8& x, f32
     if constexpr (I8) asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(w), "v"(x));
     else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(w), "v"(x));
 }
+// The accumulators start as the result of an MFMA, 0 * 0 + 0, not as ordinary register
+// writes: the compiler may sink those to just in front of the k-loop, where it cannot
+// know that the inline assembly there is an MFMA that needs wait states after them.
+// MFMA after MFMA on the same registers needs nothing.
+template <int TM, int TN>
+__device__ __forceinline__ void zero_accumulators(f32x4 (&acc)[TM][TN]) {
+    const bf16x4 zero = {0, 0, 0, 0};
+    asm volatile("s_nop 4" :: "v"(zero));
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)                 // four registers in half the time of the 16x16x32 instruction
+            asm volatile("v_mfma_f32_4x4x4_16b_bf16 %0, %1, %1, 0" : "=a"(acc[i][j]) : "v"(zero));
+}
 // Wait states between the last MFMA and the first ordinary read of its result. `last` are the
 // accumulators of the last MFMAs: the empty statements keep the compiler from reading them ahead of
 // the wait (older ones have left the matrix pipe by then, whenever they are read).
@@ -555,6 +589,7 @@ __device__ __forceinline__ void mfma_drain(f32x4 (&last)[N]) {
 struct ScalesI8 {
     const float *x, *w0, *w1;
     int rows;            // where there are no offsets: the rows of the one group
+    int splits;          // with RawSums: workgroups that share the reduction of a tile (there are no offsets then)
 };
 struct NoScales {};
 template <class Cfg> using ScalesOf = std::conditional_t<operands_i8<Cfg>::value, ScalesI8, NoScales>;
@@ -609,12 +644,13 @@ __device__ __forceinline__ TileCoord tile_of_workgroup(const int32_t* __restrict
 }
 
 // What a kernel keeps of them: nothing for bf16 operands.
-template <class Cfg> using KeptScales = TileScales<std::conditional_t<operands_i8<Cfg>::value, Cfg, void>>;
+template <class Cfg> constexpr bool is_scaled = operands_i8<Cfg>::value && !raw_sums<Cfg>::value;
+template <class Cfg> using KeptScales = TileScales<std::conditional_t<is_scaled<Cfg>, Cfg, void>>;
 template <class Cfg>
 __device__ __forceinline__ KeptScales<Cfg> load_scales(const ScalesOf<Cfg>& sc, const TileCoord& tc, int wm, int wn,
                                                        int lane, int N) {
     KeptScales<Cfg> kept;
-    if constexpr (operands_i8<Cfg>::value) kept.load(sc, tc, wm, wn, lane, N);
+    if constexpr (is_scaled<Cfg>) kept.load(sc, tc, wm, wn, lane, N);
     return kept;
 }
 
@@ -633,7 +669,7 @@ __device__ __forceinline__ void store_tile(f32x4 (&acc)[Cfg::TM][Cfg::TN], const
                                            uint16_t* __restrict__ C, int ldc, const KeptScales<Cfg>& sc) {
     constexpr bool DUAL = Cfg::DUAL;
     constexpr int DB = Cfg::DB, P = DB / 16;
-    if constexpr (operands_i8<Cfg>::value) {
+    if constexpr (is_scaled<Cfg>) {
         f32x4 cols[Cfg::TN];
 #pragma unroll
         for (int j = 0; j < Cfg::TN; ++j) cols[j] = sc.of_columns(j, fp.frag_kg);
@@ -1010,6 +1046,123 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_routed_kernel(
     }, smem, wave, lane, B0, B1, C, N, K, NoScales{});
 }
 
+// ---- kernel 1, pipelined: what ring_of_stages does, with every load behind a matrix instruction of its own -------------
+// A k-step is two halves of one MFMA k-substep each. While the MFMAs of a half issue, the fragments of the next half are read
+// and one direct-to-LDS load goes out behind every few of them; the barrier sits between the halves, where the fragments of
+// the second one are in registers, so that behind it the k-step's stage may be filled again and the next one be read. The B
+// loads of k-step kt + NSTAGE - 1 go out in the first half of k-step kt, the A loads of kt + NSTAGE in its second.
+// DIST: k-steps from this one to the last, or NSTAGE where there are at least as many. One loop and straight code behind
+// it: the accumulators are operands of inline assembly (mma16_agpr), which no join of paths may make the compiler move.
+template <class Cfg, int DIST>
+__device__ __forceinline__ void pipelined_kstep(f32x4 (&acc)[Cfg::TM][Cfg::TN], bf16x8 (&fa)[2][Cfg::TM],
+                                                bf16x8 (&fb)[2][Cfg::TN], const LoadPlan<Cfg>& lp, const FragPlan<Cfg>& fp,
+                                                unsigned char* smem, int stage, int kt) {
+    constexpr int TM = Cfg::TM, TN = Cfg::TN, NM = TM * TN, NR = TM + TN, S = Cfg::NSTAGE;
+    constexpr int LA = LoadPlan<Cfg>::LA, LB = LoadPlan<Cfg>::LB;
+    constexpr bool I8 = operands_i8<Cfg>::value;
+    const int next = stage + 1 == S ? 0 : stage + 1, previous = stage == 0 ? S - 1 : stage - 1;
+    const unsigned char *here = smem + stage * Cfg::STAGE_BYTES, *ahead = smem + next * Cfg::STAGE_BYTES;
+    auto read = [&](int r, int h, const unsigned char* from) {       // fragment r of a half: B fragments first
+        if (r < TN) fb[h][r] = lds16(from + fp.b_off[h] + r * Cfg::TILE_STEP);
+        else fa[h][r - TN] = lds16(from + fp.a_off[h] + (r - TN) * Cfg::TILE_STEP);
+    };
+#pragma unroll
+    for (int m = 0; m < NM; ++m) {
+        mma16_agpr<I8>(fb[0][m % TN], fa[0][m / TN], acc[m / TN][m % TN]);
+        MOE_FENCE();
+        // all of them within the first three quarters: they have to have returned at the barrier
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+            if (r * (3 * NM / 4) / NR == m) read(r, 1, here);
+        if constexpr (DIST >= S - 1) {
+#pragma unroll
+            for (int n = 0; n < LB; ++n)
+                if (n * NM / LB == m) lp.issue_one(LA + n, previous * Cfg::STAGE_BYTES, static_cast<size_t>(kt + S - 1) * Cfg::BK);
+        }
+        MOE_FENCE();
+    }
+    constexpr int NEWER = DIST >= S ? S - 2 : DIST >= 2 ? DIST - 1 : 0;        // k-steps on their way behind the next one
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(NEWER * Cfg::LPW) : "memory");
+    __builtin_amdgcn_s_barrier();
+    MOE_FENCE();
+#pragma unroll
+    for (int m = 0; m < NM; ++m) {
+        mma16_agpr<I8>(fb[1][m % TN], fa[1][m / TN], acc[m / TN][m % TN]);
+        MOE_FENCE();
+        if constexpr (DIST >= 1) {
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+                if (r * NM / NR == m) read(r, 0, ahead);
+        }
+        if constexpr (DIST >= S) {
+#pragma unroll
+            for (int n = 0; n < LA; ++n)
+                if (n * NM / LA == m) lp.issue_one(n, stage * Cfg::STAGE_BYTES, static_cast<size_t>(kt + S) * Cfg::BK);
+        }
+        MOE_FENCE();
+    }
+}
+
+template <class Cfg>
+__global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_pipelined_kernel(
+    const uint16_t* __restrict__ A, const uint16_t* __restrict__ B0, const uint16_t* __restrict__ B1,
+    uint16_t* __restrict__ C, const int32_t* __restrict__ offsets, RowDiv index_div, int E, int N, int K,
+    ScalesOf<Cfg> scales) {
+    constexpr int TM = Cfg::TM, TN = Cfg::TN, S = Cfg::NSTAGE, LA = LoadPlan<Cfg>::LA;
+    static_assert(Cfg::KSUB == 2 && (S - 1) * Cfg::LPW + LA < 64, "two k-substeps a stage; loads in flight");
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    TileCoord tc;
+    int KT = K / Cfg::BK;                            // >= S (checked by the launcher)
+    if constexpr (raw_sums<Cfg>::value) {            // the parts are mapped as the n-tiles of a matrix that many times as wide
+        tc = locate_tile_of_one<Cfg::BM>(scales.rows, n_tiles<Cfg>(N) * scales.splits);
+        if (tc.expert < 0) return;
+        int part;
+        tc.nt = div_small(tc.nt, scales.splits, part);
+        const int first = part * KT / scales.splits;
+        KT = (part + 1) * KT / scales.splits - first;
+        A += first * Cfg::BK;
+        B0 += first * Cfg::BK;
+        C += static_cast<size_t>(part) * scales.rows * N * 2;        // in 16-bit units
+    } else {
+        tc = tile_of_workgroup<Cfg>(offsets, scales, E, N, 0, Cut::kNever);
+        if (tc.expert < 0) return;
+    }
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / Cfg::WN, wn = wave % Cfg::WN;
+    LoadPlan<Cfg> lp;
+    lp.init_fixed(wave, lane, K);
+    lp.init(tc, wave, lane, A, B0, B1, nullptr, index_div, N, K);
+    const KeptScales<Cfg> sc = load_scales<Cfg>(scales, tc, wm, wn, lane, N);
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) lp.issue_all(s * Cfg::STAGE_BYTES, static_cast<size_t>(s) * Cfg::BK);
+    lp.issue_a_all((S - 1) * Cfg::STAGE_BYTES, static_cast<size_t>(S - 1) * Cfg::BK);
+    FragPlan<Cfg> fp;
+    fp.init(lane, wm, wn);
+    f32x4 acc[TM][TN];
+    zero_accumulators(acc);
+    wait_vmcnt<(S - 2) * Cfg::LPW + LA>();           // k-step 0 landed
+    __builtin_amdgcn_s_barrier();
+    bf16x8 fa[2][TM], fb[2][TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fb[0][j] = lds16(smem + fp.b_off[0] + j * Cfg::TILE_STEP);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) fa[0][i] = lds16(smem + fp.a_off[0] + i * Cfg::TILE_STEP);
+    MOE_FENCE();
+    int stage = 0, kt = 0;
+    for (; kt + S < KT; ++kt) {
+        pipelined_kstep<Cfg, S>(acc, fa, fb, lp, fp, smem, stage, kt);
+        stage = stage + 1 == S ? 0 : stage + 1;
+    }
+    static_for<S>([&](auto tag) {                    // the last S k-steps
+        pipelined_kstep<Cfg, S - 1 - decltype(tag)::value>(acc, fa, fb, lp, fp, smem, stage, kt);
+        stage = stage + 1 == S ? 0 : stage + 1;
+        ++kt;
+    });
+    mfma_drain(acc[TM - 1]);
+    store_tile<Cfg>(acc, tc, fp, wm, wn, C, N, sc);
+}
+
 // ---- kernel 2: operand rings of different depth, hand-placed software pipeline ---------------
 // A k-step (64 k) is two half-steps of one MFMA k-substep each. While the MFMAs of a half-step
 // issue, the fragments of the next half-step are read from LDS into the registers that the
@@ -1027,7 +1180,6 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_routed_kernel(
 // kernel waits about a third of every k-step for the slowest cache line of the next one. The
 // operand with the shallower ring is issued first within a k-step: loads complete in order, so
 // the wait for it then leaves only the newest loads of the deeper operand pending.
-#define MOE_FENCE() __builtin_amdgcn_sched_barrier(0)
 
 template <class Cfg, int NA, int NB>
 struct RingCfg {
@@ -1348,15 +1500,6 @@ __device__ __forceinline__ void store_tile_via_lds(const f32x4 (&acc)[Cfg::TM][8
 
 template <class T> struct type_tag { using type = T; };
 
-// f(integral_constant<int, 0>) ... f(integral_constant<int, N - 1>) in order
-template <int N, int I = 0, class F>
-__device__ __forceinline__ void static_for(F&& f) {
-    if constexpr (I < N) {
-        f(std::integral_constant<int, I>{});
-        static_for<N, I + 1>(f);
-    }
-}
-
 // ---- the large tiles with ONE wavefront per SIMD (4 wavefronts, 128 x 128 outputs each) -------
 // Four wavefronts read 128 KB of fragments from LDS per k-step where eight read 192 KB, and hold
 // all 256 accumulator registers of a lane's SIMD, so every fragment set can be double-buffered
@@ -1608,20 +1751,8 @@ __device__ __forceinline__ void ring_tile_1w(const TileCoord& tc, const TileCoor
 #pragma unroll
     for (int i = 0; i < TM; ++i) fa[0][i] = lds16(pa[0] + sa + i * Cfg::TILE_STEP);
     MOE_FENCE();
-    // The accumulators start as the result of an MFMA, 0 * 0 + 0, not as ordinary register
-    // writes: the compiler may sink those to just in front of the k-loop, where it cannot
-    // know that the inline assembly there is an MFMA that needs wait states after them.
-    // MFMA after MFMA on the same registers needs nothing.
     f32x4 acc[TM][TN];
-    {
-        const bf16x4 zero = {0, 0, 0, 0};
-        asm volatile("s_nop 4" :: "v"(zero));
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j)             // four registers in half the time of the 16x16x32 instruction
-                asm volatile("v_mfma_f32_4x4x4_16b_bf16 %0, %1, %1, 0" : "=a"(acc[i][j]) : "v"(zero));
-    }
+    zero_accumulators(acc);
     const uint32_t sb_next = sb + BB == R::NB * BB ? 0u : sb + BB;
     RingState1W rs{pa[1] + sa, pb[1] + sb, pa[0] + (sa ^ AB), pb[0] + sb_next, sa + wave * 1024u,
                    R::A_RING + (sb == 0 ? (R::NB - 1) * BB : sb - BB) + wave * (R::LB * 1024u), sa, sb};

@@ -79,6 +79,19 @@ int launch_grouped(const GemmEnv& env, const moe_bf16* A, const moe_bf16* B0, co
                         gemm::RowDiv(index_div), E, N, K, spread_steps(R, E, N, K, Cfg::DUAL), scales);
 }
 
+// The pipelined form of the generic kernel.
+template <class Cfg>
+int launch_pipelined(const GemmEnv& env, const moe_bf16* A, const moe_bf16* B0, const moe_bf16* B1, moe_bf16* C,
+                     const int32_t* offsets, int R, int E, int N, int K, hipStream_t s,
+                     const gemm::ScalesOf<Cfg>& scales = {}) {
+    int splits = 1;
+    if constexpr (gemm::raw_sums<Cfg>::value) splits = scales.splits;
+    if (!columns_fit<Cfg>(N) || K % Cfg::BK != 0 || K / Cfg::BK / splits < Cfg::NSTAGE) return MOE_ERR_UNSUPPORTED_SHAPE;
+    static std::atomic<uint64_t> attr_set{0};
+    return launch_tiles(env, attr_set, gemm::grouped_gemm_pipelined_kernel<Cfg>, Cfg::SMEM, Cfg::NTHREADS,
+                        most_row_tiles(R, E, Cfg::BM) * gemm::n_tiles<Cfg>(N) * splits, s, A, B0, B1, C, offsets, gemm::RowDiv(1), E, N, K, scales);
+}
+
 // Slots of all tiles that R rows in E groups can make: the tiles, and where the last round is split two slots
 // per tile there, at most ceil(cus / 2 / 8) more in every XCD's range.
 long long most_slots(int R, int E, int BM, int NT, int split_cus) {

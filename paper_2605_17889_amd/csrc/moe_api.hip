@@ -68,7 +68,7 @@ bool on_own_device(const moe_ctx* c) {
 }
 
 struct Layout {
-    size_t topk_idx, topk_w, counts, offsets, perm, inv_perm, scratch, logits, x_perm, H, y_perm, counters, split_sums, total;
+    size_t topk_idx, topk_w, counts, offsets, perm, inv_perm, scratch, logits, x_perm, H, y_perm, counters, split_sums, part_sums, total;
 };
 
 Layout layout_for(const moe_shape* s) {
@@ -89,6 +89,7 @@ Layout layout_for(const moe_shape* s) {
     L.y_perm = take(R * s->d_model * 2);
     L.counters = take(kTileCounterBytes);
     L.split_sums = take(kSplitSumBytes);
+    L.part_sums = take(kPartSums * sizeof(int32_t));
     L.total = off ? off : 256;
     return L;
 }
@@ -312,6 +313,7 @@ int moe_create(moe_ctx** out, const moe_shape* shape, int device_id) {
     c->h_scale = nullptr;
     c->gemm.tile_counters = counters;
     c->gemm.split_sums = reinterpret_cast<int32_t*>(c->base + L.split_sums);
+    c->gemm.part_sums = reinterpret_cast<int32_t*>(c->base + L.part_sums);
     c->prof_armed = false;
     c->prof_max_calls = c->prof_calls = 0;
     for (auto& v : c->prof_launches) v = 0;

@@ -139,6 +139,13 @@ def test_few_rows_with_a_split_reduction(dtype):
     ctx.close()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,K", [(272, 16384), (1040, 8192), (4112, 14336), (2048, 2048), (144, 6272), (8208, 1152), (528, 4096)])
+@pytest.mark.parametrize("T", [17, 33, 64, 100, 129, 300, 512, 1003, 2050])
+def test_one_matrix_in_every_tile_and_split(T, N, K, dtype):
+    gemm_case([T], N, K, dtype, seed=T + N, dense=True)
+
+
 @pytest.mark.parametrize("counts,d,f", [([1, 0], 512, 1024), ([5, 9, 0, 40], 1024, 512), ([0, 0, 16], 2048, 1152), ([3], 4096, 256)])
 def test_few_rows_and_few_tiles(counts, d, f):
     ffn_case(counts, d, f, seed=len(counts))
