@@ -252,3 +252,15 @@ def test_binding_refuses_other_tensors():
     for args in ((x.float(), q, scale), (x, q[:2], scale), (x, q, scale[:1]), (x, None, scale), (x, q, None)):
         with pytest.raises(B.MoeError):
             B.moe_quantize_i8(*args)
+
+
+@pytest.mark.parametrize("d", [512, 520, 1024, 1032, 1536, 1544, 2048, 2049, 4096, 4104, 6152, 8192, 8193, 16385, 32768, 32769])
+def test_every_width_class(d):
+    for T in (1, 5):
+        x, res, w = make(T, d, torch.bfloat16, gap=3, seed=d)
+        got = outputs(T, d, torch.bfloat16)
+        B.moe_rmsnorm_i8(x, res, w, EPS, *got)
+        check(x, res, w, got)
+        _, _, q, scale = outputs(T, d, None)
+        B.moe_quantize_i8(x, q, scale)
+        check_q(q, scale, x.double(), 2 * HALF32)
