@@ -185,6 +185,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_rows_i8_kernel(
 }
 
 using Piped32x64       = I8<Config<32, 64, 64, 2, 2, 4, false>>;
+using PipedShort       = I8<Config<64, 128, 64, 2, 2, 3, false>>;
 using Piped64x64       = I8<Config<64, 64, 64, 2, 2, 5, false>>;
 using Piped64x128      = I8<Config<64, 128, 64, 2, 2, 6, false>>;
 using Piped128x128     = I8<Config<128, 128, 64, 2, 2, 5, false>>;
@@ -289,6 +290,14 @@ int few_rows(const Call& c) {
 }
 bool large_takes(int N, int K) { return gemm::offsets_fit_1w(N, K) && K >= 256; }
 
+// Few rows for each of many experts with a short reduction: three rounds and more of 128-column tiles are mostly what a tile
+// costs outside its reduction, and tiles of 256 weight rows are half as many. 32- or 64-row tiles -> 96-row ones, through 8 of
+// 128 experts of 2048 x 768: 120 tokens 113 -> 104 us, 300 122 -> 111, 600 132 -> 123; 37 tokens (2.7 rounds) 92 -> 94, 300
+// through 6 of 64 of 2048 x 1408 (2.7) 101 -> 103.
+bool many_short_tiles(const Call& c) {
+    return c.env.forced_config < 0 && c.K <= 1024 && touched(c) * (c.N / 128) >= 2.9 * compute_units(c.env.device);
+}
+
 int gateup(const Call& c) {
     if (few_rows_fits(c)) return few_rows<true, false>(c);
     int config = pick_config(c.env, c.R, c.E, gateup_tiles(c.E, c.K, c.N));
@@ -299,14 +308,20 @@ int gateup(const Call& c) {
         case 4: return grouped<GateUpMid96, GateUpMid96S>(c);
         case 3: {
             if (!single_m_tile(c.env, c.R, c.E, 32)) return grouped<GateUpTiny>(c);
+            if (many_short_tiles(c)) return grouped<GateUpMid96S>(c);
             const double nt = touched(c) * (c.N / 64);
             const int cus = compute_units(c.env.device);
             if (narrow_gateup_tiles(c.R, c.E, c.N, cus) || narrow_short_gateup_tiles(c.R, c.E, c.K, c.N, cus))
                 return one_tile_per_cu(c.R, c.E, c.N, cus) ? grouped<GateUpFewDeepS>(c) : grouped<GateUpFewS>(c);
+            // Long reductions, every expert with a few rows: 64-row tiles leave more loads in flight. 32- -> 64-row ones, layers
+            // of experts of 4096 x 14336: 16 tokens through 2 of 8 213 -> 207 us, 64 223 -> 216; 4 tokens (one row each) 139 -> 145
+            if (c.K > 1024 && c.R >= 4 * c.E) return grouped<GateUpSmallS>(c);
             return last_round_use(nt, 2.0 * cus) < 0.93 * last_round_use(nt, cus) ? grouped<GateUpTinyDeepS>(c)
                                                                                  : grouped<GateUpTinyS>(c);
         }
-        default: return grouped<GateUpSmall, GateUpSmallS>(c);
+        default:
+            if (many_short_tiles(c)) return grouped<GateUpMid96, GateUpMid96S>(c);
+            return grouped<GateUpSmall, GateUpSmallS>(c);
     }
 }
 
@@ -397,6 +412,12 @@ int product(const Call& c) {
     if (config == 0 && (!large_takes(d, c.K) || d < 256)) config = 1;
     if ((config == 1 || config == 4) && d < 128) config = 2;
     if (config == 2 && d < 64) config = 3;
+    // Reductions of up to 1024 elements over many tiles: the pipelined 64 x 128 tile, two on a compute unit. Grouped forms -> so,
+    // through 8 of 128 experts of 2048 x 768: 120 tokens 113 -> 111 us, 300 122 -> 115, 600 132 -> 122, 1000 140 -> 131 (all with
+    // gate/up); 1408 elements, 600 tokens through 6 of 64 119 -> 122.
+    if (c.env.forced_config < 0 && (config == 2 || config == 3 || config == 4) && c.K <= 512 && c.K / 64 >= PipedShort::NSTAGE &&
+        d >= 128 && touched(c) * (d / 128) >= 3.5 * cus)
+        return piped<Out<F32, PipedShort>>(c);
     switch (config) {
         case 0: return large<Out<F32, Plain1W>>(c);
         case 1:

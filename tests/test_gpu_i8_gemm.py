@@ -245,7 +245,8 @@ def ffn_case(counts, d, f, k=1, seed=0, config=None, ctx=None, check=True, sprea
 @pytest.mark.parametrize("counts,d,f", [
     ([1], 512, 128), ([0, 1, 0, 0], 512, 256), ([2, 0, 17, 40], 512, 1408), ([16] * 8, 1024, 384), ([33, 1, 64, 5], 1024, 896),
     ([100, 0, 70], 512, 640), ([300, 200], 1024, 1024), ([1000, 3], 512, 2048), ([0, 2500, 700], 1536, 768),
-    ([1, 0] * 64, 2048, 768), ([9] * 64, 2048, 1408), ([120] * 16, 512, 128)])
+    ([1, 0] * 64, 2048, 768), ([9] * 64, 2048, 1408), ([120] * 16, 512, 128), ([8, 3, 30, 1] * 32, 2048, 768),
+    ([40, 25] * 64, 2048, 768), ([5, 70] * 64, 512, 1024), ([12, 0, 5, 6], 4096, 2048)])
 def test_experts(counts, d, f):
     ffn_case(counts, d, f, seed=sum(counts))
 
