@@ -80,7 +80,7 @@ enum {
     MOE_STAGE_PERMUTE = 1,          /* histogram, scan, stable scatter */
     MOE_STAGE_GATHER = 2,           /* x -> x_perm row gather */
     MOE_STAGE_GATEUP = 3,           /* grouped GEMM  H = SiLU(Xp W1^T) * (Xp W3^T) */
-    MOE_STAGE_DOWN = 4,             /* grouped GEMM  Yp = H W2^T */
+    MOE_STAGE_DOWN = 4,             /* grouped GEMM  Yp = H W2^T (in 8 bits with H's conversion, two launches) */
     MOE_STAGE_COMBINE = 5,          /* gate-weighted gather-reduce */
     MOE_NUM_STAGES = 6
 };
@@ -208,8 +208,8 @@ int moe_last_routing(moe_ctx* ctx, int32_t T, int32_t* topk_idx, float* topk_w, 
                      int32_t* offsets, int32_t* perm, int32_t* inv_perm, void* stream);
 
 /* Per-stage device timing for measurement. moe_profile_begin() arms up to `max_calls`
- * subsequent moe_layer_forward / moe_layer_forward_microbatched / moe_layer_forward_streamed /
- * moe_expert_ffn calls: each records HIP events on the caller's stream between stages (the
+ * subsequent moe_layer_forward / moe_layer_forward_microbatched / moe_layer_forward_streamed / moe_layer_forward_i8 /
+ * moe_expert_ffn / moe_expert_ffn_i8 calls: each records HIP events on the caller's stream between stages (the
  * two GEMM stages for moe_expert_ffn). moe_profile_end() waits for those events and
  * writes, per stage, the total milliseconds (stage_ms[MOE_NUM_STAGES], host), the number of
  * kernel launches (stage_launches[MOE_NUM_STAGES], host) and the number of layer calls
@@ -363,12 +363,21 @@ int moe_gemm_i8(moe_ctx* ctx, const moe_i8* x, const float* x_scale, const int32
  * x_perm [R,d_model]; x_scale [R]; W1, W3 [E,d_ff,d_model], their scales [E,d_ff]; W2
  * [E,d_model,d_ff], w2_scale [E,d_model]; y_perm [R,d_model] bf16 out; R <= T_max * k; x_perm, the
  * weights and y_perm start at multiples of 16 bytes (not checked). d_ff <= 65536. The first call allocates
- * T_max * k * (d_ff + 4) bytes, kept until moe_destroy (MOE_ERR_WORKSPACE if that fails): make one
+ * T_max * k * (d_ff + 8) bytes, kept until moe_destroy (MOE_ERR_WORKSPACE if that fails): make one
  * before recording such calls into a HIP graph. */
 int moe_expert_ffn_i8(moe_ctx* ctx, const moe_i8* x_perm, const float* x_scale,
                       const int32_t* offsets, int32_t R, const moe_i8* W1, const float* w1_scale,
                       const moe_i8* W3, const float* w3_scale, const moe_i8* W2,
                       const float* w2_scale, moe_bf16* y_perm, void* stream);
+
+/* moe_layer_forward with its experts in 8 bits: the router reads the tokens x [T,d_model] in bf16, the experts the
+ * same tokens in 8 bits, x_i8 [T,d_model] and x_scale [T] (both are outputs of moe_rmsnorm_i8); route ->
+ * permute -> gather -> expert FFN as in moe_expert_ffn_i8 -> combine. Weights, scales, limits and the
+ * memory of the first call as there; moe_set_expert_output_fp32 and moe_last_routing as for moe_layer_forward. */
+int moe_layer_forward_i8(moe_ctx* ctx, const moe_bf16* x, const moe_i8* x_i8, const float* x_scale,
+                         const float* w_router, const float* bias, const moe_i8* W1,
+                         const float* w1_scale, const moe_i8* W3, const float* w3_scale,
+                         const moe_i8* W2, const float* w2_scale, int32_t T, moe_bf16* y, void* stream);
 
 #ifdef __cplusplus
 }

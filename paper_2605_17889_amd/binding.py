@@ -25,6 +25,7 @@ EXPORTS = (
     "moe_set_gemm_config", "moe_estimate_expert_stage", "moe_layer_forward_streamed",
     "moe_estimate_streamed_stage", "moe_permute_static", "moe_set_expert_output_fp32",
     "moe_profile_end_per_call", "moe_rmsnorm_i8", "moe_quantize_i8", "moe_gemm_i8", "moe_expert_ffn_i8",
+    "moe_layer_forward_i8",
 )
 
 
@@ -58,6 +59,7 @@ _I8_ARGUMENTS = {
     "moe_quantize_i8": (_P, _L, _I, _I, _P, _P, _P),
     "moe_gemm_i8": (_P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _I, _P),
     "moe_expert_ffn_i8": (_P, _P, _P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _P),
+    "moe_layer_forward_i8": (_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _P),
 }
 
 
@@ -392,3 +394,18 @@ def moe_expert_ffn_i8(ctx: MoeContext, x_perm, x_scale, offsets, R, W1, w1_scale
                                    _addr(offsets, torch.int32, (E + 1,), "offsets"), R, w1, s1, w3, s3, w2, s2,
                                    _addr(y_perm, torch.bfloat16, (R, d), "y_perm"), _stream_addr(stream)),
            "moe_expert_ffn_i8")
+
+
+def moe_layer_forward_i8(ctx: MoeContext, x, x_i8, x_scale, w_router, bias, W1, w1_scale, W3, w3_scale, W2, w2_scale, T, y,
+                         stream=None):
+    """moe_layer_forward with experts in 8 bits: x [T,d] bf16 for the router, x_i8 [T,d] int8 and x_scale [T] fp32 for the
+    experts (all three are outputs of moe_rmsnorm_i8), weights as for moe_expert_ffn_i8, y [T,d] bf16."""
+    d, f, E = ctx.d_model, ctx.d_ff, ctx.E
+    w1, s1 = _matrices(E, f, d, W1, w1_scale, "W1")
+    w3, s3 = _matrices(E, f, d, W3, w3_scale, "W3")
+    w2, s2 = _matrices(E, d, f, W2, w2_scale, "W2")
+    _check(lib().moe_layer_forward_i8(ctx._h, _addr(x, torch.bfloat16, (T, d), "x"), _addr(x_i8, torch.int8, (T, d), "x_i8"),
+                                      _addr(x_scale, torch.float32, (T,), "x_scale"),
+                                      _addr(w_router, torch.float32, (d, E), "w_router"),
+                                      _addr(bias, torch.float32, (E,), "bias"), w1, s1, w3, s3, w2, s2, T,
+                                      _addr(y, torch.bfloat16, (T, d), "y"), _stream_addr(stream)), "moe_layer_forward_i8")

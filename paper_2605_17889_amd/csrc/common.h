@@ -101,6 +101,9 @@ int launch_rmsnorm_i8(const moe_bf16* x, long long x_stride, const void* residua
                       const moe_bf16* weight, float eps, int T, int d, void* residual_out, moe_bf16* y, moe_i8* q,
                       float* q_scale, hipStream_t s);
 int launch_quantize_i8(const moe_bf16* x, long long x_stride, int T, int d, moe_i8* q, float* q_scale, hipStream_t s);
+// Token rows in 8 bits with their scales, grouped by expert (d a multiple of 16, every row of perm filled).
+int launch_gather_i8(const moe_i8* q, const float* scale, const int32_t* perm, int R, int d, int k, moe_i8* q_perm,
+                     float* scale_perm, hipStream_t s);
 // Products of 8-bit integers with scales (expert_gemm_i8.hip). R rows in E groups; without offsets they are one group.
 int launch_gateup_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, int d, int f,
                      int E, const moe_i8* W1, const float* w1_scale, const moe_i8* W3, const float* w3_scale, moe_bf16* H,

@@ -26,9 +26,10 @@ struct moe_ctx {
     moe_bf16* H;         // [R_max, f]
     moe_bf16* y_perm;    // [R_max, d]
     float* y_perm_f32;   // [R_max, d], allocated by moe_set_expert_output_fp32; null = keep bf16
-    // 8-bit experts (created by the first call of them, kept until destroy): H in 8 bits [R_max, f] and its scales [R_max]
+    // 8-bit experts (created by the first call of them, kept until destroy): H in 8 bits [R_max, f], its scales [R_max] and
+    // those of a layer call's grouped rows [R_max], which are kept in x_perm
     moe_i8* h_i8;
-    float* h_scale;
+    float *h_scale, *x_scale;
     // profiling
     bool prof_armed;
     int prof_max_calls, prof_calls;
@@ -192,13 +193,35 @@ int ensure_i8(moe_ctx* c) {
     if (c->h_i8) return MOE_OK;
     const size_t rows = static_cast<size_t>(c->shape.T_max) * c->shape.k, bytes = align_up(rows * c->shape.d_ff);
     void* p = nullptr;
-    if (hipMalloc(&p, bytes + rows * sizeof(float)) != hipSuccess) {
+    if (hipMalloc(&p, bytes + 2 * rows * sizeof(float)) != hipSuccess) {
         (void)hipGetLastError();
         return MOE_ERR_WORKSPACE;
     }
     c->h_i8 = static_cast<moe_i8*>(p);
     c->h_scale = reinterpret_cast<float*>(c->h_i8 + bytes);
+    c->x_scale = c->h_scale + rows;
     return MOE_OK;
+}
+
+struct ExpertsI8 {
+    const moe_i8 *w1, *w3, *w2;
+    const float *s1, *s3, *s2;
+    bool complete() const { return w1 && w3 && w2 && s1 && s3 && s2; }
+};
+
+// Expert FFN over grouped rows in 8 bits; the down projection's stage holds H's conversion too.
+int expert_ffn_i8(moe_ctx* c, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, const ExpertsI8& w, void* y,
+                  bool y_f32, hipStream_t s) {
+    const moe_shape& sh = c->shape;
+    const int rc = run_stage(c, MOE_STAGE_GATEUP, 1, s, [&] {
+        return launch_gateup_i8(c->gemm, x, x_scale, offsets, R, sh.d_model, sh.d_ff, sh.E, w.w1, w.s1, w.w3, w.s3, c->H, s);
+    });
+    if (rc != MOE_OK) return rc;
+    return run_stage(c, MOE_STAGE_DOWN, 2, s, [&] {
+        const int rc = launch_quantize_i8(c->H, sh.d_ff, R, sh.d_ff, c->h_i8, c->h_scale, s);
+        if (rc != MOE_OK) return rc;
+        return launch_product_i8(c->gemm, c->h_i8, c->h_scale, offsets, R, sh.d_model, sh.d_ff, sh.E, w.w2, w.s2, y, y_f32, s);
+    });
 }
 
 int ensure_streaming(moe_ctx* c) {
@@ -310,7 +333,7 @@ int moe_create(moe_ctx** out, const moe_shape* shape, int device_id) {
     c->y_perm = reinterpret_cast<moe_bf16*>(c->base + L.y_perm);
     c->y_perm_f32 = nullptr;
     c->h_i8 = nullptr;
-    c->h_scale = nullptr;
+    c->h_scale = c->x_scale = nullptr;
     c->gemm.tile_counters = counters;
     c->gemm.split_sums = reinterpret_cast<int32_t*>(c->base + L.split_sums);
     c->gemm.part_sums = reinterpret_cast<int32_t*>(c->base + L.part_sums);
@@ -699,16 +722,41 @@ int moe_expert_ffn_i8(moe_ctx* c, const moe_i8* x_perm, const float* x_scale, co
     const moe_shape& sh = c->shape;
     if (sh.d_model > kMaxSumI8 || sh.d_ff > kMaxRowI8) return MOE_ERR_UNSUPPORTED_SHAPE;
     if (R == 0) return MOE_OK;
-    if (!x_perm || !x_scale || !offsets || !W1 || !w1_scale || !W3 || !w3_scale || !W2 || !w2_scale || !y_perm)
-        return MOE_ERR_INVALID_ARG;
+    const ExpertsI8 w{W1, W3, W2, w1_scale, w3_scale, w2_scale};
+    if (!x_perm || !x_scale || !offsets || !w.complete() || !y_perm) return MOE_ERR_INVALID_ARG;
+    const int rc = ensure_i8(c);
+    if (rc != MOE_OK) return rc;
+    if (c->prof_armed) ++c->prof_calls;
+    return expert_ffn_i8(c, x_perm, x_scale, offsets, R, w, y_perm, false, static_cast<hipStream_t>(stream));
+}
+
+int moe_layer_forward_i8(moe_ctx* c, const moe_bf16* x, const moe_i8* x_i8, const float* x_scale, const float* w_router,
+                         const float* bias, const moe_i8* W1, const float* w1_scale, const moe_i8* W3, const float* w3_scale,
+                         const moe_i8* W2, const float* w2_scale, int32_t T, moe_bf16* y, void* stream) {
+    if (!c || T < 0 || T > c->shape.T_max) return MOE_ERR_INVALID_ARG;
+    if (!on_own_device(c)) return MOE_ERR_INVALID_ARG;
+    const moe_shape& sh = c->shape;
+    if (sh.d_model > kMaxSumI8 || sh.d_ff > kMaxRowI8) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (T == 0) return MOE_OK;
+    const ExpertsI8 w{W1, W3, W2, w1_scale, w3_scale, w2_scale};
+    if (!x || !x_i8 || !x_scale || !w_router || !w.complete() || !y) return MOE_ERR_INVALID_ARG;
     int rc = ensure_i8(c);
     if (rc != MOE_OK) return rc;
+    if (c->prof_armed) ++c->prof_calls;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    rc = launch_gateup_i8(c->gemm, x_perm, x_scale, offsets, R, sh.d_model, sh.d_ff, sh.E, W1, w1_scale, W3, w3_scale, c->H, s);
+    const int R = T * sh.k;
+    rc = route_and_permute(c, x, w_router, bias, T, s);
     if (rc != MOE_OK) return rc;
-    rc = launch_quantize_i8(c->H, sh.d_ff, R, sh.d_ff, c->h_i8, c->h_scale, s);
+    moe_i8* grouped = reinterpret_cast<moe_i8*>(c->x_perm);
+    rc = run_stage(c, MOE_STAGE_GATHER, 1, s, [&] {
+        return launch_gather_i8(x_i8, x_scale, c->perm, R, sh.d_model, sh.k, grouped, c->x_scale, s);
+    });
     if (rc != MOE_OK) return rc;
-    return launch_product_i8(c->gemm, c->h_i8, c->h_scale, offsets, R, sh.d_model, sh.d_ff, sh.E, W2, w2_scale, y_perm, false, s);
+    rc = expert_ffn_i8(c, grouped, c->x_scale, c->offsets, R, w, expert_out(c), c->y_perm_f32 != nullptr, s);
+    if (rc != MOE_OK) return rc;
+    return run_stage(c, MOE_STAGE_COMBINE, 1, s, [&] {
+        return launch_combine(expert_out(c), c->y_perm_f32 != nullptr, c->inv_perm, c->topk_w, T, sh.d_model, sh.k, y, s);
+    });
 }
 
 }  // extern "C"

@@ -301,4 +301,25 @@ int launch_quantize_i8(const moe_bf16* x, long long x_stride, int T, int d, moe_
     return launch_rows_of<false, uint16_t>(a, s);
 }
 
+// Token rows in 8 bits and their scales in the order of the grouped rows: row p is token perm[p] / k. A wavefront per row.
+__global__ __launch_bounds__(256) void gather_i8_kernel(const uint4* __restrict__ q, const float* __restrict__ scale,
+                                                        const int32_t* __restrict__ perm, int R, int pieces, int k,
+                                                        uint4* __restrict__ q_perm, float* __restrict__ scale_perm) {
+    const int p = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (p >= R) return;
+    const int t = perm[p] / k;
+    const uint4* from = q + static_cast<size_t>(t) * pieces;
+    uint4* to = q_perm + static_cast<size_t>(p) * pieces;
+    for (int i = lane; i < pieces; i += kWave) to[i] = from[i];
+    if (lane == 0) scale_perm[p] = scale[t];
+}
+
+int launch_gather_i8(const moe_i8* q, const float* scale, const int32_t* perm, int R, int d, int k, moe_i8* q_perm,
+                     float* scale_perm, hipStream_t s) {
+    if (R == 0) return MOE_OK;
+    hipLaunchKernelGGL(gather_i8_kernel, dim3((R + 3) / 4), dim3(256), 0, s, reinterpret_cast<const uint4*>(q), scale, perm, R,
+                       d / 16, k, reinterpret_cast<uint4*>(q_perm), scale_perm);
+    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
 }  // namespace moe

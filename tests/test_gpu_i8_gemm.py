@@ -411,3 +411,100 @@ def test_refusals():
         with pytest.raises(B.MoeError):
             experts(**bad)
     ctx.close()
+
+
+# ------------------------------------------------------------------------------- the layer
+
+@pytest.mark.parametrize("fp32", [False, True])
+@pytest.mark.parametrize("T,d,f,E,k", [(1, 512, 256, 8, 2), (37, 512, 640, 8, 2), (64, 1024, 384, 128, 8), (700, 512, 1024, 20, 3),
+                                       (2500, 512, 256, 64, 6)])
+def test_layer_is_its_stages(T, d, f, E, k, fp32):
+    """Bit for bit what routing, grouping, expert FFN and combine give one by one (rows of bf16 outputs)."""
+    g = gen(T)
+    x = torch.randn((T, d), generator=g, device="cuda").bfloat16()
+    q, s = torch.empty((T, d), dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+    B.moe_quantize_i8(x, q, s)
+    wr = torch.randn((d, E), generator=g, device="cuda") * 0.02
+    w = [t for shape in ((f, d), (f, d), (d, f)) for t in (whole(g, E, *shape), positive(g, E, shape[0]) / 40)]
+    ctx = B.MoeContext(T, d, f, E, k)
+    if fp32:
+        B.moe_set_expert_output_fp32(ctx, True)
+    y = torch.empty((T, d), dtype=torch.bfloat16, device="cuda")
+    B.moe_layer_forward_i8(ctx, x, q, s, wr, None, *w, T, y)
+    new = lambda *n, dtype=torch.int32: torch.empty(n, dtype=dtype, device="cuda")
+    idx, gate, counts, offsets, perm, inv = new(T, k), new(T, k, dtype=torch.float32), new(E), new(E + 1), new(T * k), new(T * k)
+    B.moe_last_routing(ctx, T, idx, gate, counts, offsets, perm, inv)
+    rows = (perm // k).long()
+    yp = new(T * k, d, dtype=torch.bfloat16)
+    other = B.MoeContext(T, d, f, E, k)
+    B.moe_expert_ffn_i8(other, q[rows], s[rows], offsets, T * k, *w, yp)
+    if fp32:        # one rounding fewer: within that of the bf16 rows
+        each = yp[inv.long()].view(T, k, d).double() * gate[..., None].double()
+        assert_near(y, each.sum(1), HALF16, HALF16 * each.abs().sum(1) * 1.01 + (k + 2) * HALF32 * each.abs().sum(1))
+    else:
+        want = torch.empty_like(y)
+        B.moe_combine(other, yp, inv, gate, T, want)
+        assert torch.equal(y, want)
+    same = new(T, k), new(T, k, dtype=torch.float32)
+    B.moe_route(other, x, wr, None, T, *same)
+    assert torch.equal(same[0], idx)
+    ctx.close()
+    other.close()
+
+
+def test_layer_replayed_and_timed_by_stage():
+    T, d, f, E, k = 40, 512, 384, 16, 4
+    g = gen(1)
+    x, q, s = torch.randn((T, d), generator=g, device="cuda").bfloat16(), whole(g, T, d), positive(g, T)
+    wr = torch.randn((d, E), generator=g, device="cuda") * 0.02
+    w = [t for shape in ((f, d), (f, d), (d, f)) for t in (whole(g, E, *shape), positive(g, E, shape[0]) / 40)]
+    ctx = B.MoeContext(T, d, f, E, k)
+    y = torch.empty((T, d), dtype=torch.bfloat16, device="cuda")
+    call = lambda: B.moe_layer_forward_i8(ctx, x, q, s, wr, None, *w, T, y)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for seed in range(4):
+        x.normal_(generator=gen(seed))
+        q.copy_(whole(gen(seed), T, d))
+        call()
+        want = y.clone()
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+    B.moe_profile_begin(ctx, 3)
+    for _ in range(3):
+        call()
+    ms, launches, calls = B.moe_profile_end(ctx)
+    assert calls == 3 and launches["gateup"] == 3 and launches["down"] == 6 and launches["gather"] == 3
+    assert all(ms[n] > 0 for n in ("route", "permute", "gather", "gateup", "down", "combine"))
+    with pytest.raises(B.MoeError):
+        B.moe_layer_forward_i8(ctx, x, q, s, wr, None, *w, T + 1, y)
+    with pytest.raises(B.MoeError):
+        B.moe_layer_forward_i8(ctx, x, None, s, wr, None, *w, T, y)
+    B.moe_layer_forward_i8(ctx, x[:0], q[:0], s[:0], wr, None, *w, 0, y[:0])
+    ctx.close()
+
+
+def test_example_block_is_near_its_bf16_form():
+    """All operators together (examples/block_i8.py). 8-bit rows and weights are off by half a step of max / 127 each: with
+    values of a normal distribution, whose largest of some hundred is 3 to 4 standard deviations, an element's error is
+    3.5 / 127 / sqrt(12) = 0.8 % of one, uncorrelated, and a product's 1.1 %; two products in a row and the head stay below 5 %."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "block_i8.py")
+    spec = importlib.util.spec_from_file_location("block_i8", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    from paper_2605_17889_amd import synth
+    cfg = synth.LayerConfig("small", 100, 512, 1024, 16, 4, seed=3)
+    block = example.Block(cfg, 2000)
+    x = synth.make_tokens(cfg, "cuda")
+    for T in (100, 1, 33):
+        logits = block(x[:T], x[:T] * 0.5)
+        want = block.in_bf16(x[:T], x[:T] * 0.5)
+        assert ((logits - want).norm() / want.norm()).item() < 0.05
+    block.ctx.close()

@@ -61,3 +61,4 @@ def gemm(lib, ctx=NULL, x=P, xs=P, offsets=NULL, R=4, E=1, N=64, K=256, w=P, ws=
 def test_products_without_a_context_are_refused(lib):
     assert gemm(lib) == INVALID
     assert lib.moe_expert_ffn_i8(NULL, P, P, P, C.c_int32(4), P, P, P, P, P, P, P, NULL) == INVALID
+    assert lib.moe_layer_forward_i8(NULL, P, P, P, P, NULL, P, P, P, P, P, P, C.c_int32(4), P, NULL) == INVALID
