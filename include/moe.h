@@ -80,7 +80,7 @@ enum {
     MOE_STAGE_PERMUTE = 1,          /* histogram, scan, stable scatter */
     MOE_STAGE_GATHER = 2,           /* x -> x_perm row gather */
     MOE_STAGE_GATEUP = 3,           /* grouped GEMM  H = SiLU(Xp W1^T) * (Xp W3^T) */
-    MOE_STAGE_DOWN = 4,             /* grouped GEMM  Yp = H W2^T (in 8 bits with H's conversion, two launches) */
+    MOE_STAGE_DOWN = 4,             /* grouped GEMM  Yp = H W2^T (in 8 bits with H's conversion, one launch or two) */
     MOE_STAGE_COMBINE = 5,          /* gate-weighted gather-reduce */
     MOE_NUM_STAGES = 6
 };

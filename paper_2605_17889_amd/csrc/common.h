@@ -108,6 +108,10 @@ int launch_gather_i8(const moe_i8* q, const float* scale, const int32_t* perm, i
 int launch_gateup_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, int d, int f,
                      int E, const moe_i8* W1, const float* w1_scale, const moe_i8* W3, const float* w3_scale, moe_bf16* H,
                      hipStream_t s);
+// The down projection straight from H in bf16, whose rows it brings to 8 bits by itself; whether it takes such a call.
+bool down_converts(const GemmEnv& env, int R, int d, int f, int E);
+int launch_down_converting_i8(const GemmEnv& env, const moe_bf16* H, const int32_t* offsets, int R, int d, int f, int E,
+                              const moe_i8* W2, const float* w2_scale, void* y, bool y_f32, hipStream_t s);
 int launch_product_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, int N, int K,
                       int E, const moe_i8* W, const float* w_scale, void* out, bool out_f32, hipStream_t s);
 

@@ -6,6 +6,7 @@
 // The kernels and the rules by which tiles are chosen are those of the bf16 products, with rows of half as many 16-bit
 // units (expert_gemm_kernel.h). The sums are whole numbers: every tile and order of them gives the same bits.
 #include "expert_gemm_launch.h"
+#include "rows_i8.h"
 
 namespace moe {
 namespace {
@@ -185,10 +186,131 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_rows_i8_kernel(
 }
 
 using Piped32x64       = I8<Config<32, 64, 64, 2, 2, 4, false>>;
+using Converted16      = I8<Config<16, 64, 64, 1, 2, 4, false, true>>;
 using PipedShort       = I8<Config<64, 128, 64, 2, 2, 3, false>>;
 using Piped64x64       = I8<Config<64, 64, 64, 2, 2, 5, false>>;
 using Piped64x128      = I8<Config<64, 128, 64, 2, 2, 6, false>>;
 using Piped128x128     = I8<Config<128, 128, 64, 2, 2, 5, false>>;
+
+// ---- down projection of a few rows straight from bf16 H -------------------------------------------------------------------
+// C = H W^T with H's rows brought to 8 bits by every workgroup for itself: the rows of its tile (K <= 2048) go through registers
+// (largest element, scale, 8-bit values: the formulas of moe_quantize_i8, bit for bit) into LDS, where they stay for the whole
+// reduction while the weights stream through a ring of stages. It saves the launch in between and costs every tile the conversion
+// of its rows. Expert FFN with the launch -> without: one token through 8 of 128 experts of 2048 x 768 13.5 -> 10.9 us, 2 17.5 ->
+// 14.9, 8 40.1 -> 38.1; one through 2 of 8 of 512 x 1024 9.5 -> 8.3, 16 (four rows an expert) 11.2 -> 10.3, 64 (16 rows) 11.9 -> 12.2.
+constexpr int kConvertedK = 2048;
+template <class Cfg>
+constexpr int converted_smem(int K) { return K / 128 * Cfg::A_BYTES + Cfg::NSTAGE * Cfg::B_BYTES + Cfg::BM * 4; }
+
+template <class Cfg, int ITS>        // ITS: 512 elements of a row each
+__global__ __launch_bounds__(Cfg::NTHREADS) void converted_rows_kernel(const uint16_t* __restrict__ H,
+                                                                       const uint16_t* __restrict__ B0, uint16_t* __restrict__ C,
+                                                                       const int32_t* __restrict__ offsets, int E, int N, int K,
+                                                                       gemm::ScalesI8 scales) {
+    using namespace gemm;
+    using Plan = LoadPlan<Cfg>;
+    constexpr int TM = Cfg::TM, TN = Cfg::TN, S = Cfg::NSTAGE, LB = Plan::LB, RPW = Cfg::BM / Cfg::NW;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const TileCoord tc = locate_tile<Cfg::BM>(offsets, E, n_tiles<Cfg>(N));
+    if (tc.expert < 0) return;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / Cfg::WN, wn = wave % Cfg::WN;
+    const int KT = K / Cfg::BK, f = 2 * K;           // K counts pairs of elements
+    const uint32_t ring = KT * Cfg::A_BYTES;
+    float* row_scale = reinterpret_cast<float*>(smem + ring + S * Cfg::B_BYTES);
+    TileScales<Cfg> sc;
+    sc.load_columns(scales, tc, wn, lane, N);
+    Raw16 raw[RPW][ITS] = {};
+#pragma unroll
+    for (int q = 0; q < RPW; ++q) {
+        const int r = q * Cfg::NW + wave;            // rows in turn: a few rows keep all wavefronts busy
+        if (r >= tc.rows) continue;
+        const uint16_t* row = H + static_cast<size_t>(tc.row0 + r) * f;
+#pragma unroll
+        for (int i = 0; i < ITS; ++i)
+            if ((i * kWave + lane) * kVec < f) raw[q][i] = load_any<Raw16>(row + (i * kWave + lane) * kVec);
+    }
+    Plan lp;
+    lp.init_fixed(wave, lane, K);
+    lp.init_b(tc, wave, B0, nullptr, N, K);
+    auto issue = [&](int stage, int kt) {
+#pragma unroll
+        for (int i = 0; i < LB; ++i)
+            dma16<Cfg::STREAM_B>(lp.b_src(i) + static_cast<size_t>(kt) * Cfg::BK, lp.b_voff[i],
+                                 ring + stage * Cfg::B_BYTES + (lp.b_lds - Cfg::A_BYTES) + i * 1024);
+    };
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s)
+        if (s < KT) issue(s, s);
+    auto convert = [&](int q) {
+        const int r = q * Cfg::NW + wave;
+        if (r >= tc.rows) return;
+        uint32_t peak = 0;
+#pragma unroll
+        for (int i = 0; i < ITS; ++i)
+#pragma unroll
+            for (int v = 0; v < kVec; ++v) peak = max(peak, __float_as_uint(unpack(raw[q][i], v)) & 0x7fffffffu);
+        auto with = [&](int other) { peak = max(peak, static_cast<uint32_t>(other)); };
+        with(row_move<0x111, 0xf>(peak));            // the largest of all lanes ends up in lane 63
+        with(row_move<0x112, 0xf>(peak));
+        with(row_move<0x114, 0xf>(peak));
+        with(row_move<0x118, 0xf>(peak));
+        with(row_move<0x142, 0xa>(peak));
+        with(row_move<0x143, 0xc>(peak));
+        peak = __builtin_amdgcn_readlane(static_cast<int>(peak), 63);
+        const bool fine = peak < 0x7f800000u;
+        const Factors8 by = factors_8_bits(peak);
+#pragma unroll
+        for (int i = 0; i < ITS; ++i) {
+            const int piece = i * kWave + lane;      // of 8 elements; 16 to a k-step
+            if (piece * kVec >= f) continue;
+            float u[kVec];
+#pragma unroll
+            for (int v = 0; v < kVec; ++v) u[v] = unpack(raw[q][i], v) * by.up;
+            const int chunk = (piece & 15) >> 1;
+            store_any(smem + (piece >> 4) * Cfg::A_BYTES + r * Cfg::ROW_BYTES + ((chunk ^ swz<Cfg::BK>(r)) << 4) + (piece & 1) * 8,
+                      to_8_bits(u, by.k, fine));
+        }
+        if (lane == 0) row_scale[r] = fine ? __uint_as_float(peak) / 127.f : __builtin_nanf("");
+    };
+#pragma unroll
+    for (int q = 0; q < RPW; ++q) convert(q);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TileScales<Cfg>::NX; ++i) sc.x[i] = row_scale[min(wm * Cfg::WTM + i * 64 + lane, tc.rows - 1)];
+
+    FragPlan<Cfg> fp;
+    fp.init(lane, wm, wn);
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    int stage = 0;
+    for (int kt = 0; kt < KT; ++kt) {
+        if (kt + S - 2 < KT) wait_vmcnt<(S - 2) * LB>(); else wait_vmcnt<0>();
+        __builtin_amdgcn_s_barrier();                // stage `stage` is there, the one before is no longer read
+        const unsigned char *a = smem + kt * Cfg::A_BYTES, *b = smem + ring + stage * Cfg::B_BYTES - Cfg::A_BYTES;
+        bf16x8 af[2][TM], bfr[2][TN];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) af[h][i] = lds16(a + fp.a_off[h] + i * Cfg::TILE_STEP);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) bfr[h][j] = lds16(b + fp.b_off[h] + j * Cfg::TILE_STEP);
+        }
+        if (kt + S - 1 < KT) issue(stage == 0 ? S - 1 : stage - 1, kt + S - 1);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = mma16<true>(bfr[h][j], af[h][i], acc[i][j]);
+        stage = stage + 1 == S ? 0 : stage + 1;
+    }
+    store_tile<Cfg>(acc, tc, fp, wm, wn, C, N, sc);
+}
 
 // A product's operands: matrices as 16-bit units, K of them per row.
 struct Call {
@@ -296,6 +418,16 @@ bool large_takes(int N, int K) { return gemm::offsets_fit_1w(N, K) && K >= 256; 
 // through 6 of 64 of 2048 x 1408 (2.7) 101 -> 103.
 bool many_short_tiles(const Call& c) {
     return c.env.forced_config < 0 && c.K <= 1024 && touched(c) * (c.N / 128) >= 2.9 * compute_units(c.env.device);
+}
+
+template <class Cfg>
+int converted(const Call& c) {
+    static std::atomic<uint64_t> attr_set[2];
+    const int which = c.K <= 512 ? 0 : 1;
+    const auto kern = which == 0 ? converted_rows_kernel<Cfg, 2> : converted_rows_kernel<Cfg, 4>;
+    return launch_tiles(c.env, attr_set[which], kern, converted_smem<Cfg>(which == 0 ? 1024 : kConvertedK), Cfg::NTHREADS,
+                        most_row_tiles(c.R, c.E, Cfg::BM) * gemm::n_tiles<Cfg>(c.N), c.s, c.A, c.B0,
+                        static_cast<uint16_t*>(c.C), c.offsets, c.E, c.N, c.K, c.scales);
 }
 
 int gateup(const Call& c) {
@@ -447,6 +579,23 @@ int launch_gateup_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, 
                      hipStream_t s) {
     if (R == 0) return MOE_OK;
     return gateup(Call{env, units(x), units(W1), units(W3), H, offsets, {x_scale, w1_scale, w3_scale, R, 1}, R, E, f, d / 2, s});
+}
+
+// A few rows for each expert that has any, and not so many tiles that the conversions add up.
+bool down_converts(const GemmEnv& env, int R, int d, int f, int E) {
+    const double touched = E == 1 ? 1.0 : touched_experts(R, E);
+    return env.forced_config < 0 && f <= kConvertedK && R <= 5.0 * touched && touched * (d / 64) <= 6.0 * compute_units(env.device);
+}
+
+int launch_down_converting_i8(const GemmEnv& env, const moe_bf16* H, const int32_t* offsets, int R, int d, int f, int E,
+                              const moe_i8* W2, const float* w2_scale, void* y, bool y_f32, hipStream_t s) {
+    if (R == 0) return MOE_OK;
+    const Call c{env, H, units(W2), nullptr, y, offsets, {nullptr, w2_scale, nullptr, R, 1}, R, E, d, f / 2, s};
+    // More than two tiles per compute unit: 16 rows and weights past the caches (8 tokens through 8 of 128 of 2048 x 768 40.8 ->
+    // 38.1 us; with fewer tiles the 32-row form, whose four wavefronts share the conversion: 16 tokens of 512 x 1024 11.3 -> 10.3)
+    if (touched(c) * (d / 64) > 2.0 * compute_units(env.device))
+        return y_f32 ? converted<gemm::F32Out<Converted16>>(c) : converted<Converted16>(c);
+    return y_f32 ? converted<gemm::F32Out<PlainTiny>>(c) : converted<PlainTiny>(c);
 }
 
 int launch_product_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, int N, int K,

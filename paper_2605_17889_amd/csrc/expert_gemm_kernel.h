@@ -607,6 +607,9 @@ struct TileScales {
         const float* xs = sc.x + tc.row0;
 #pragma unroll
         for (int i = 0; i < NX; ++i) x[i] = xs[min(wm * Cfg::WTM + i * 64 + lane, tc.rows - 1)];
+        load_columns(sc, tc, wn, lane, N);
+    }
+    __device__ __forceinline__ void load_columns(const ScalesI8& sc, const TileCoord& tc, int wn, int lane, int N) {
         const size_t first = static_cast<size_t>(tc.expert) * N + first_column<Cfg>(tc, N) + wn * COLS;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {

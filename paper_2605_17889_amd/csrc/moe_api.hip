@@ -209,7 +209,8 @@ struct ExpertsI8 {
     bool complete() const { return w1 && w3 && w2 && s1 && s3 && s2; }
 };
 
-// Expert FFN over grouped rows in 8 bits; the down projection's stage holds H's conversion too.
+// Expert FFN over grouped rows in 8 bits; the down projection's stage holds H's conversion too, in a
+// launch of its own unless the projection makes it.
 int expert_ffn_i8(moe_ctx* c, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, const ExpertsI8& w, void* y,
                   bool y_f32, hipStream_t s) {
     const moe_shape& sh = c->shape;
@@ -217,6 +218,10 @@ int expert_ffn_i8(moe_ctx* c, const moe_i8* x, const float* x_scale, const int32
         return launch_gateup_i8(c->gemm, x, x_scale, offsets, R, sh.d_model, sh.d_ff, sh.E, w.w1, w.s1, w.w3, w.s3, c->H, s);
     });
     if (rc != MOE_OK) return rc;
+    if (down_converts(c->gemm, R, sh.d_model, sh.d_ff, sh.E))
+        return run_stage(c, MOE_STAGE_DOWN, 1, s, [&] {
+            return launch_down_converting_i8(c->gemm, c->H, offsets, R, sh.d_model, sh.d_ff, sh.E, w.w2, w.s2, y, y_f32, s);
+        });
     return run_stage(c, MOE_STAGE_DOWN, 2, s, [&] {
         const int rc = launch_quantize_i8(c->H, sh.d_ff, R, sh.d_ff, c->h_i8, c->h_scale, s);
         if (rc != MOE_OK) return rc;

@@ -6,36 +6,11 @@
 // One pass over the data: a row stays in registers between its loads and its stores. With u = h * w the largest |y| is
 // the largest |u| times r and y / scale is u * 127 / max|u|, so the sum of squares and the maximum are reduced
 // together, once per row, and q does not wait for r. All of it is fp32; the sum's order is fixed by d and T.
-#include "common.h"
+#include "rows_i8.h"
 
 namespace moe {
 namespace {
 
-constexpr int kVec = 8;             // consecutive elements that a thread holds per chunk
-
-// Addresses need not be multiples of anything: rows of odd lengths and rows cut out of wider tensors start anywhere.
-// The compiler makes one wide load or store of these (the hardware takes any address).
-struct Raw16 { uint32_t w[4]; };
-struct Raw8 { uint32_t w[2]; };
-template <class T> __device__ __forceinline__ T load_any(const void* p) {
-    T v;
-    __builtin_memcpy(&v, p, sizeof(T));
-    return v;
-}
-template <class T> __device__ __forceinline__ void store_any(void* p, const T& v) { __builtin_memcpy(p, &v, sizeof(T)); }
-
-// Elements [at, at + n) of a row, n <= 8; those past n are zero. bf16 ones stay packed, two to a register.
-__device__ __forceinline__ Raw16 load_packed(const uint16_t* row, int at, int n) {
-    if (n == kVec) return load_any<Raw16>(row + at);
-    Raw16 r{};
-#pragma unroll
-    for (int i = 0; i < kVec; ++i)
-        if (i < n) r.w[i >> 1] |= static_cast<uint32_t>(row[at + i]) << (16 * (i & 1));
-    return r;
-}
-__device__ __forceinline__ float unpack(const Raw16& r, int i) {
-    return __uint_as_float((i & 1) ? (r.w[i >> 1] & 0xffff0000u) : (r.w[i >> 1] << 16));
-}
 __device__ __forceinline__ void load_row(const uint16_t* row, int at, int n, float (&v)[kVec]) {
     const Raw16 r = load_packed(row, at, n);
 #pragma unroll
@@ -84,19 +59,8 @@ __device__ __forceinline__ void store_row(float* row, int at, int n, const float
     }
 }
 
-// q = rint(u * k), |u * k| <= 127 up to rounding: in fma(u, k, 1.5 * 2^23) the sum's unit is 1, so that the one rounding
-// of the fused operation is the one to the nearest integer (ties to even), whose two's complement is the low byte.
 __device__ __forceinline__ void store_q(int8_t* row, int at, int n, const float (&u)[kVec], float k, bool fine) {
-    uint32_t b[kVec];
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) b[i] = __float_as_uint(fmaf(u[i], k, 12582912.f));
-    Raw8 r;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t lo = __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u);
-        const uint32_t hi = __builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x04000c0cu);
-        r.w[i] = fine ? lo | hi : 0u;
-    }
+    const Raw8 r = to_8_bits(u, k, fine);
     if (n == kVec) {
         store_any(row + at, r);
     } else {
@@ -236,16 +200,14 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_i8_kernel(RowArgs 
     }
     if (a.q) {
         const bool fine = peak < 0x7f800000u && top < __builtin_inff();
-        // 127 / max|u| leaves the range of fp32 for the smallest maxima: both factors are then moved by 2^100
-        const float up = peak < 0x0d800000u ? 0x1p100f : 1.f;        // below 2^-100
-        const float k = peak == 0 ? 0.f : 127.f / (__uint_as_float(peak) * up);
+        const Factors8 by = factors_8_bits(peak);
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
             if (count(c) > 0) {
                 float u[kVec];
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) u[i] = weighted(c, i) * up;
-                store_q(a.q + row, at(c), count(c), u, k, fine);
+                for (int i = 0; i < kVec; ++i) u[i] = weighted(c, i) * by.up;
+                store_q(a.q + row, at(c), count(c), u, by.k, fine);
             }
         if (lane == 0) a.scale[t] = fine ? top / 127.f : __builtin_nanf("");
     }

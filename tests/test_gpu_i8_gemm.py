@@ -263,6 +263,33 @@ def test_experts_in_every_tile(config):
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("f", [128, 640, 1024, 1152, 1408, 2048, 2176])
+@pytest.mark.parametrize("counts,d", [([1], 512), ([3, 0, 9, 1, 2, 0, 0, 1], 1024), ([1, 0, 0, 2] * 32, 2048)])
+def test_a_few_rows_convert_on_the_way(counts, d, f):
+    """H's rows in 8 bits inside the down projection are those of a launch of their own, rows of zeros and of NaN too."""
+    want = ffn_case(counts, d, f, seed=f, config=3)
+    got = ffn_case(counts, d, f, seed=f)
+    assert torch.equal(got, want)
+    g = gen(f)
+    E, R = len(counts), sum(counts)
+    x, xs, offsets = whole(g, R, d), positive(g, R), groups(counts)
+    w = [t for shape in ((f, d), (f, d), (d, f)) for t in (whole(g, E, *shape), positive(g, E, shape[0]) / 40)]
+    xs[0] = float("nan")
+    xs[R // 2] = 1e30 if R > 2 else xs[R // 2]          # H past the range: infinities
+    xs[R - 1] = 0 if R > 1 else xs[R - 1]
+    out = []
+    for config in (-1, 3):
+        ctx = B.MoeContext(R, d, f, E, 1)
+        B.moe_set_gemm_config(ctx, config)
+        y = torch.empty((R, d), dtype=torch.bfloat16, device="cuda")
+        B.moe_expert_ffn_i8(ctx, x, xs, offsets, R, *w, y)
+        torch.cuda.synchronize()
+        ctx.close()
+        out.append(y)
+    assert out[0][0].isnan().all() and (R == 1 or not out[0][R - 1].any())
+    assert torch.equal(out[0].isnan(), out[1].isnan()) and torch.equal(out[0].nan_to_num(7.0), out[1].nan_to_num(7.0))
+
+
 def test_rows_of_nothing_and_rows_of_nan():
     """A row of zeros gives zeros, a row whose scale is NaN gives NaN, and the others are what they are without them."""
     g = gen(4)
@@ -479,7 +506,7 @@ def test_layer_replayed_and_timed_by_stage():
     for _ in range(3):
         call()
     ms, launches, calls = B.moe_profile_end(ctx)
-    assert calls == 3 and launches["gateup"] == 3 and launches["down"] == 6 and launches["gather"] == 3
+    assert calls == 3 and launches["gateup"] == 3 and launches["down"] in (3, 6) and launches["gather"] == 3
     assert all(ms[n] > 0 for n in ("route", "permute", "gather", "gateup", "down", "combine"))
     with pytest.raises(B.MoeError):
         B.moe_layer_forward_i8(ctx, x, q, s, wr, None, *w, T + 1, y)
