@@ -61,13 +61,14 @@ int launch_select_hist_permute(const float* logits, int T, int E, int k, int32_t
                                int32_t* seg_tables, hipStream_t s);
 int launch_gather(const moe_bf16* x, const int32_t* perm, const int32_t* offsets, int R, int d,
                   int k, int E, moe_bf16* x_perm, hipStream_t s);
-// Counters from which persistent workgroups draw their tiles, zero between launches. A context takes a set of its
-// device's 64 and gives it back; set -1: there is none left (the caller then zeroes memory of its own). The
-// calling thread's current device must be `device`.
+// Memory that is zero between launches: counters from which persistent workgroups draw their tiles, then the sums and counters
+// of split reductions. A context takes a set of its device's 64 and gives it back; set -1: there is none left (the caller
+// then zeroes memory of its own). The calling thread's current device must be `device`.
 constexpr size_t kTileCounterBytes = kXcds * 128;
 constexpr int kPartSums = 6 << 18;        // 6 MB of them
 constexpr int kSplitTiles = 128;
 constexpr size_t kSplitSumBytes = kSplitTiles * (256 + 1) * sizeof(int32_t);   // of 256 sums and a counter each
+constexpr size_t kZeroedBytes = kTileCounterBytes + kSplitSumBytes;
 int32_t* take_tile_counters(int device, int* set);
 void give_tile_counters(int device, int set);
 // Where and how a context launches its expert GEMMs: its device, its tile counters and the tuning knobs of

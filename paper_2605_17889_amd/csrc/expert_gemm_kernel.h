@@ -1163,6 +1163,10 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_pipelined_kernel(
         ++kt;
     });
     mfma_drain(acc[TM - 1]);
+#pragma unroll
+    for (int i = 0; i < TM - 1; ++i)                 // of tiles this small the older ones too
+#pragma unroll
+        for (int j = 0; j < TN; ++j) asm volatile("" : "+a"(acc[i][j]));
     store_tile<Cfg>(acc, tc, fp, wm, wn, C, N, sc);
 }
 

@@ -69,7 +69,7 @@ bool on_own_device(const moe_ctx* c) {
 }
 
 struct Layout {
-    size_t topk_idx, topk_w, counts, offsets, perm, inv_perm, scratch, logits, x_perm, H, y_perm, counters, split_sums, part_sums, total;
+    size_t topk_idx, topk_w, counts, offsets, perm, inv_perm, scratch, logits, x_perm, H, y_perm, counters, part_sums, total;
 };
 
 Layout layout_for(const moe_shape* s) {
@@ -88,8 +88,7 @@ Layout layout_for(const moe_shape* s) {
     L.x_perm = take(R * s->d_model * 2);
     L.H = take(R * s->d_ff * 2);
     L.y_perm = take(R * s->d_model * 2);
-    L.counters = take(kTileCounterBytes);
-    L.split_sums = take(kSplitSumBytes);
+    L.counters = take(kZeroedBytes);
     L.part_sums = take(kPartSums * sizeof(int32_t));
     L.total = off ? off : 256;
     return L;
@@ -308,13 +307,9 @@ int moe_create(moe_ctx** out, const moe_shape* shape, int device_id) {
     if (err == hipSuccess) err = hipMalloc(&p, L.total);
     int32_t* counters = err == hipSuccess ? take_tile_counters(device_id, &c->counter_set) : nullptr;
     if (err == hipSuccess && counters == nullptr) {          // a copy of the host's: it has ended when it returns
-        const unsigned char zeros[kTileCounterBytes] = {};
+        static const unsigned char zeros[kZeroedBytes] = {};
         counters = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(p) + L.counters);
         err = hipMemcpy(counters, zeros, sizeof(zeros), hipMemcpyHostToDevice);
-    }
-    if (err == hipSuccess) {
-        static const unsigned char zeros[kSplitSumBytes] = {};
-        err = hipMemcpy(static_cast<unsigned char*>(p) + L.split_sums, zeros, sizeof(zeros), hipMemcpyHostToDevice);
     }
     const hipError_t back = hipSetDevice(caller_device);
     if (err != hipSuccess || back != hipSuccess) {
@@ -340,7 +335,7 @@ int moe_create(moe_ctx** out, const moe_shape* shape, int device_id) {
     c->h_i8 = nullptr;
     c->h_scale = c->x_scale = nullptr;
     c->gemm.tile_counters = counters;
-    c->gemm.split_sums = reinterpret_cast<int32_t*>(c->base + L.split_sums);
+    c->gemm.split_sums = counters + kTileCounterBytes / sizeof(int32_t);
     c->gemm.part_sums = reinterpret_cast<int32_t*>(c->base + L.part_sums);
     c->prof_armed = false;
     c->prof_max_calls = c->prof_calls = 0;

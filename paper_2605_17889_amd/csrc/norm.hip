@@ -214,11 +214,26 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_i8_kernel(RowArgs 
 }
 
 template <int TPR, int CHUNKS, bool NORM, class Residual>
-int launch_rows(const RowArgs& a, hipStream_t s) {
-    const int rows = TPR == 64 ? 4 : 1;
-    hipLaunchKernelGGL((rows_i8_kernel<TPR, CHUNKS, NORM, Residual>), dim3((a.T + rows - 1) / rows),
-                       dim3(TPR == 64 ? 256 : TPR), 0, s, a);
-    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+int launch_rows(const RowArgs& all, hipStream_t s) {
+    constexpr int rows = TPR == 64 ? 4 : 1, threads = TPR == 64 ? 256 : TPR;
+    constexpr int most = (1 << 30) / threads * rows;     // of a launch, whose threads have to be fewer than 2^32
+    for (int t0 = 0; t0 < all.T; t0 += most) {
+        RowArgs a = all;
+        a.T = all.T - t0 < most ? all.T - t0 : most;
+        const size_t at = static_cast<size_t>(t0) * all.d;
+        a.x += t0 * all.x_stride;
+        if (a.residual) a.residual = static_cast<const Residual*>(a.residual) + at;
+        if (a.residual_out) a.residual_out = static_cast<Residual*>(a.residual_out) + at;
+        if (a.y) a.y += at;
+        if (a.q) {
+            a.q += at;
+            a.scale += t0;
+        }
+        hipLaunchKernelGGL((rows_i8_kernel<TPR, CHUNKS, NORM, Residual>), dim3((a.T + rows - 1) / rows), dim3(threads), 0, s, a);
+        if (hipGetLastError() != hipSuccess) return MOE_ERR_HIP;
+        if (all.T - t0 <= most) break;                   // t0 + most may pass the range
+    }
+    return MOE_OK;
 }
 
 // Threads and chunks by the row's length: the norm, which holds three tensors' chunks, runs with one chunk per thread up to

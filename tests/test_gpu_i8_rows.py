@@ -264,3 +264,18 @@ def test_every_width_class(d):
         _, _, q, scale = outputs(T, d, None)
         B.moe_quantize_i8(x, q, scale)
         check_q(q, scale, x.double(), 2 * HALF32)
+
+
+def test_more_rows_than_a_launch_has_threads_for():
+    """2^24 rows and more, four to a workgroup of 256: the last ones are what a call of them alone gives."""
+    T, d = (1 << 24) + 77, 8
+    x = torch.randn((T, d), generator=gen(1), device="cuda").bfloat16()
+    q, scale = torch.empty((T, d), dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+    B.moe_quantize_i8(x, q, scale)
+    for rows in (slice(0, 5000), slice((1 << 24) - 50, T)):
+        check_q(q[rows], scale[rows], x[rows].double(), 2 * HALF32)
+    res, w = x.float() * 2, torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    h, y = torch.empty_like(res), torch.empty_like(x)
+    B.moe_rmsnorm_i8(x, res, w, EPS, h, y, q, scale)
+    for rows in (slice(0, 5000), slice((1 << 24) - 50, T)):
+        check(x[rows], res[rows], w, (h[rows], y[rows], q[rows], scale[rows]))
