@@ -13,11 +13,12 @@
 // it sustains ~13 % more FLOP/s on random operands. The weight fragment is the first MFMA
 // operand, so a lane ends up with four consecutive output columns of one row (one 8-byte store).
 //
-// Four kernels share the tile mapping, the LDS layout and the fragment plan:
+// Five kernels share the tile mapping, the LDS layout and the fragment plan:
 //   grouped_gemm_kernel       ring of NSTAGE LDS stages, compiler-scheduled k-step (small tiles:
 //                           decode and micro-batch sized expert groups, HBM-bound);
 //   grouped_gemm_routed_kernel  the same tiles for gate/up of a few tokens, which finds its groups
 //                           in the selected experts instead of a permutation's tables;
+//   grouped_gemm_pipelined_kernel  small tiles with every load behind an MFMA (8-bit operands);
 //   grouped_gemm_1w_kernel    the large compute-bound tiles, one wavefront per SIMD: hand-placed
 //                           software pipeline with at most a few other instructions behind every
 //                           MFMA, tiles of five heights, in short reductions persistent workgroups;
