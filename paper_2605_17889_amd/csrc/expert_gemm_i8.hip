@@ -377,9 +377,10 @@ int grouped(const Call& c) {
 template <class Cfg>
 int large(const Call& c) {
     uint16_t* out = static_cast<uint16_t*>(c.C);
-    if (c.K % 128 == 0)
-        return launch_1w<Cfg, false>(c.env, c.A, c.B0, c.B1, out, c.offsets, nullptr, 1, c.R, c.E, c.N, c.K, c.s, c.scales);
-    return launch_1w<Cfg, true>(c.env, c.A, c.B0, c.B1, out, c.offsets, nullptr, 1, c.R, c.E, c.N, c.K, c.s, c.scales);
+    if constexpr (!Cfg::DUAL)                        // gate/up reduces over d_model, a multiple of 512
+        if (c.K % 128 != 0)
+            return launch_1w<Cfg, true>(c.env, c.A, c.B0, c.B1, out, c.offsets, nullptr, 1, c.R, c.E, c.N, c.K, c.s, c.scales);
+    return launch_1w<Cfg, false>(c.env, c.A, c.B0, c.B1, out, c.offsets, nullptr, 1, c.R, c.E, c.N, c.K, c.s, c.scales);
 }
 // Experts that the call is expected to touch.
 double touched(const Call& c) { return c.E == 1 ? 1.0 : touched_experts(c.R, c.E); }
@@ -457,38 +458,42 @@ int gateup(const Call& c) {
     }
 }
 
-// ---- one matrix: its tiles are known, so the tile and the split of the reduction are priced ------------------------------
+// ---- one matrix, or a few not so large ones: the tile and the split of the reduction are priced ---------------------------
 // A compute unit takes in 50 GB/s of rows and weights that come from memory (85 from L2), whatever the tile, so that a k-step
 // costs by the bytes of its stage; small tiles load each byte more often, large ones leave compute units without any. Where
 // both hurt (few rows, narrow outputs, long reductions) the reduction is split over workgroups, whose int32 sums go to memory
 // and are joined by a second launch. us of a k-step of 128 elements, weights from memory; `pair`: of two workgroups on a
 // compute unit. Priced -> the tile that the grouped rules take, in us: 64 rows, 14336 x 4096 columns 30.8 -> 17.7; 128 rows there
 // 36.0 -> 22.9; 512 rows 93 -> 51; 1003 92 -> 68; 256 rows, 8192 x 1024 17.8 -> 11.9; 2048 rows there 50.7 -> 28.8; 128 rows,
-// 16384 x 256 24.6 -> 9.2; 1003 rows, 2048 x 2048 13.6 -> 9.2; 512 rows, 8192 x 8192 53 -> 41.
-enum class OneTile { t32x64, t64x64, t64x128, t128x128, large };
-struct OneTilePrice {
-    OneTile tile;
+// 16384 x 256 24.6 -> 9.2; 1003 rows, 2048 x 2048 13.6 -> 9.2; 512 rows, 8192 x 8192 53 -> 41. Groups of 128 rows and more, up to
+// 128 MB of weights: 750 rows for each of 2 of 2048 x 2048 18.3 -> 14.1, 188 of 8 there 19.1 -> 16.9, 150 of 2 of 8192 x 4096 33.6
+// -> 28.0; with more weights or fewer rows their stream decides, for which the grouped rules are drawn (112 rows of 64 of 1408 x
+// 2048, 184 MB, gate/up included: 149, priced 162).
+enum class Tile { t32x64, t64x64, t64x128, t128x128, large };
+struct TilePrice {
+    Tile tile;
     int rows, cols, stages;
     double step, pair, fixed;        // us; without a pair one workgroup fills a compute unit
 };
-constexpr OneTilePrice kOneTiles[] = {
-    {OneTile::t32x64, 32, 64, 4, 0.28, 0.46, 1.5},    {OneTile::t64x64, 64, 64, 5, 0.32, 0.57, 1.5},
-    {OneTile::t64x128, 64, 128, 6, 0.47, 0.0, 1.5},   {OneTile::t128x128, 128, 128, 5, 0.62, 0.0, 1.5},
-    {OneTile::large, 256, 256, 4, 1.45, 0.0, 4.0},
+constexpr TilePrice kTiles[] = {
+    {Tile::t32x64, 32, 64, 4, 0.28, 0.46, 1.5},    {Tile::t64x64, 64, 64, 5, 0.32, 0.57, 1.5},
+    {Tile::t64x128, 64, 128, 6, 0.47, 0.0, 1.5},   {Tile::t128x128, 128, 128, 5, 0.62, 0.0, 1.5},
+    {Tile::large, 256, 256, 4, 1.45, 0.0, 4.0},
 };
-struct OnePlan {
-    OneTile tile;
+struct Plan {
+    Tile tile;
     int splits;
     double us;
 };
-OnePlan plan_one(const Call& c) {
+Plan price(const Call& c) {
     const int cus = compute_units(c.env.device);
-    const double bytes = 2.0 * c.N * c.K, ksteps = c.K / 64.0;
-    OnePlan best{OneTile::t32x64, 1, 1e30};
-    for (const OneTilePrice& t : kOneTiles) {
-        if (c.N < t.cols || c.K / 64 < t.stages || (t.tile == OneTile::large && !large_takes(c.N, c.K))) continue;
-        const double tiles = std::ceil(c.R / static_cast<double>(t.rows)) * ((c.N + t.cols - 1) / t.cols);
-        const bool can_split = c.offsets == nullptr && t.tile <= OneTile::t64x128;
+    const double bytes = 2.0 * c.E * c.N * c.K, ksteps = c.K / 64.0;
+    Plan best{Tile::t32x64, 1, 1e30};
+    for (const TilePrice& t : kTiles) {
+        if (c.N < t.cols || c.K / 64 < t.stages || (t.tile == Tile::large && !large_takes(c.N, c.K))) continue;
+        const double row_tiles_of = c.E == 1 ? std::ceil(c.R / static_cast<double>(t.rows)) : row_tiles(c.R, c.E, t.rows);
+        const double tiles = row_tiles_of * ((c.N + t.cols - 1) / t.cols);
+        const bool can_split = c.offsets == nullptr && t.tile <= Tile::t64x128;
         for (int s = 1; s <= (can_split ? 16 : 1); ++s) {
             if (c.K / 64 / s < t.stages || (s > 1 && static_cast<double>(s) * c.R * c.N > kPartSums)) break;
             const double n = tiles * s, each = std::ceil(n / cus);           // workgroups of a compute unit
@@ -497,7 +502,7 @@ OnePlan plan_one(const Call& c) {
                 rounds = std::ceil(each / 2);
                 step = std::floor(each / 2) * t.pair + (each - 2 * std::floor(each / 2)) * t.step;
             }
-            if (t.tile == OneTile::large) {          // the tiles of a last round that is less than half full are run as two halves
+            if (t.tile == Tile::large) {          // the tiles of a last round that is less than half full are run as two halves
                 const double rem = n - std::floor(n / cus) * cus;
                 if (rem > 0 && 2 * rem <= cus) step += 0.88 - t.step;
             }
@@ -505,7 +510,7 @@ OnePlan plan_one(const Call& c) {
             const double us = std::max(ksteps / s * step, bytes / 6e6) + rounds * t.fixed +
                               (s > 1 ? 3.0 + 8e-6 / 4 * s * c.R * c.N : 0.0);
             const double price = s > 1 ? us / 0.9 : us;
-            if (price < best.us) best = OnePlan{t.tile, s, price};
+            if (price < best.us) best = Plan{t.tile, s, price};
         }
     }
     return best;
@@ -516,14 +521,18 @@ int one_tile(const Call& c, int splits) {
         if (splits > 1) return split<F32, Cfg>(c, splits);
     return piped<Out<F32, Cfg>>(c);
 }
+bool is_priced(const Call& c) {
+    if (c.env.forced_config >= 0 || c.R <= kFewRows) return false;
+    return c.E == 1 || (c.R >= 128.0 * c.E && 2.0 * c.E * c.N * c.K <= 128e6);
+}
 template <bool F32>
-int product_of_one(const Call& c) {
-    const OnePlan plan = plan_one(c);
+int priced(const Call& c) {
+    const Plan plan = price(c);
     switch (plan.tile) {
-        case OneTile::t64x64: return one_tile<F32, Piped64x64>(c, plan.splits);
-        case OneTile::t64x128: return one_tile<F32, Piped64x128>(c, plan.splits);
-        case OneTile::t128x128: return one_tile<F32, Piped128x128>(c, 1);
-        case OneTile::large: return large<Out<F32, Plain1W>>(c);
+        case Tile::t64x64: return one_tile<F32, Piped64x64>(c, plan.splits);
+        case Tile::t64x128: return one_tile<F32, Piped64x128>(c, plan.splits);
+        case Tile::t128x128: return one_tile<F32, Piped128x128>(c, 1);
+        case Tile::large: return large<Out<F32, Plain1W>>(c);
         default: break;
     }
     // narrower or shorter than every tile of the table (or a reduction of less than four k-steps): the grouped forms
@@ -535,7 +544,7 @@ int product_of_one(const Call& c) {
 template <bool F32>
 int product(const Call& c) {
     if (few_rows_fits(c)) return few_rows<false, F32>(c);
-    if (c.E == 1 && c.R > kFewRows && c.env.forced_config < 0) return product_of_one<F32>(c);
+    if (is_priced(c)) return priced<F32>(c);
     const int d = c.N;
     const bool wide_mid = static_cast<long long>(c.E) * (d / 256) >= 160;
     const int cus = compute_units(c.env.device);
