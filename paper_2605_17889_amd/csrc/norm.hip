@@ -109,7 +109,9 @@ struct RowArgs {
     float* scale;                    // [T]
 };
 
-// TPR threads per row, each with CHUNKS chunks of 8 elements: chunk c of thread t is elements 8 * (c * TPR + t) to + 7.
+// TPR threads per row, each with CHUNKS chunks of 8 elements: chunk c of thread t is elements 8 * (c * TPR + t) to + 7. The last
+// chunk of a width that is no multiple of 8 starts at d - 8: it holds some elements of the one before a second time, leaves
+// them out of the sum and stores the same bits to them. Element by element, in one lane of a row, it cost more than all others.
 // A workgroup holds one row, or with TPR = 64 a row per wavefront.
 template <int TPR, int CHUNKS, bool NORM, class Residual>
 __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_i8_kernel(RowArgs a) {
@@ -122,8 +124,9 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_i8_kernel(RowArgs 
     const size_t row = static_cast<size_t>(t) * a.d;
     const uint16_t* x = a.x + static_cast<long long>(t) * a.x_stride;
     const Residual* res = a.residual ? static_cast<const Residual*>(a.residual) + row : nullptr;
-    auto at = [&](int c) { return (c * TPR + lane) * kVec; };
-    auto count = [&](int c) { return min(kVec, a.d - at(c)); };      // 0 or less: nothing of this chunk is in the row
+    auto nominal = [&](int c) { return (c * TPR + lane) * kVec; };
+    auto at = [&](int c) { return min(nominal(c), max(a.d - kVec, 0)); };
+    auto count = [&](int c) { return nominal(c) < a.d ? min(kVec, a.d) : 0; };       // 0: nothing of this chunk is in the row
 
     float h[CHUNKS][kVec];
 #pragma unroll
@@ -157,7 +160,10 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_i8_kernel(RowArgs 
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                if constexpr (NORM) sum = fmaf(h[c][i], h[c][i], sum);
+                if constexpr (NORM) {
+                    const float once = nominal(c) <= at(c) + i ? h[c][i] : 0.f;
+                    sum = fmaf(once, once, sum);
+                }
                 peak = max(peak, __float_as_uint(weighted(c, i)) & 0x7fffffffu);
             }
         reduce_row<WAVES>(sum, peak, sums[which], peaks[which]);

@@ -279,3 +279,27 @@ def test_more_rows_than_a_launch_has_threads_for():
     B.moe_rmsnorm_i8(x, res, w, EPS, h, y, q, scale)
     for rows in (slice(0, 5000), slice((1 << 24) - 50, T)):
         check(x[rows], res[rows], w, (h[rows], y[rows], q[rows], scale[rows]))
+
+
+@pytest.mark.parametrize("d", [1, 5, 7, 8, 9, 15, 61, 509, 1021, 1111, 2047, 4093, 8191, 16383, 32767, 65521, 65529, 65531, 65535])
+def test_odd_widths_at_every_alignment(d):
+    """Rows of odd widths, from any element on and in place; nothing beside them is written."""
+    T = 17
+    for kind in (None, torch.bfloat16, torch.float32):
+        x, res, w = make(T, d, kind, gap=5, seed=d)
+        flat = [torch.full((T * d + 64,), 7, dtype=t, device="cuda") if t is not None else None
+                for t in (kind, torch.bfloat16, torch.int8)]
+        for start in (0, 1, 8):
+            for f in flat:
+                if f is not None:
+                    f.fill_(7)
+            h, y, q = (None if f is None else f[start + 8:start + 8 + T * d].view(T, d) for f in flat)
+            scale = torch.full((T,), -1.0, device="cuda")
+            B.moe_rmsnorm_i8(x, res, w, EPS, h, y, q, scale)
+            check(x, res, w, (h, y, q, scale))
+            if res is not None:
+                stream = res.clone()
+                B.moe_rmsnorm_i8(x, stream, w, EPS, residual_out=stream, y=(again := torch.empty_like(y)))
+                assert torch.equal(stream, h) and torch.equal(again, y)
+            for f in flat:
+                assert f is None or ((f[:start + 8] == 7).all() and (f[start + 8 + T * d:] == 7).all())
