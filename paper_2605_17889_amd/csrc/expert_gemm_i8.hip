@@ -469,7 +469,7 @@ int gateup(const Call& c) {
 // 128 MB of weights: 750 rows for each of 2 of 2048 x 2048 18.3 -> 14.1, 188 of 8 there 19.1 -> 16.9, 150 of 2 of 8192 x 4096 33.6
 // -> 28.0; with more weights or fewer rows their stream decides, for which the grouped rules are drawn (112 rows of 64 of 1408 x
 // 2048, 184 MB, gate/up included: 149, priced 162).
-enum class Tile { t32x64, t64x64, t64x128, t128x128, large };
+enum class Tile { t32x64, t64x64, t64x128, short64x128, t128x128, large };
 struct TilePrice {
     Tile tile;
     int rows, cols, stages;
@@ -477,8 +477,8 @@ struct TilePrice {
 };
 constexpr TilePrice kTiles[] = {
     {Tile::t32x64, 32, 64, 4, 0.28, 0.46, 1.5},    {Tile::t64x64, 64, 64, 5, 0.32, 0.57, 1.5},
-    {Tile::t64x128, 64, 128, 6, 0.47, 0.0, 1.5},   {Tile::t128x128, 128, 128, 5, 0.62, 0.0, 1.5},
-    {Tile::large, 256, 256, 4, 1.45, 0.0, 4.0},
+    {Tile::t64x128, 64, 128, 6, 0.47, 0.0, 1.5},   {Tile::short64x128, 64, 128, 3, 0.50, 0.85, 1.5},
+    {Tile::t128x128, 128, 128, 5, 0.62, 0.0, 1.5}, {Tile::large, 256, 256, 4, 1.45, 0.0, 4.0},
 };
 struct Plan {
     Tile tile;
@@ -531,14 +531,17 @@ int priced(const Call& c) {
     switch (plan.tile) {
         case Tile::t64x64: return one_tile<F32, Piped64x64>(c, plan.splits);
         case Tile::t64x128: return one_tile<F32, Piped64x128>(c, plan.splits);
+        case Tile::short64x128: return one_tile<F32, PipedShort>(c, 1);
         case Tile::t128x128: return one_tile<F32, Piped128x128>(c, 1);
         case Tile::large: return large<Out<F32, Plain1W>>(c);
         default: break;
     }
-    // narrower or shorter than every tile of the table (or a reduction of less than four k-steps): the grouped forms
     if (c.N < 64) return grouped<Out<F32, PlainFew>>(c);
-    if (c.K / 64 < Piped32x64::NSTAGE) return grouped<Out<F32, PlainTiny>>(c);
-    return one_tile<F32, Piped32x64>(c, plan.splits);
+    if (c.K / 64 >= Piped32x64::NSTAGE) return one_tile<F32, Piped32x64>(c, plan.splits);
+    // Shorter than the rings of the table's tiles: the grouped form of two workgroups per compute unit where they fill those (6649
+    // rows, 256 x 11776 110 -> 72 us, 1000 rows, 256 x 4096 9.0 -> 6.4), else smaller tiles (300 rows, 256 x 2048 4.2, 3.5)
+    if (c.N >= 128 && std::ceil(c.R / 64.0) * (c.N / 128) >= compute_units(c.env.device)) return grouped<Out<F32, PlainSmallWide>>(c);
+    return grouped<Out<F32, PlainSmall>>(c);
 }
 
 template <bool F32>

@@ -139,6 +139,13 @@ def test_few_rows_with_a_split_reduction(dtype):
     ctx.close()
 
 
+@pytest.mark.parametrize("T,N,K", [(6649, 1776, 128), (6649, 1776, 256), (5000, 2064, 384), (1000, 4096, 512), (300, 2048, 256),
+                                   (300, 2048, 384), (40, 64, 384), (100, 32000, 384), (3000, 96, 256)])
+def test_short_reductions(T, N, K):
+    for dtype in (torch.bfloat16, torch.float32):
+        gemm_case([T], N, K, dtype, seed=T + K, dense=True)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("N,K", [(272, 16384), (1040, 8192), (4112, 14336), (2048, 2048), (144, 6272), (8208, 1152), (528, 4096)])
 @pytest.mark.parametrize("T", [17, 33, 64, 100, 129, 300, 512, 1003, 2050])
