@@ -72,10 +72,11 @@ __device__ __forceinline__ void store_q(int8_t* row, int at, int n, const float 
 
 // Sum and maximum over the threads of a row, the same bits in all of them: butterflies inside a wavefront, then the
 // wavefronts' results in their order. |values| as integers: a NaN counts as more than infinity and stays.
-template <int WAVES>
+template <int TPR>
 __device__ __forceinline__ void reduce_row(float& sum, uint32_t& peak, float* sums, uint32_t* peaks) {
+    constexpr int WAVES = TPR / kWave;
 #pragma unroll
-    for (int s = 32; s > 0; s >>= 1) {
+    for (int s = (TPR < kWave ? TPR : kWave) / 2; s > 0; s >>= 1) {
         sum += __shfl_xor(sum, s);
         peak = max(peak, static_cast<uint32_t>(__shfl_xor(static_cast<int>(peak), s)));
     }
@@ -109,18 +110,20 @@ struct RowArgs {
     float* scale;                    // [T]
 };
 
+constexpr int threads_of(int tpr) { return tpr <= kWave ? 256 : tpr; }
+
 // TPR threads per row, each with CHUNKS chunks of 8 elements: chunk c of thread t is elements 8 * (c * TPR + t) to + 7. The last
 // chunk of a width that is no multiple of 8 starts at d - 8: it holds some elements of the one before a second time, leaves
 // them out of the sum and stores the same bits to them. Element by element, in one lane of a row, it cost more than all others.
-// A workgroup holds one row, or with TPR = 64 a row per wavefront.
+// A workgroup holds one row, or with up to 64 threads per row as many as its 256 threads have room for.
 template <int TPR, int CHUNKS, bool NORM, class Residual>
-__global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_i8_kernel(RowArgs a) {
-    constexpr int WAVES = TPR / kWave;
+__global__ __launch_bounds__(threads_of(TPR)) void rows_i8_kernel(RowArgs a) {
+    constexpr int WAVES = TPR > kWave ? TPR / kWave : 1, ROWS = threads_of(TPR) / TPR;
     __shared__ float sums[2][WAVES];
     __shared__ uint32_t peaks[2][WAVES];
-    const int t = TPR == 64 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-    if (TPR == 64 && t >= a.T) return;               // the whole wavefront; no barrier follows with TPR = 64
-    const int lane = TPR == 64 ? threadIdx.x & 63 : threadIdx.x;
+    const int t = blockIdx.x * ROWS + threadIdx.x / TPR;
+    if (ROWS > 1 && t >= a.T) return;                // all threads of the row; no barrier follows where there are several
+    const int lane = threadIdx.x % TPR;
     const size_t row = static_cast<size_t>(t) * a.d;
     const uint16_t* x = a.x + static_cast<long long>(t) * a.x_stride;
     const Residual* res = a.residual ? static_cast<const Residual*>(a.residual) + row : nullptr;
@@ -166,7 +169,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_i8_kernel(RowArgs 
                 }
                 peak = max(peak, __float_as_uint(weighted(c, i)) & 0x7fffffffu);
             }
-        reduce_row<WAVES>(sum, peak, sums[which], peaks[which]);
+        reduce_row<TPR>(sum, peak, sums[which], peaks[which]);
     };
     float sum;
     uint32_t peak;
@@ -221,7 +224,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR) void rows_i8_kernel(RowArgs 
 
 template <int TPR, int CHUNKS, bool NORM, class Residual>
 int launch_rows(const RowArgs& all, hipStream_t s) {
-    constexpr int rows = TPR == 64 ? 4 : 1, threads = TPR == 64 ? 256 : TPR;
+    constexpr int threads = threads_of(TPR), rows = threads / TPR;
     constexpr int most = (1 << 30) / threads * rows;     // of a launch, whose threads have to be fewer than 2^32
     for (int t0 = 0; t0 < all.T; t0 += most) {
         RowArgs a = all;
@@ -246,11 +249,15 @@ int launch_rows(const RowArgs& all, hipStream_t s) {
 // 1024 threads, the conversion with a wavefront per row (no barrier) or a few chunks per thread. us, 256 threads -> so: norm of
 // 8192 rows of 4096 57.1 -> 51.4 (5.9 TB/s), of 6144 89.6 -> 84.9 (5.3), with an fp32 residual 128 -> 116 (5.6), 16384 of 768
 // 31.4 -> 22.9, one of 6144 4.5 -> 3.5; rows in 8 bits, 40024 of 768 33.6 -> 19.7 (4.7), of 1408 39.0 -> 29.9 (5.7), 16384 of 16384
-// 146 -> 133 (6.1), 32 of 14336 4.7 -> 3.2; 4000 of 4096 10.7 with two chunks, 11.6 with 512 threads.
+// 146 -> 133 (6.1), 32 of 14336 4.7 -> 3.2; 4000 of 4096 10.7 with two chunks, 11.6 with 512 threads. Narrow rows (one head) share a
+// wavefront, a wavefront per row -> so: norm of 390625 rows of 128 190 -> 83 us, rows in 8 bits 89 -> 29, of 64 166 -> 29 (781250).
 template <bool NORM, class Residual>
 int launch_rows_of(const RowArgs& a, hipStream_t s) {
     if (a.T == 0) return MOE_OK;
     const int chunks = (a.d + kVec - 1) / kVec;
+    if (chunks <= 8) return launch_rows<8, 1, NORM, Residual>(a, s);
+    if (chunks <= 16) return launch_rows<16, 1, NORM, Residual>(a, s);
+    if (chunks <= 32) return launch_rows<32, 1, NORM, Residual>(a, s);
     if (chunks <= 64) return launch_rows<64, 1, NORM, Residual>(a, s);
     if constexpr (NORM) {
         if (chunks <= 128) return launch_rows<128, 1, NORM, Residual>(a, s);

@@ -254,9 +254,9 @@ def test_binding_refuses_other_tensors():
             B.moe_quantize_i8(*args)
 
 
-@pytest.mark.parametrize("d", [512, 520, 1024, 1032, 1536, 1544, 2048, 2049, 4096, 4104, 6152, 8192, 8193, 16385, 32768, 32769])
+@pytest.mark.parametrize("d", [1, 8, 63, 64, 65, 127, 128, 129, 200, 255, 256, 257, 512, 520, 1024, 1032, 1536, 1544, 2048, 2049, 4096, 4104, 6152, 8192, 8193, 16385, 32768, 32769])
 def test_every_width_class(d):
-    for T in (1, 5):
+    for T in (1, 5, 67):
         x, res, w = make(T, d, torch.bfloat16, gap=3, seed=d)
         got = outputs(T, d, torch.bfloat16)
         B.moe_rmsnorm_i8(x, res, w, EPS, *got)
@@ -267,18 +267,22 @@ def test_every_width_class(d):
 
 
 def test_more_rows_than_a_launch_has_threads_for():
-    """2^24 rows and more, four to a workgroup of 256: the last ones are what a call of them alone gives."""
-    T, d = (1 << 24) + 77, 8
-    x = torch.randn((T, d), generator=gen(1), device="cuda").bfloat16()
+    """2^20 rows and more of 1024 threads each are several launches: rows on both sides of the border, in every tensor."""
+    T, d = (1 << 20) + 5, 8200
+    x = torch.empty((T, d), dtype=torch.bfloat16, device="cuda")
+    x[:] = torch.randn(d, generator=gen(1), device="cuda").bfloat16()
+    near_border = slice((1 << 20) - 3, T)
+    x[near_border] = torch.randn((8, d), generator=gen(2), device="cuda").bfloat16()
     q, scale = torch.empty((T, d), dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
     B.moe_quantize_i8(x, q, scale)
-    for rows in (slice(0, 5000), slice((1 << 24) - 50, T)):
+    for rows in (slice(0, 3), near_border):
         check_q(q[rows], scale[rows], x[rows].double(), 2 * HALF32)
-    res, w = x.float() * 2, torch.ones(d, dtype=torch.bfloat16, device="cuda")
-    h, y = torch.empty_like(res), torch.empty_like(x)
-    B.moe_rmsnorm_i8(x, res, w, EPS, h, y, q, scale)
-    for rows in (slice(0, 5000), slice((1 << 24) - 50, T)):
-        check(x[rows], res[rows], w, (h[rows], y[rows], q[rows], scale[rows]))
+    assert torch.equal(q[1000], q[0]) and torch.equal(scale[:(1 << 20) - 3], scale[:1].expand((1 << 20) - 3))
+    w = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    B.moe_rmsnorm_i8(x, x, w, EPS, h, y, q, scale)
+    for rows in (slice(0, 3), near_border):
+        check(x[rows], x[rows], w, (h[rows], y[rows], q[rows], scale[rows]))
 
 
 @pytest.mark.parametrize("d", [1, 5, 7, 8, 9, 15, 61, 509, 1021, 1111, 2047, 4093, 8191, 16383, 32767, 65521, 65529, 65531, 65535])
