@@ -426,9 +426,9 @@ int converted(const Call& c) {
     static std::atomic<uint64_t> attr_set[2];
     const int which = c.K <= 512 ? 0 : 1;
     const auto kern = which == 0 ? converted_rows_kernel<Cfg, 2> : converted_rows_kernel<Cfg, 4>;
-    return launch_tiles(c.env, attr_set[which], kern, converted_smem<Cfg>(which == 0 ? 1024 : kConvertedK), Cfg::NTHREADS,
-                        most_row_tiles(c.R, c.E, Cfg::BM) * gemm::n_tiles<Cfg>(c.N), c.s, c.A, c.B0,
-                        static_cast<uint16_t*>(c.C), c.offsets, c.E, c.N, c.K, c.scales);
+    return launch_tiles_sized(c.env, attr_set[which], kern, converted_smem<Cfg>(which == 0 ? 1024 : kConvertedK),
+                              converted_smem<Cfg>(2 * c.K), Cfg::NTHREADS, most_row_tiles(c.R, c.E, Cfg::BM) * gemm::n_tiles<Cfg>(c.N),
+                              c.s, c.A, c.B0, static_cast<uint16_t*>(c.C), c.offsets, c.E, c.N, c.K, c.scales);
 }
 
 int gateup(const Call& c) {
@@ -603,9 +603,10 @@ int launch_down_converting_i8(const GemmEnv& env, const moe_bf16* H, const int32
                               const moe_i8* W2, const float* w2_scale, void* y, bool y_f32, hipStream_t s) {
     if (R == 0) return MOE_OK;
     const Call c{env, H, units(W2), nullptr, y, offsets, {nullptr, w2_scale, nullptr, R, 1}, R, E, d, f / 2, s};
-    // More than two tiles per compute unit: 16 rows and weights past the caches (8 tokens through 8 of 128 of 2048 x 768 40.8 ->
-    // 38.1 us; with fewer tiles the 32-row form, whose four wavefronts share the conversion: 16 tokens of 512 x 1024 11.3 -> 10.3)
-    if (touched(c) * (d / 64) > 2.0 * compute_units(env.device))
+    // Where the tiles are more than a few: 16 rows and weights past the caches (8 tokens through 8 of 128 of 2048 x 768 40.8 ->
+    // 38.1 us, 2 through 6 of 64 of 2048 x 1408 27.5 -> 24.0); with fewer tiles the 32-row form, whose four wavefronts share the
+    // conversion (16 tokens of 512 x 1024 11.3 -> 10.3, one through 8 of 128 11.2 -> 10.6)
+    if (touched(c) * (d / 64) > (f <= 1024 ? 2.0 : 1.0) * compute_units(env.device))
         return y_f32 ? converted<gemm::F32Out<Converted16>>(c) : converted<Converted16>(c);
     return y_f32 ? converted<gemm::F32Out<PlainTiny>>(c) : converted<PlainTiny>(c);
 }

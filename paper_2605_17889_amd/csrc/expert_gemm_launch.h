@@ -14,16 +14,17 @@ using gemm::Config;
 template <bool F32, class Cfg>
 using Out = std::conditional_t<F32, gemm::F32Out<Cfg>, Cfg>;
 
+// `most_smem`: the LDS of the largest launch of this kernel, `smem` that of this one.
 template <class Kernel, class... Args>
-int launch_tiles(const GemmEnv& env, std::atomic<uint64_t>& attr_set, Kernel kern, int smem,
-                 int threads, long long grid, hipStream_t s, Args... args) {
+int launch_tiles_sized(const GemmEnv& env, std::atomic<uint64_t>& attr_set, Kernel kern, int most_smem, int smem,
+                       int threads, long long grid, hipStream_t s, Args... args) {
     // The attribute belongs to the kernel's code object on ONE device: one bit per device, set
     // by whichever thread launches this kernel there first (setting it twice is harmless).
     if (env.device < 0 || env.device >= 64) return MOE_ERR_INVALID_ARG;
     const uint64_t bit = 1ull << env.device;
     if (!(attr_set.load(std::memory_order_acquire) & bit)) {
         if (hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, smem) != hipSuccess)
+                                hipFuncAttributeMaxDynamicSharedMemorySize, most_smem) != hipSuccess)
             return MOE_ERR_HIP;
         attr_set.fetch_or(bit, std::memory_order_release);
     }
@@ -31,6 +32,11 @@ int launch_tiles(const GemmEnv& env, std::atomic<uint64_t>& attr_set, Kernel ker
     if (grid > 0x7fffffffLL) return MOE_ERR_UNSUPPORTED_SHAPE;
     hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid)), dim3(threads), smem, s, args...);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+template <class Kernel, class... Args>
+int launch_tiles(const GemmEnv& env, std::atomic<uint64_t>& attr_set, Kernel kern, int smem,
+                 int threads, long long grid, hipStream_t s, Args... args) {
+    return launch_tiles_sized(env, attr_set, kern, smem, smem, threads, grid, s, args...);
 }
 
 // Most row tiles that R rows in E groups can make: a group of m > 0 rows has ceil(m / BM) of them, so
