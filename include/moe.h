@@ -348,7 +348,7 @@ enum { MOE_OUT_BF16 = 0, MOE_OUT_FP32 = 1 };
  * the sum exact (int32), rounded to fp32, multiplied by x_scale[p], then by w_scale[e,n] in fp32, and
  * rounded to out's type. offsets [E+1] int32 (device), or NULL with E == 1: all R rows are one group
  * (one matrix for all tokens). x [R,K]; x_scale [R]; W [E,N,K]; w_scale [E,N]; out [R,N] of out_type.
- * x, W and out start at multiples of 16 bytes (not checked). R <= T_max * k of the context, whose
+ * x, W and out start at multiples of 16 bytes (else MOE_ERR_INVALID_ARG). R <= T_max * k of the context, whose
  * d_model, d_ff and E play no part here. E <= 256; K a multiple of 128 up to 130944 (the sums
  * fit 32 bits); N a multiple of 16, 32 <= N <= 2^23; else MOE_ERR_UNSUPPORTED_SHAPE. */
 int moe_gemm_i8(moe_ctx* ctx, const moe_i8* x, const float* x_scale, const int32_t* offsets,
@@ -362,7 +362,7 @@ int moe_gemm_i8(moe_ctx* ctx, const moe_i8* x, const float* x_scale, const int32
  *   y_perm[p,:] = bf16 product of q, s with W2.
  * x_perm [R,d_model]; x_scale [R]; W1, W3 [E,d_ff,d_model], their scales [E,d_ff]; W2
  * [E,d_model,d_ff], w2_scale [E,d_model]; y_perm [R,d_model] bf16 out; R <= T_max * k; x_perm, the
- * weights and y_perm start at multiples of 16 bytes (not checked). d_ff <= 65536. The first call allocates
+ * weights and y_perm start at multiples of 16 bytes (else MOE_ERR_INVALID_ARG). d_ff <= 65536. The first call allocates
  * T_max * k * (d_ff + 8) bytes, kept until moe_destroy (MOE_ERR_WORKSPACE if that fails): make one
  * before recording such calls into a HIP graph. */
 int moe_expert_ffn_i8(moe_ctx* ctx, const moe_i8* x_perm, const float* x_scale,
@@ -372,7 +372,8 @@ int moe_expert_ffn_i8(moe_ctx* ctx, const moe_i8* x_perm, const float* x_scale,
 
 /* moe_layer_forward with its experts in 8 bits: the router reads the tokens x [T,d_model] in bf16, the experts the
  * same tokens in 8 bits, x_i8 [T,d_model] and x_scale [T] (both are outputs of moe_rmsnorm_i8); route ->
- * permute -> gather -> expert FFN as in moe_expert_ffn_i8 -> combine. Weights, scales, limits and the
+ * permute -> gather -> expert FFN as in moe_expert_ffn_i8 -> combine. Weights, scales, limits, addresses
+ * (x_i8 as x_perm there) and the
  * memory of the first call as there; moe_set_expert_output_fp32 and moe_last_routing as for moe_layer_forward. */
 int moe_layer_forward_i8(moe_ctx* ctx, const moe_bf16* x, const moe_i8* x_i8, const float* x_scale,
                          const float* w_router, const float* bias, const moe_i8* W1,

@@ -202,10 +202,18 @@ int ensure_i8(moe_ctx* c) {
     return MOE_OK;
 }
 
+// Operands that are loaded, and outputs that are stored, 16 bytes at a time: rows are multiples of that long, so their first
+// one decides. Views of a buffer of bytes start anywhere.
+template <class... Ptr>
+bool at_16_bytes(Ptr... p) {
+    return ((reinterpret_cast<uintptr_t>(p) | ...) & 15) == 0;
+}
+
 struct ExpertsI8 {
     const moe_i8 *w1, *w3, *w2;
     const float *s1, *s3, *s2;
     bool complete() const { return w1 && w3 && w2 && s1 && s3 && s2; }
+    bool aligned() const { return at_16_bytes(w1, w3, w2); }
 };
 
 // Expert FFN over grouped rows in 8 bits; the down projection's stage holds H's conversion too, in a
@@ -708,7 +716,7 @@ int moe_gemm_i8(moe_ctx* c, const moe_i8* x, const float* x_scale, const int32_t
     if (out_type != MOE_OUT_BF16 && out_type != MOE_OUT_FP32) return MOE_ERR_INVALID_ARG;
     if (E > kMaxExperts || N % 16 != 0 || N < 32 || N > kMaxDimI8 || K % 128 != 0 || K > kMaxSumI8) return MOE_ERR_UNSUPPORTED_SHAPE;
     if (R == 0) return MOE_OK;
-    if (!x || !x_scale || !W || !w_scale || !out) return MOE_ERR_INVALID_ARG;
+    if (!x || !x_scale || !W || !w_scale || !out || !at_16_bytes(x, W, out)) return MOE_ERR_INVALID_ARG;
     return launch_product_i8(c->gemm, x, x_scale, offsets, R, N, K, E, W, w_scale, out, out_type == MOE_OUT_FP32,
                              static_cast<hipStream_t>(stream));
 }
@@ -724,6 +732,7 @@ int moe_expert_ffn_i8(moe_ctx* c, const moe_i8* x_perm, const float* x_scale, co
     if (R == 0) return MOE_OK;
     const ExpertsI8 w{W1, W3, W2, w1_scale, w3_scale, w2_scale};
     if (!x_perm || !x_scale || !offsets || !w.complete() || !y_perm) return MOE_ERR_INVALID_ARG;
+    if (!at_16_bytes(x_perm, y_perm) || !w.aligned()) return MOE_ERR_INVALID_ARG;
     const int rc = ensure_i8(c);
     if (rc != MOE_OK) return rc;
     if (c->prof_armed) ++c->prof_calls;
@@ -740,6 +749,7 @@ int moe_layer_forward_i8(moe_ctx* c, const moe_bf16* x, const moe_i8* x_i8, cons
     if (T == 0) return MOE_OK;
     const ExpertsI8 w{W1, W3, W2, w1_scale, w3_scale, w2_scale};
     if (!x || !x_i8 || !x_scale || !w_router || !w.complete() || !y) return MOE_ERR_INVALID_ARG;
+    if (!at_16_bytes(x_i8) || !w.aligned()) return MOE_ERR_INVALID_ARG;
     int rc = ensure_i8(c);
     if (rc != MOE_OK) return rc;
     if (c->prof_armed) ++c->prof_calls;

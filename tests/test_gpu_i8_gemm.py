@@ -447,6 +447,50 @@ def test_refusals():
     ctx.close()
 
 
+def later(t, elements):
+    """The same values in a buffer that starts `elements` further on."""
+    held = torch.empty(t.numel() + elements, dtype=t.dtype, device="cuda")
+    view = held[elements:].view(t.shape)
+    view.copy_(t)
+    return view
+
+
+def test_operands_that_start_between_16_bytes_are_refused():
+    ctx = B.MoeContext(8, 512, 128, 2, 1)
+    g = gen(0)
+    x, xs, w, ws = whole(g, 8, 256), positive(g, 8), whole(g, 64, 256), positive(g, 64)
+    for dtype in (torch.bfloat16, torch.float32):
+        out = torch.full((8, 64), 7.0, dtype=dtype, device="cuda")
+        size = out.element_size()
+        for bad in (dict(x=later(x, 1)), dict(x=later(x, 8)), dict(w=later(w, 4)), dict(out=later(out, 8 // size)),
+                    dict(out=later(out, 4 // size))):
+            a = dict(x=x, w=w, out=out) | bad
+            with pytest.raises(B.MoeError):
+                B.moe_gemm_i8(ctx, a["x"], xs, None, 8, 1, 64, 256, a["w"], ws, a["out"])
+            assert (a["out"] == 7).all()
+        # at 16 bytes, and scales from any element on
+        want = torch.empty_like(out)
+        B.moe_gemm_i8(ctx, x, xs, None, 8, 1, 64, 256, w, ws, want)
+        got = later(out, 16 // size)
+        B.moe_gemm_i8(ctx, later(x, 16), later(xs, 1), None, 8, 1, 64, 256, later(w, 48), later(ws, 3), got)
+        assert torch.equal(got, want)
+
+    a = dict(x=whole(g, 8, 512), w1=whole(g, 2, 128, 512), w3=whole(g, 2, 128, 512), w2=whole(g, 2, 512, 128),
+             y=torch.full((8, 512), 7.0, dtype=torch.bfloat16, device="cuda"))
+    s1, s3, s2, offsets = positive(g, 2, 128), positive(g, 2, 128), positive(g, 2, 512), groups([5, 3])
+    bf, router = torch.zeros((8, 512), dtype=torch.bfloat16, device="cuda"), torch.zeros((512, 2), device="cuda")
+    for name in a:
+        b = a | {name: later(a[name], 4)}
+        with pytest.raises(B.MoeError):
+            B.moe_expert_ffn_i8(ctx, b["x"], xs, offsets, 8, b["w1"], s1, b["w3"], s3, b["w2"], s2, b["y"])
+        assert (b["y"] == 7).all()
+        if name != "y":
+            with pytest.raises(B.MoeError):
+                B.moe_layer_forward_i8(ctx, bf, b["x"], xs, router, None, b["w1"], s1, b["w3"], s3, b["w2"], s2, 8, b["y"])
+            assert (b["y"] == 7).all()
+    ctx.close()
+
+
 # ------------------------------------------------------------------------------- the layer
 
 @pytest.mark.parametrize("fp32", [False, True])
