@@ -544,6 +544,27 @@ int priced(const Call& c) {
     return grouped<Out<F32, PlainSmall>>(c);
 }
 
+// Long reductions whose weights stream past groups of few rows: a tile with rows to spare takes the time of one that just
+// holds the mean, and a group that outgrows its tile costs a second tile's stream, often a second round. Where one round of 96-
+// and 128-row tiles leaves few compute units idle, those, from 10240 elements on; small -> so, us, groups alike | as skewed as
+// rank^-0.5: 8 experts of 4096 x 14336, 20 rows each 73 -> 70 | 98 -> 71, 36 78 -> 76 | 115 -> 78, 52 114 -> 77 | 108 -> 82, 62 79 ->
+// 81 | 126 -> 139, 72 81 -> 84 | 130 -> 87, of 6144 x 16384 20 126 -> 129 | 150 -> 130, 38 129 -> 135 | 170 -> 135, 54 149 -> 134 | 170
+// -> 137, of 5120 x 10240 22 82 -> 84 | 98 -> 79, 38 84 -> 80 | 97 -> 85, 54 96 -> 83 | 115 -> 88. With 8192 elements small tiles stay
+// (8 of 8192 x 8192, 38 rows 92, 128-row tiles 115 | 113, 115). 64- instead of 32-row tiles from 4096 elements on: 18 rows, 4096 x
+// 14336 as above, 16 of 4096 x 4096 46 -> 46 | 51 -> 48, 8 of 2048 x 8192 27 -> 27 | 33 -> 27; below that 32-row ones are the faster
+// (60 of 1536 x 1536, 14 rows 26.0, 28.2 | 25.5, 29.9). 128- instead of 96-row ones there too: 72 rows, 8 of 8192 x 8192 118 -> 118 |
+// 152 -> 118, 16 of 4096 x 4096 65 -> 65 | 81 -> 83; 64 of 2048 x 1408 43, 45 | 51, 55.
+int tiles_of_uneven_groups(const Call& c, int config, int mid_n_tiles) {
+    const double avg = static_cast<double>(c.R) / c.E;
+    if (config < 2 || avg < 16.0) return config;
+    const int cus = compute_units(c.env.device);
+    const double mid = static_cast<double>(c.E) * mid_n_tiles;
+    if (c.K >= 5120 && mid >= 0.6 * cus && mid <= cus) return avg <= 32.0 ? 4 : 1;
+    if (c.K < 2048) return config;
+    if (config == 3 && static_cast<double>(c.E) * (c.N / 64) >= cus) return 2;
+    return config == 4 ? 1 : config;
+}
+
 template <bool F32>
 int product(const Call& c) {
     if (few_rows_fits(c)) return few_rows<false, F32>(c);
@@ -556,6 +577,7 @@ int product(const Call& c) {
     if (config == 0 && (!large_takes(d, c.K) || d < 256)) config = 1;
     if ((config == 1 || config == 4) && d < 128) config = 2;
     if (config == 2 && d < 64) config = 3;
+    if (c.env.forced_config < 0) config = tiles_of_uneven_groups(c, config, wide_mid ? d / 256 : d / 128);
     // Reductions of up to 1024 elements over many tiles: the pipelined 64 x 128 tile, two on a compute unit. Grouped forms -> so,
     // through 8 of 128 experts of 2048 x 768: 120 tokens 113 -> 111 us, 300 122 -> 115, 600 132 -> 122, 1000 140 -> 131 (all with
     // gate/up); 1408 elements, 600 tokens through 6 of 64 119 -> 122.

@@ -159,6 +159,14 @@ def test_few_rows_and_few_tiles(counts, d, f):
     gemm_case(counts, f, d, torch.float32, seed=d)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("counts,N,K", [
+    ([40, 9, 0, 31], 4096, 10368), ([97, 20, 3, 60], 8192, 10240), ([130, 1, 64, 65], 4112, 11264), ([33, 0, 15, 16], 4096, 4096),
+    ([20, 2, 31, 40], 4112, 4224), ([129, 70, 0, 96], 2048, 8192)])
+def test_long_reductions_of_uneven_groups(counts, N, K, dtype):
+    gemm_case(counts, N, K, dtype, seed=N + K)
+
+
 def test_sums_at_the_ends_of_the_range():
     """The longest reduction, all products alike: sums of 2^31 - 2^21 and -2^31 + 2^24 or so, exactly."""
     K, N = 130944, 32
