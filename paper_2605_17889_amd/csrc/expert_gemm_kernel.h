@@ -861,7 +861,7 @@ struct LoadPlan {
 // Workgroups that start together stay at the same k, where weight rows whose pitch is a multiple of 4 KB fall on
 // few memory channels. In long reductions the first workgroup of every compute unit starts later by its place in its
 // XCD: they then stream different k, and what a late start costs is less than what the channels gain; the
-// order of the sums is the same. `spread` is the step in units of 768 cycles (spread_steps in expert_gemm.hip).
+// order of the sums is the same. `spread` is the step in units of 768 cycles (spread_steps in expert_gemm_launch.h).
 constexpr int kSpreadSlots = 32;     // compute units of an XCD
 __device__ __forceinline__ void spread_start(int spread) {
     const int slot = blockIdx.x / kXcds;
@@ -869,29 +869,43 @@ __device__ __forceinline__ void spread_start(int spread) {
     for (int i = slot * spread; i > 0; --i) __builtin_amdgcn_s_sleep(12);
 }
 
+// Sums of whole numbers may start anywhere: the k-steps of an n-tile in turn from one that its number draws, so that
+// workgroups that start together stream different k at no cost. Those that share an n-tile's weights still share its order.
+// (Which products do: turned_ksteps in expert_gemm_launch.h.)
+template <class Cfg>
+__device__ __forceinline__ int first_kstep(const TileCoord& tc, int N, int KT, bool turned) {
+    if (!operands_i8<Cfg>::value || !turned) return 0;
+    const uint32_t tile = static_cast<uint32_t>(tc.expert) * n_tiles<Cfg>(N) + tc.nt;
+    return static_cast<int>(__umulhi(tile * 0x9e3779b9u, static_cast<uint32_t>(KT)));
+}
+
 // One tile: `init_a` sets the A addresses of the load plan, after the first weights have gone out.
 template <class Cfg, class InitA>
 __device__ __forceinline__ void ring_of_stages(const TileCoord& tc, LoadPlan<Cfg>& lp, InitA&& init_a, unsigned char* smem,
                                                int wave, int lane, const uint16_t* __restrict__ B0,
                                                const uint16_t* __restrict__ B1, uint16_t* __restrict__ C, int N,
-                                               int K, const ScalesOf<Cfg>& scales) {
+                                               int K, bool turned, const ScalesOf<Cfg>& scales) {
     constexpr bool I8 = operands_i8<Cfg>::value;
     constexpr int BK = Cfg::BK, TM = Cfg::TM, TN = Cfg::TN, LPW = Cfg::LPW, NSTAGE = Cfg::NSTAGE;
     static_assert(Cfg::KSUB == 2, "two k-substeps a stage");
     const int wm = wave / Cfg::WN, wn = wave % Cfg::WN;
     // ---- first loads: the first weights go out under the latency of the row index (layer call of 64 tokens through
     // 8 experts of 512 x 1024 20.5 us, with two stages of weights 21.0; one token through 8 of 128 of 2048 x 768 29.2, 29.4)
-    const int KT = K / BK;
+    const int KT = K / BK, first = first_kstep<Cfg>(tc, N, KT, turned);
+    auto offset = [&](int s) {                       // of the k-step that is number s here
+        const int t = first + s;
+        return static_cast<size_t>(I8 && t >= KT ? t - KT : t) * BK;
+    };
     lp.init_fixed(wave, lane, K);
     lp.init_b(tc, wave, B0, B1, N, K);
     // ahead of the others: loads complete in order, and these are counted with none of the stages that are waited for
     const KeptScales<Cfg> sc = load_scales<Cfg>(scales, tc, wm, wn, lane, N);
-    lp.issue_b_all(0, 0);
+    lp.issue_b_all(0, offset(0));
     init_a();
-    lp.issue_a_all(0, 0);
+    lp.issue_a_all(0, offset(0));
 #pragma unroll
     for (int s = 1; s < NSTAGE - 1; ++s)
-        if (s < KT) lp.issue_all(s * Cfg::STAGE_BYTES, static_cast<size_t>(s) * BK);
+        if (s < KT) lp.issue_all(s * Cfg::STAGE_BYTES, offset(s));
 
     f32x4 acc[TM][TN];
 #pragma unroll
@@ -912,7 +926,7 @@ __device__ __forceinline__ void ring_of_stages(const TileCoord& tc, LoadPlan<Cfg
         const int nk = kt + NSTAGE - 1;
         const unsigned char* st = smem + stage * Cfg::STAGE_BYTES;
         const uint32_t into = (stage == 0 ? NSTAGE - 1 : stage - 1) * Cfg::STAGE_BYTES;
-        const size_t koff = static_cast<size_t>(nk) * BK;
+        const size_t koff = offset(nk);
         // Fragments of the first k-substep are asked for ahead of the loads, which leave a wavefront some 100 cycles
         // apart, those of the second ahead of the first one's MFMAs (layer calls with the loads first -> so: one token
         // through 8 experts of 512 x 1024 20.0 -> 19.6 us, 5 through 6 of 64 of 2048 x 1408 93.9 -> 92.3, 37 through 8 of 128
@@ -949,12 +963,12 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_kernel(
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const TileCoord tc = tile_of_workgroup<Cfg>(offsets, scales, E, N, 0, Cut::kNever);
     if (tc.expert < 0) return;
-    spread_start(spread);
+    if (spread > 0) spread_start(spread);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     LoadPlan<Cfg> lp;
     ring_of_stages<Cfg>(tc, lp, [&] { lp.init_a(tc, wave, lane, A, row_index, index_div, K); }, smem, wave, lane, B0, B1,
-                        C, N, K, scales);
+                        C, N, K, spread < 0, scales);
 }
 
 // ---- kernel 1, few tokens: tiles straight from the selected experts ---------------------------
@@ -1047,20 +1061,21 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_routed_kernel(
             const int id = list[row];
             return index_div.mul == 0 ? id : static_cast<int>(__umulhi(static_cast<uint32_t>(id), index_div.mul) >> index_div.shift);
         });
-    }, smem, wave, lane, B0, B1, C, N, K, NoScales{});
+    }, smem, wave, lane, B0, B1, C, N, K, false, NoScales{});
 }
 
 // ---- kernel 1, pipelined: what ring_of_stages does, with every load behind a matrix instruction of its own -------------
 // A k-step is two halves of one MFMA k-substep each. While the MFMAs of a half issue, the fragments of the next half are read
 // and one direct-to-LDS load goes out behind every few of them; the barrier sits between the halves, where the fragments of
 // the second one are in registers, so that behind it the k-step's stage may be filled again and the next one be read. The B
-// loads of k-step kt + NSTAGE - 1 go out in the first half of k-step kt, the A loads of kt + NSTAGE in its second.
+// loads of k-step kt + NSTAGE - 1 go out in the first half of k-step kt, the A loads of kt + NSTAGE in its second, from
+// elements b_from and a_from of a row.
 // DIST: k-steps from this one to the last, or NSTAGE where there are at least as many. One loop and straight code behind
 // it: the accumulators are operands of inline assembly (mma16_agpr), which no join of paths may make the compiler move.
 template <class Cfg, int DIST>
 __device__ __forceinline__ void pipelined_kstep(f32x4 (&acc)[Cfg::TM][Cfg::TN], bf16x8 (&fa)[2][Cfg::TM],
                                                 bf16x8 (&fb)[2][Cfg::TN], const LoadPlan<Cfg>& lp, const FragPlan<Cfg>& fp,
-                                                unsigned char* smem, int stage, int kt) {
+                                                unsigned char* smem, int stage, size_t b_from, size_t a_from) {
     constexpr int TM = Cfg::TM, TN = Cfg::TN, NM = TM * TN, NR = TM + TN, S = Cfg::NSTAGE;
     constexpr int LA = LoadPlan<Cfg>::LA, LB = LoadPlan<Cfg>::LB;
     constexpr bool I8 = operands_i8<Cfg>::value;
@@ -1081,7 +1096,7 @@ __device__ __forceinline__ void pipelined_kstep(f32x4 (&acc)[Cfg::TM][Cfg::TN], 
         if constexpr (DIST >= S - 1) {
 #pragma unroll
             for (int n = 0; n < LB; ++n)
-                if (n * NM / LB == m) lp.issue_one(LA + n, previous * Cfg::STAGE_BYTES, static_cast<size_t>(kt + S - 1) * Cfg::BK);
+                if (n * NM / LB == m) lp.issue_one(LA + n, previous * Cfg::STAGE_BYTES, b_from);
         }
         MOE_FENCE();
     }
@@ -1101,7 +1116,7 @@ __device__ __forceinline__ void pipelined_kstep(f32x4 (&acc)[Cfg::TM][Cfg::TN], 
         if constexpr (DIST >= S) {
 #pragma unroll
             for (int n = 0; n < LA; ++n)
-                if (n * NM / LA == m) lp.issue_one(n, stage * Cfg::STAGE_BYTES, static_cast<size_t>(kt + S) * Cfg::BK);
+                if (n * NM / LA == m) lp.issue_one(n, stage * Cfg::STAGE_BYTES, a_from);
         }
         MOE_FENCE();
     }
@@ -1111,7 +1126,7 @@ template <class Cfg>
 __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_pipelined_kernel(
     const uint16_t* __restrict__ A, const uint16_t* __restrict__ B0, const uint16_t* __restrict__ B1,
     uint16_t* __restrict__ C, const int32_t* __restrict__ offsets, RowDiv index_div, int E, int N, int K,
-    ScalesOf<Cfg> scales) {
+    bool turned, ScalesOf<Cfg> scales) {
     constexpr int TM = Cfg::TM, TN = Cfg::TN, S = Cfg::NSTAGE, LA = LoadPlan<Cfg>::LA;
     static_assert(Cfg::KSUB == 2 && (S - 1) * Cfg::LPW + LA < 64, "two k-substeps a stage; loads in flight");
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -1138,9 +1153,14 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_pipelined_kernel(
     lp.init_fixed(wave, lane, K);
     lp.init(tc, wave, lane, A, B0, B1, nullptr, index_div, N, K);
     const KeptScales<Cfg> sc = load_scales<Cfg>(scales, tc, wm, wn, lane, N);
+    const int turn = first_kstep<Cfg>(tc, N, KT, turned);
+    auto offset = [&](int s) {                       // of the k-step that is number s here
+        const int t = turn + s;
+        return static_cast<size_t>(t >= KT ? t - KT : t) * Cfg::BK;
+    };
 #pragma unroll
-    for (int s = 0; s < S - 1; ++s) lp.issue_all(s * Cfg::STAGE_BYTES, static_cast<size_t>(s) * Cfg::BK);
-    lp.issue_a_all((S - 1) * Cfg::STAGE_BYTES, static_cast<size_t>(S - 1) * Cfg::BK);
+    for (int s = 0; s < S - 1; ++s) lp.issue_all(s * Cfg::STAGE_BYTES, offset(s));
+    lp.issue_a_all((S - 1) * Cfg::STAGE_BYTES, offset(S - 1));
     FragPlan<Cfg> fp;
     fp.init(lane, wm, wn);
     f32x4 acc[TM][TN];
@@ -1155,11 +1175,11 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void grouped_gemm_pipelined_kernel(
     MOE_FENCE();
     int stage = 0, kt = 0;
     for (; kt + S < KT; ++kt) {
-        pipelined_kstep<Cfg, S>(acc, fa, fb, lp, fp, smem, stage, kt);
+        pipelined_kstep<Cfg, S>(acc, fa, fb, lp, fp, smem, stage, offset(kt + S - 1), offset(kt + S));
         stage = stage + 1 == S ? 0 : stage + 1;
     }
     static_for<S>([&](auto tag) {                    // the last S k-steps
-        pipelined_kstep<Cfg, S - 1 - decltype(tag)::value>(acc, fa, fb, lp, fp, smem, stage, kt);
+        pipelined_kstep<Cfg, S - 1 - decltype(tag)::value>(acc, fa, fb, lp, fp, smem, stage, offset(kt + S - 1), 0);
         stage = stage + 1 == S ? 0 : stage + 1;
         ++kt;
     });

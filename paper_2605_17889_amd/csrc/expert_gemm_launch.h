@@ -66,6 +66,27 @@ int spread_steps(int R, int E, int N, int K, bool dual) {
     return K < 6144 || bytes < 0.8e9 ? 0 : K % 16384 == 0 ? 2 : 1;
 }
 
+// Whether the n-tiles of a product of whole numbers start at k-steps of their own (gemm::first_kstep) instead of together or
+// late: at pitches of whole 4 KB, where weight rows fall on few memory channels. Expert FFN and its down projection alone,
+// together -> so, us: 12 rows for each of 8 experts of 8192 x 8192 271 and 92 -> 257 and 85, 64 317 and 116 -> 260 and 84, 4 of
+// 16 of 4096 x 4096 151 and 49 -> 133 and 44, 64 190 and 67 -> 148 and 48, 24 of 8 of 6144 x 16384 (late before) 397 and 127 -> 389
+// and 120; one matrix of 8192 x 8192, 37 rows 20.3 -> 17.8. 96- and 128-row tiles at all longer pitches: 90 rows, 8 of 4096 x 14336,
+// down turned too 290 -> 275, 16 of 6144 x 6144 367 -> 347, 8 of 5120 x 10240 290 -> 280. Lower ones lose at others (down at 14336
+// bytes 70 -> 72; gate/up at 7168 67 -> 69.5), and those of 16 rows at all (8192 x 2048, one row 19.6 -> 22). At 2 KB gate/up of
+// many n-tiles gains (8 of 2048 x 8192, 12 rows 56 -> 50), of few not (64 of 2048 x 1408, 24 rows 69 -> 72), nor does down
+// (7168 x 2048 22 -> 23). Pipelined tiles turn for one row tile: several share an n-tile's weights, but each n-tile then asks for
+// rows of its own (14336 x 4096, 1003 rows 68 -> 75, 8192 x 8192, 512 40 -> 44; 2048 x 32000, 37 rows 17 -> 15).
+template <class Cfg>
+bool turned_ksteps(int N, int K) {
+    if (!gemm::operands_i8<Cfg>::value || Cfg::BM == 16) return false;
+    const int pitch = 2 * K;
+    return pitch % 4096 == 0 || (Cfg::BM >= 96 && pitch > 4096) || (pitch == 2048 && Cfg::DUAL && N >= 32 * Cfg::BN_OUT);
+}
+template <class Cfg>
+bool turned_ksteps_of_one(int R, int E, int K) {
+    return E == 1 && R <= Cfg::BM && (2 * K % 4096 == 0 || 2 * K == 2048);
+}
+
 // Whether tiles of Cfg::BN_OUT columns cover N of them (gemm::n_tiles).
 template <class Cfg>
 bool columns_fit(int N) {
@@ -82,7 +103,8 @@ int launch_grouped(const GemmEnv& env, const moe_bf16* A, const moe_bf16* B0, co
     const long long max_mt = most_row_tiles(R, E, Cfg::BM);
     return launch_tiles(env, attr_set, gemm::grouped_gemm_kernel<Cfg>, Cfg::SMEM, Cfg::NTHREADS,
                         max_mt * gemm::n_tiles<Cfg>(N), s, A, B0, B1, C, offsets, row_index,
-                        gemm::RowDiv(index_div), E, N, K, spread_steps(R, E, N, K, Cfg::DUAL), scales);
+                        gemm::RowDiv(index_div), E, N, K,
+                        turned_ksteps<Cfg>(N, K) ? -1 : spread_steps(R, E, N, K, Cfg::DUAL), scales);
 }
 
 // The pipelined form of the generic kernel.
@@ -95,7 +117,8 @@ int launch_pipelined(const GemmEnv& env, const moe_bf16* A, const moe_bf16* B0, 
     if (!columns_fit<Cfg>(N) || K % Cfg::BK != 0 || K / Cfg::BK / splits < Cfg::NSTAGE) return MOE_ERR_UNSUPPORTED_SHAPE;
     static std::atomic<uint64_t> attr_set{0};
     return launch_tiles(env, attr_set, gemm::grouped_gemm_pipelined_kernel<Cfg>, Cfg::SMEM, Cfg::NTHREADS,
-                        most_row_tiles(R, E, Cfg::BM) * gemm::n_tiles<Cfg>(N) * splits, s, A, B0, B1, C, offsets, gemm::RowDiv(1), E, N, K, scales);
+                        most_row_tiles(R, E, Cfg::BM) * gemm::n_tiles<Cfg>(N) * splits, s, A, B0, B1, C, offsets, gemm::RowDiv(1), E, N, K,
+                        turned_ksteps_of_one<Cfg>(R, E, K), scales);
 }
 
 // Slots of all tiles that R rows in E groups can make: the tiles, and where the last round is split two slots
