@@ -545,22 +545,23 @@ int priced(const Call& c) {
 }
 
 // Long reductions whose weights stream past groups of few rows: a tile with rows to spare takes the time of one that just
-// holds the mean, and a group that outgrows its tile costs a second tile's stream, often a second round. Where one round of 96-
-// and 128-row tiles leaves few compute units idle, those, from 10240 elements on; small -> so, us, groups alike | as skewed as
-// rank^-0.5: 8 experts of 4096 x 14336, 20 rows each 73 -> 70 | 98 -> 71, 36 78 -> 76 | 115 -> 78, 52 114 -> 77 | 108 -> 82, 62 79 ->
-// 81 | 126 -> 139, 72 81 -> 84 | 130 -> 87, of 6144 x 16384 20 126 -> 129 | 150 -> 130, 38 129 -> 135 | 170 -> 135, 54 149 -> 134 | 170
-// -> 137, of 5120 x 10240 22 82 -> 84 | 98 -> 79, 38 84 -> 80 | 97 -> 85, 54 96 -> 83 | 115 -> 88. With 8192 elements small tiles stay
-// (8 of 8192 x 8192, 38 rows 92, 128-row tiles 115 | 113, 115). 64- instead of 32-row tiles from 4096 elements on: 18 rows, 4096 x
-// 14336 as above, 16 of 4096 x 4096 46 -> 46 | 51 -> 48, 8 of 2048 x 8192 27 -> 27 | 33 -> 27; below that 32-row ones are the faster
-// (60 of 1536 x 1536, 14 rows 26.0, 28.2 | 25.5, 29.9). 128- instead of 96-row ones there too: 72 rows, 8 of 8192 x 8192 118 -> 118 |
-// 152 -> 118, 16 of 4096 x 4096 65 -> 65 | 81 -> 83; 64 of 2048 x 1408 43, 45 | 51, 55.
+// holds the mean, and a group that outgrows its tile costs a second tile's stream, often a second round. From 4096 elements on:
+// 96- and 128-row tiles where their rounds (one, or two full ones) leave few compute units idle; 32- or 64-row tiles -> so, us,
+// groups alike | as skewed as rank^-0.5: 8 experts of 4096 x 14336, 20 rows each 72 -> 76 | 99 -> 73, 38 77 -> 77 | 116 -> 77, 52 114
+// -> 78 | 108 -> 84, of 6144 x 16384 20 127 -> 122 | 151 -> 124, 52 166 -> 127 | 163 -> 131, of 5120 x 10240 38 84 -> 80 | 95 -> 84, of
+// 8192 x 8192 20 88 -> 85 | 98 -> 82, 52 110 -> 82 | 111 -> 86, 16 of 4096 x 4096 20 45 -> 45 | 49 -> 45, 52 58 -> 44 | 58 -> 48, of
+// 2048 x 4096 20 24 -> 25 | 28 -> 25, 52 32 -> 25 | 33 -> 27. With half of them idle small tiles stay (8 of 2048 x 8192, 28 rows 22,
+// 96-row tiles 34), and with a round and a half (16 of 6144 x 6144, 20 rows 96, 114 | 101, 106). Elsewhere 64- instead of 32-row tiles
+// (8 of 2048 x 8192, 18 rows 27 -> 27 | 33 -> 27; below 4096 elements 60 of 1536 x 1536, 14 rows 26.0, 28.2 | 25.5, 29.9) and 128-
+// instead of 96-row ones (72 rows, 16 of 6144 x 6144 119 -> 120 | 120 -> 119, 8 of 8192 x 8192 84 -> 85 | 130 -> 88; below, 64 of 2048 x
+// 1408 43, 45 | 51, 55).
 int tiles_of_uneven_groups(const Call& c, int config, int mid_n_tiles) {
     const double avg = static_cast<double>(c.R) / c.E;
     if (config < 2 || avg < 16.0) return config;
     const int cus = compute_units(c.env.device);
     const double mid = static_cast<double>(c.E) * mid_n_tiles;
-    if (c.K >= 5120 && mid >= 0.6 * cus && mid <= cus) return avg <= 32.0 ? 4 : 1;
     if (c.K < 2048) return config;
+    if (mid >= 0.6 * cus && mid <= 2.0 * cus && (mid <= cus || last_round_use(mid, cus) >= 0.95)) return avg <= 32.0 ? 4 : 1;
     if (config == 3 && static_cast<double>(c.E) * (c.N / 64) >= cus) return 2;
     return config == 4 ? 1 : config;
 }
