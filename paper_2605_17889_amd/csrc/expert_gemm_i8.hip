@@ -421,6 +421,29 @@ bool many_short_tiles(const Call& c) {
     return c.env.forced_config < 0 && c.K <= 1024 && touched(c) * (c.N / 128) >= 2.9 * compute_units(c.env.device);
 }
 
+// Whether the groups mostly fit 128 rows, 1.5 standard deviations above the mean, in reductions from 4096 elements on with tiles for
+// all compute units: a second tile for the largest costs less than 256-row ones for all, of half the height too. 256- -> 128-row tiles, 110 rows each, us, groups alike | as skewed as rank^-0.5: gate/up, 8
+// experts of 4096 x 14336 217 -> 200 | 246 -> 215, 8192 x 8192 225 -> 202 | 249 -> 229, 6144 x 16384 318 -> 313 | 351 -> 342, 5120 x 10240
+// 200 -> 196 | 213 -> 228, 16 of 4096 x 4096 129 -> 113 | 137 -> 125; down at 4096 x 14336 120 -> 96 | 117 -> 152, 8192 x 8192 129 -> 102 |
+// 139 -> 141, 16 of 4096 x 4096 72 -> 55 | 79 -> 79. With fewer tiles two experts of 4096 x 14336 59 -> 74, down at 5120 x 10240 99 ->
+// 107. 130 rows, 4096 x 14336: gate/up 223 -> 245 | 238 -> 234, down 121 -> 157 | 117 -> 148.
+bool most_fit_128_rows(const Call& c, int mid_n_tiles) {
+    const double avg = static_cast<double>(c.R) / c.E;
+    return c.K >= 2048 && static_cast<double>(c.E) * mid_n_tiles >= compute_units(c.env.device) &&
+           avg + 1.5 * std::sqrt(avg) <= 128.0;
+}
+
+// Gate/up reductions from 4096 elements on: 128- instead of 64- and 96-row tiles from 46 rows a group on, us, groups alike | as
+// skewed as rank^-0.5: 46 rows for each of 8 experts of 4096 x 14336 166 -> 171 | 183 -> 176, 6144 x 16384 280 -> 267 | 311 -> 277, 8192 x
+// 8192 173 -> 174 | 200 -> 173, 5120 x 10240 157 -> 164 | 179 -> 169, 16 of 6144 x 6144 211 -> 201 | 230 -> 205; 34 rows 156 -> 167 | 161 ->
+// 170, 264 -> 264 | 273 -> 260, 171 -> 174 | 174 -> 172, 149 -> 159 | 151 -> 161, 198 -> 196 | 220 -> 202; 58 rows, of 96 179 -> 179 | 207
+// -> 184, 283 -> 282 | 331 -> 289, 177 -> 175 | 218 -> 175, 167 -> 172 | 205 -> 178, 210 -> 208 | 237 -> 241.
+bool gateup_of_128_rows(const Call& c, int config) {
+    if (config == 0) return most_fit_128_rows(c, c.N / 128);
+    return (config == 2 || config == 4) && c.K >= 2048 && c.R >= 46.0 * c.E &&
+           static_cast<double>(c.E) * (c.N / 128) >= compute_units(c.env.device);
+}
+
 template <class Cfg>
 int converted(const Call& c) {
     static std::atomic<uint64_t> attr_set[2];
@@ -435,6 +458,7 @@ int gateup(const Call& c) {
     if (few_rows_fits(c)) return few_rows<true, false>(c);
     int config = pick_config(c.env, c.R, c.E, gateup_tiles(c.E, c.K, c.N));
     if (config == 0 && !large_takes(c.N, c.K)) config = 1;
+    if (c.env.forced_config < 0 && gateup_of_128_rows(c, config)) config = 1;
     switch (config) {
         case 0: return large<GateUp1W>(c);
         case 1: return grouped<GateUpMid, GateUpMidS>(c);
@@ -557,7 +581,8 @@ int priced(const Call& c) {
 // 1408 43, 45 | 51, 55).
 int tiles_of_uneven_groups(const Call& c, int config, int mid_n_tiles) {
     const double avg = static_cast<double>(c.R) / c.E;
-    if (config < 2 || avg < 16.0) return config;
+    if (config == 0) return most_fit_128_rows(c, mid_n_tiles) ? 1 : 0;
+    if (config == 1 || avg < 16.0) return config;
     const int cus = compute_units(c.env.device);
     const double mid = static_cast<double>(c.E) * mid_n_tiles;
     if (c.K < 2048) return config;

@@ -266,6 +266,11 @@ def test_experts(counts, d, f):
     ffn_case(counts, d, f, seed=sum(counts))
 
 
+@pytest.mark.parametrize("counts,d,f", [([60, 31, 90, 3], 4096, 8192), ([129, 64, 120, 128], 4096, 8192), ([47] * 4, 8192, 8192)])
+def test_experts_of_uneven_groups(counts, d, f):
+    ffn_case(counts, d, f)
+
+
 def test_experts_with_large_gates():
     """|g| of some tens: SiLU between nothing and g itself."""
     ffn_case([40, 3], 512, 256, seed=9, spread=40.0)
