@@ -183,10 +183,11 @@ __global__ __launch_bounds__(threads_of(TPR)) void rows_i8_kernel(RowArgs a) {
     float r = 1.f;
     if constexpr (NORM) {
         float down = 1.f;
-        // values past 2^63 or so, whose squares leave the range of fp32: again with the row scaled by 2^-64 (the same
-        // decision in all threads of the row; a row that holds an infinity or a NaN stays one that does)
+        // A sum of squares that leaves the range of fp32: again with the row scaled by 2^-96 (the same decision in all threads of
+        // the row; a row that holds an infinity or a NaN stays one that does). Of at most 2^16 values one is then 2^56 or more, its
+        // square 2^-80, and the sum stays below 2^(64 + 16). An eps that falls below the range on that scale is nothing beside it.
         if (!(sum < __builtin_inff())) {
-            down = 0x1p-64f;
+            down = 0x1p-96f;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll

@@ -307,3 +307,24 @@ def test_odd_widths_at_every_alignment(d):
                 assert torch.equal(stream, h) and torch.equal(again, y)
             for f in flat:
                 assert f is None or ((f[:start + 8] == 7).all() and (f[start + 8 + T * d:] == 7).all())
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("largest", [1e37, 3e38])
+@pytest.mark.parametrize("d", [64, 1111, 8192, 65536])
+def test_norm_of_values_up_to_the_largest(d, largest, kind):
+    """Rows whose sum of squares leaves the range of fp32 by up to 2^144: the result is that of 64 bits. Their scaling is by a power
+    of two, so the tolerances are the usual ones."""
+    T, g = 6, gen(d)
+    whole = (torch.rand((T, d), generator=g, device="cuda") * 2 - 1) * largest
+    whole[1] = largest                                   # all alike: the largest sum
+    whole[2] = torch.randn(d, generator=g, device="cuda")
+    whole[2, d - 1] = largest                            # one beside ordinary ones
+    whole[3] = torch.randn(d, generator=g, device="cuda")          # no such value at all
+    _, _, w = make(1, d, None, seed=d)
+    x = (whole if KINDS[kind] is None else whole / 2).bfloat16()
+    res = None if KINDS[kind] is None else (whole / 2).to(KINDS[kind])
+    got = outputs(T, d, KINDS[kind])
+    B.moe_rmsnorm_i8(x, res, w, EPS, *got)
+    assert got[2].abs().amax(1).eq(127).all() and (got[3] > 0).all()
+    check(x, res, w, got)
