@@ -599,3 +599,34 @@ def test_example_block_is_near_its_bf16_form():
         want = block.in_bf16(x[:T], x[:T] * 0.5)
         assert ((logits - want).norm() / want.norm()).item() < 0.05
     block.ctx.close()
+
+
+@pytest.mark.parametrize("rows", [128, 8])
+def test_ties_of_h_go_to_even(rows):
+    """H's rows in 8 bits read back one by one (W2 the identity), half the largest element among them for every mantissa of it, in
+    a launch of their own and, 8 rows at a time, inside the down projection. x picks two channels, 2 W[j,2r] + W[j,2r+1]: gate 32,
+    of which SiLU is 32 up to a rounding, and up b s3[j], b = 128 .. 255, so that H is 32 b s3[j] in bf16."""
+    d, f, E = 512, 512, 8
+    pick = torch.arange(rows, device="cuda")
+    ctx = B.MoeContext(rows, d, f, E, 1)
+    w2 = torch.eye(d, dtype=torch.int8, device="cuda").expand(E, d, d).contiguous()
+    s3 = torch.rand(f, generator=gen(rows), device="cuda") * 2 - 1
+    s3[0], s3[1], s3[f - 1] = 1.0, 0.5, -0.5
+    one = torch.ones((E, f), device="cuda")
+    for first in range(128, 256, rows):
+        b = first + pick
+        x, w1, w3 = (torch.zeros(shape, dtype=torch.int8, device="cuda") for shape in ((rows, d), (E, f, d), (E, f, d)))
+        x[pick, 2 * pick], x[pick, 2 * pick + 1] = 2, 1
+        w1[:, :, 2 * pick] = 16
+        w3[:, :, 2 * pick], w3[:, :, 2 * pick + 1] = (b // 2).to(torch.int8), (b % 2).to(torch.int8)
+        y = torch.empty((rows, d), dtype=torch.bfloat16, device="cuda")
+        B.moe_expert_ffn_i8(ctx, x, torch.ones(rows, device="cuda"), groups([rows // E] * E), rows, w1, one, w3,
+                            s3.expand(E, f).contiguous(), w2, one, y)
+        exact = 32 * b[:, None].double() * s3[None].double()
+        lo, h, hi = ((exact * (1 + off)).bfloat16().double() for off in (-2.0 ** -20, 0, 2.0 ** -20))
+        peak = h.abs().amax(1, keepdim=True)
+        want = (h * 127 / peak).round()
+        assert (want[:, 1] == 64).all() and (want[:, f - 1] == -64).all()
+        q = y.double() * 127 / peak                  # off by y's rounding, 2^-8 of up to 127: less than half a step
+        assert ((q - want).abs() <= 0.51)[lo == hi].all() and (lo == hi).double().mean() > 0.99
+    ctx.close()

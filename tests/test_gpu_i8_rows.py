@@ -328,3 +328,30 @@ def test_norm_of_values_up_to_the_largest(d, largest, kind):
     B.moe_rmsnorm_i8(x, res, w, EPS, *got)
     assert got[2].abs().amax(1).eq(127).all() and (got[3] > 0).all()
     check(x, res, w, got)
+
+
+def rows_with_ties(rows, d, seed):
+    """bf16 rows, the largest element's mantissa every one of the 128 in turn, with its halves and other short fractions of it
+    (among which, for bf16 rows, the halves alone are ties unless the mantissa is that of 127)."""
+    g = gen(seed)
+    peak = (1 + torch.arange(rows, device="cuda") % 128 / 128.0) * 2.0 ** (torch.arange(rows, device="cuda") // 128 % 7 * 30 - 90)
+    part = torch.rand((rows, d), generator=g, device="cuda") * 2 - 1
+    part[:, ::3] = torch.randint(-256, 257, (rows, (d + 2) // 3), generator=g, device="cuda") / 256.0
+    part[:, 1], part[:, d // 2], part[:, d - 1] = 0.5, -0.5, 1.0
+    return (part * peak[:, None]).bfloat16()
+
+
+def test_ties_go_to_even_in_every_row():
+    """q is what 64 bits give, bit for bit: a product of 127 and a bf16 number is exact there, and a quotient of such numbers that
+    is no tie differs from one by 1 / (2 * 255 * 127) of itself or more, far more than any rounding."""
+    for d in (64, 1111, 4096):
+        x = rows_with_ties(7 * 128, d, seed=d)
+        _, y, q, scale = outputs(7 * 128, d, None)
+        want = (x.double() * 127 / x.double().abs().amax(1, keepdim=True)).round()
+        assert (want[:, 1] == 64).all() and (want[:, d // 2] == -64).all()
+        B.moe_quantize_i8(x, q, scale)
+        assert torch.equal(q.double(), want)
+        # the norm, weights of one: u is the row itself
+        q.fill_(77)
+        B.moe_rmsnorm_i8(x, None, torch.ones(d, dtype=torch.bfloat16, device="cuda"), EPS, y=y, q=q, q_scale=scale)
+        assert torch.equal(q.double(), want)
