@@ -210,7 +210,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void rows_i8_kernel(RowArgs a) {
     }
     if (a.q) {
         const bool fine = peak < 0x7f800000u && top < __builtin_inff();
-        const Factors8 by = factors_8_bits(peak);
+        const Factors8 by = factors_8_bits(top > 0.f ? peak : 0u);     // a row of zeros, also by the product with r
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
             if (count(c) > 0) {

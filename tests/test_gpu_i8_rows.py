@@ -355,3 +355,14 @@ def test_ties_go_to_even_in_every_row():
         q.fill_(77)
         B.moe_rmsnorm_i8(x, None, torch.ones(d, dtype=torch.bfloat16, device="cuda"), EPS, y=y, q=q, q_scale=scale)
         assert torch.equal(q.double(), want)
+
+
+def test_norm_that_falls_below_the_range_is_a_row_of_zeros():
+    """Values so small beside eps that v is zero in fp32: scale 0 and q 0, as for every row of zeros."""
+    x = torch.zeros((4, 200), dtype=torch.bfloat16, device="cuda")
+    x[1], x[2, 7], x[3] = 1e-36, -1e-37, 1.0
+    w = torch.ones(200, dtype=torch.bfloat16, device="cuda")
+    _, y, q, scale = outputs(4, 200, None)
+    B.moe_rmsnorm_i8(x, None, w, 1e30, y=y, q=q, q_scale=scale)
+    assert not scale[:3].any() and not q[:3].any() and not y[:3].any()
+    check(x[3:], None, w, (None, y[3:], q[3:], scale[3:]), 1e30)
