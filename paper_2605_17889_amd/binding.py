@@ -52,7 +52,7 @@ class MoeStreamedEstimate(C.Structure):
 
 
 # Argument types of the 8-bit calls: ctypes then converts plain numbers by itself. Host time of a call, with an object for every
-# argument and for the stream -> so: moe_rmsnorm_i8 11.5 -> 7.3 us, moe_gemm_i8 10.3 -> 6.8, moe_expert_ffn_i8 18.5 -> 13.7.
+# argument and for the stream -> so: moe_rmsnorm_i8 11.5 -> 7.4 us, moe_gemm_i8 10.3 -> 6.5, moe_expert_ffn_i8 18.5 -> 11.7.
 _P, _I, _L, _F = C.c_void_p, C.c_int32, C.c_int64, C.c_float
 _I8_ARGUMENTS = {
     "moe_rmsnorm_i8": (_P, _L, _P, _I, _P, _F, _I, _I, _P, _P, _P, _P, _P),
@@ -314,27 +314,29 @@ def moe_set_expert_output_fp32(ctx: MoeContext, enable: bool):
            "moe_set_expert_output_fp32")
 
 
-def _addr(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, what: str) -> Optional[int]:
-    """Address of a contiguous cuda tensor of that type and shape."""
+def _addr(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, device: int, what: str) -> Optional[int]:
+    """Address of a contiguous tensor of that type and shape on that GPU, the one that the call's kernels run on."""
     if t is None:
         return None
-    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+    if t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous():
         return t.data_ptr()
-    raise MoeError(f"{what}: expected a contiguous cuda tensor of {dtype}, shape {shape}, got {t.dtype} on {t.device}, "
-                   f"shape {tuple(t.shape)}, strides {t.stride()}")
+    raise MoeError(f"{what}: expected a contiguous tensor of {dtype}, shape {shape}, on cuda:{device}, got {t.dtype} on "
+                   f"{t.device}, shape {tuple(t.shape)}, strides {t.stride()}")
 
 
-def _rows_addr(t: torch.Tensor, what: str):
-    """-> (address, row stride) of a 2-D bf16 cuda tensor whose rows are contiguous and do not overlap."""
-    if t.dtype is not torch.bfloat16 or t.dim() != 2 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise MoeError(f"{what}: expected a 2-D cuda tensor of {torch.bfloat16} with contiguous rows, got "
+def _rows_addr(t: torch.Tensor, device: int, what: str):
+    """-> (address, row stride) of a 2-D bf16 tensor on that GPU whose rows are contiguous and do not overlap."""
+    if t.dtype is not torch.bfloat16 or t.dim() != 2 or t.get_device() != device or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise MoeError(f"{what}: expected a 2-D tensor of {torch.bfloat16} with contiguous rows on cuda:{device}, got "
                        f"{t.dtype} on {t.device}, shape={tuple(t.shape)}, strides={t.stride()}")
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-def _stream_addr(stream) -> int:
+def _stream_addr(stream, device: int) -> int:
     if stream is None:      # torch.cuda.current_stream() makes an object for it, 2.7 us
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return torch._C._cuda_getCurrentRawStream(device)
+    if stream.device_index != device:
+        raise MoeError(f"stream: expected one of cuda:{device}, got {stream}")
     return stream.cuda_stream
 
 
@@ -342,57 +344,64 @@ def moe_rmsnorm_i8(x, residual, weight, eps, residual_out=None, y=None, q=None, 
     """x [T,d] bf16 (rows may be strided), residual [T,d] bf16 or fp32 or None, weight [d] bf16 ->
     residual_out = x + residual, y = norm in bf16, q and q_scale = norm in 8 bits; outputs that are None
     are not written."""
-    ptr, stride = _rows_addr(x, "x")
+    device = torch.cuda.current_device()
+    ptr, stride = _rows_addr(x, device, "x")
     shape = T, d = x.shape
     held = residual if residual is not None else residual_out
     kind = torch.bfloat16 if held is None else held.dtype
     if kind is not torch.bfloat16 and kind is not torch.float32:
         raise MoeError(f"residual: expected bfloat16 or float32, got {kind}")
-    _check(lib().moe_rmsnorm_i8(ptr, stride, _addr(residual, kind, shape, "residual"), 1 if kind is torch.float32 else 0,
-                                _addr(weight, torch.bfloat16, (d,), "weight"), eps, T, d,
-                                _addr(residual_out, kind, shape, "residual_out"), _addr(y, torch.bfloat16, shape, "y"),
-                                _addr(q, torch.int8, shape, "q"), _addr(q_scale, torch.float32, (T,), "q_scale"),
-                                _stream_addr(stream)), "moe_rmsnorm_i8")
+    _check(lib().moe_rmsnorm_i8(ptr, stride, _addr(residual, kind, shape, device, "residual"), 1 if kind is torch.float32 else 0,
+                                _addr(weight, torch.bfloat16, (d,), device, "weight"), eps, T, d,
+                                _addr(residual_out, kind, shape, device, "residual_out"),
+                                _addr(y, torch.bfloat16, shape, device, "y"), _addr(q, torch.int8, shape, device, "q"),
+                                _addr(q_scale, torch.float32, (T,), device, "q_scale"),
+                                _stream_addr(stream, device)), "moe_rmsnorm_i8")
 
 
 def moe_quantize_i8(x, q, q_scale, stream=None):
     """x [T,d] bf16 (rows may be strided) -> q [T,d] int8, q_scale [T] fp32. Weights: x = W.view(-1, K)."""
-    ptr, stride = _rows_addr(x, "x")
+    device = torch.cuda.current_device()
+    ptr, stride = _rows_addr(x, device, "x")
     T, d = x.shape
-    _check(lib().moe_quantize_i8(ptr, stride, T, d, _addr(q, torch.int8, (T, d), "q"),
-                                 _addr(q_scale, torch.float32, (T,), "q_scale"), _stream_addr(stream)), "moe_quantize_i8")
+    _check(lib().moe_quantize_i8(ptr, stride, T, d, _addr(q, torch.int8, (T, d), device, "q"),
+                                 _addr(q_scale, torch.float32, (T,), device, "q_scale"), _stream_addr(stream, device)),
+           "moe_quantize_i8")
 
 
-def _matrices(E: int, N: int, K: int, W, scale, what: str):
+def _matrices(E: int, N: int, K: int, device: int, W, scale, what: str):
     """Addresses of matrices [E,N,K] in 8 bits and their scales [E,N]; of one matrix also [N,K] and [N]."""
     one = E == 1 and W is not None and W.dim() == 2
-    return (_addr(W, torch.int8, (N, K) if one else (E, N, K), what),
-            _addr(scale, torch.float32, (N,) if E == 1 and scale is not None and scale.dim() == 1 else (E, N), what + "_scale"))
+    return (_addr(W, torch.int8, (N, K) if one else (E, N, K), device, what),
+            _addr(scale, torch.float32, (N,) if E == 1 and scale is not None and scale.dim() == 1 else (E, N), device,
+                  what + "_scale"))
 
 
 def moe_gemm_i8(ctx: MoeContext, x, x_scale, offsets, R, E, N, K, W, w_scale, out, stream=None):
     """out[p,n] = x_scale[p] * w_scale[e,n] * sum_k x[p,k] W[e,n,k] for the rows p of expert e; offsets None: one
     matrix for all rows. x [R,K] int8, W [E,N,K] int8, scales fp32, out [R,N] bf16 or fp32."""
-    w, ws = _matrices(E, N, K, W, w_scale, "W")
+    device = ctx.device
+    w, ws = _matrices(E, N, K, device, W, w_scale, "W")
     kind = torch.float32 if out is not None and out.dtype is torch.float32 else torch.bfloat16
-    _check(lib().moe_gemm_i8(ctx._h, _addr(x, torch.int8, (R, K), "x"), _addr(x_scale, torch.float32, (R,), "x_scale"),
-                             _addr(offsets, torch.int32, (E + 1,), "offsets"), R, E, N, K, w, ws,
-                             _addr(out, kind, (R, N), "out"), 1 if kind is torch.float32 else 0, _stream_addr(stream)),
-           "moe_gemm_i8")
+    _check(lib().moe_gemm_i8(ctx._h, _addr(x, torch.int8, (R, K), device, "x"),
+                             _addr(x_scale, torch.float32, (R,), device, "x_scale"),
+                             _addr(offsets, torch.int32, (E + 1,), device, "offsets"), R, E, N, K, w, ws,
+                             _addr(out, kind, (R, N), device, "out"), 1 if kind is torch.float32 else 0,
+                             _stream_addr(stream, device)), "moe_gemm_i8")
 
 
 def moe_expert_ffn_i8(ctx: MoeContext, x_perm, x_scale, offsets, R, W1, w1_scale, W3, w3_scale, W2, w2_scale, y_perm,
                       stream=None):
     """moe_expert_ffn over rows and weights in 8 bits: x_perm [R,d] int8, W1, W3 [E,f,d] and W2 [E,d,f] int8, scales fp32
     for each row and each output channel, y_perm [R,d] bf16."""
-    d, f, E = ctx.d_model, ctx.d_ff, ctx.E
-    w1, s1 = _matrices(E, f, d, W1, w1_scale, "W1")
-    w3, s3 = _matrices(E, f, d, W3, w3_scale, "W3")
-    w2, s2 = _matrices(E, d, f, W2, w2_scale, "W2")
-    _check(lib().moe_expert_ffn_i8(ctx._h, _addr(x_perm, torch.int8, (R, d), "x_perm"),
-                                   _addr(x_scale, torch.float32, (R,), "x_scale"),
-                                   _addr(offsets, torch.int32, (E + 1,), "offsets"), R, w1, s1, w3, s3, w2, s2,
-                                   _addr(y_perm, torch.bfloat16, (R, d), "y_perm"), _stream_addr(stream)),
+    d, f, E, device = ctx.d_model, ctx.d_ff, ctx.E, ctx.device
+    w1, s1 = _matrices(E, f, d, device, W1, w1_scale, "W1")
+    w3, s3 = _matrices(E, f, d, device, W3, w3_scale, "W3")
+    w2, s2 = _matrices(E, d, f, device, W2, w2_scale, "W2")
+    _check(lib().moe_expert_ffn_i8(ctx._h, _addr(x_perm, torch.int8, (R, d), device, "x_perm"),
+                                   _addr(x_scale, torch.float32, (R,), device, "x_scale"),
+                                   _addr(offsets, torch.int32, (E + 1,), device, "offsets"), R, w1, s1, w3, s3, w2, s2,
+                                   _addr(y_perm, torch.bfloat16, (R, d), device, "y_perm"), _stream_addr(stream, device)),
            "moe_expert_ffn_i8")
 
 
@@ -400,12 +409,14 @@ def moe_layer_forward_i8(ctx: MoeContext, x, x_i8, x_scale, w_router, bias, W1, 
                          stream=None):
     """moe_layer_forward with experts in 8 bits: x [T,d] bf16 for the router, x_i8 [T,d] int8 and x_scale [T] fp32 for the
     experts (all three are outputs of moe_rmsnorm_i8), weights as for moe_expert_ffn_i8, y [T,d] bf16."""
-    d, f, E = ctx.d_model, ctx.d_ff, ctx.E
-    w1, s1 = _matrices(E, f, d, W1, w1_scale, "W1")
-    w3, s3 = _matrices(E, f, d, W3, w3_scale, "W3")
-    w2, s2 = _matrices(E, d, f, W2, w2_scale, "W2")
-    _check(lib().moe_layer_forward_i8(ctx._h, _addr(x, torch.bfloat16, (T, d), "x"), _addr(x_i8, torch.int8, (T, d), "x_i8"),
-                                      _addr(x_scale, torch.float32, (T,), "x_scale"),
-                                      _addr(w_router, torch.float32, (d, E), "w_router"),
-                                      _addr(bias, torch.float32, (E,), "bias"), w1, s1, w3, s3, w2, s2, T,
-                                      _addr(y, torch.bfloat16, (T, d), "y"), _stream_addr(stream)), "moe_layer_forward_i8")
+    d, f, E, device = ctx.d_model, ctx.d_ff, ctx.E, ctx.device
+    w1, s1 = _matrices(E, f, d, device, W1, w1_scale, "W1")
+    w3, s3 = _matrices(E, f, d, device, W3, w3_scale, "W3")
+    w2, s2 = _matrices(E, d, f, device, W2, w2_scale, "W2")
+    _check(lib().moe_layer_forward_i8(ctx._h, _addr(x, torch.bfloat16, (T, d), device, "x"),
+                                      _addr(x_i8, torch.int8, (T, d), device, "x_i8"),
+                                      _addr(x_scale, torch.float32, (T,), device, "x_scale"),
+                                      _addr(w_router, torch.float32, (d, E), device, "w_router"),
+                                      _addr(bias, torch.float32, (E,), device, "bias"), w1, s1, w3, s3, w2, s2, T,
+                                      _addr(y, torch.bfloat16, (T, d), device, "y"), _stream_addr(stream, device)),
+           "moe_layer_forward_i8")

@@ -62,3 +62,81 @@ def test_products_without_a_context_are_refused(lib):
     assert gemm(lib) == INVALID
     assert lib.moe_expert_ffn_i8(NULL, P, P, P, C.c_int32(4), P, P, P, P, P, P, P, NULL) == INVALID
     assert lib.moe_layer_forward_i8(NULL, P, P, P, P, NULL, P, P, P, P, P, P, C.c_int32(4), P, NULL) == INVALID
+
+
+class Tensor:
+    """What the binding asks of a tensor, for a GPU that this machine need not have."""
+
+    def __init__(self, dtype, *shape, device=0):
+        import torch
+        self.dtype, self.shape, self.device = dtype, torch.Size(shape), torch.device("cuda", device)
+        self.is_cuda = True
+
+    def get_device(self): return self.device.index
+    def is_contiguous(self): return True
+    def data_ptr(self): return 64
+    def dim(self): return len(self.shape)
+    def stride(self, dim=None):
+        strides = [1] * len(self.shape)
+        for i in reversed(range(len(strides) - 1)):
+            strides[i] = strides[i + 1] * self.shape[i + 1]
+        return strides if dim is None else strides[dim]
+
+
+class Stream:
+    def __init__(self, device): self.device_index, self.cuda_stream = device, 0
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Names of the calls that got through the binding's checks; the current device is 0."""
+    import torch
+    from paper_2605_17889_amd import binding
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *arguments: made.append(name) or 0
+
+    made = []
+    monkeypatch.setattr(binding, "lib", Library)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    return made
+
+
+def arguments_of(name):
+    """Arguments of a complete call, the context apart, and how many of its first ones are tensors' places."""
+    import torch
+    bf, i8, f32, i32 = torch.bfloat16, torch.int8, torch.float32, torch.int32
+    T = Tensor
+    matrices = lambda: [t for n, k in ((128, 512), (128, 512), (512, 128)) for t in (T(i8, 2, n, k), T(f32, 2, n))]
+    return {
+        "moe_rmsnorm_i8": lambda: [T(bf, 4, 64), T(bf, 4, 64), T(bf, 64), 1e-6, T(bf, 4, 64), T(bf, 4, 64), T(i8, 4, 64), T(f32, 4)],
+        "moe_quantize_i8": lambda: [T(bf, 4, 64), T(i8, 4, 64), T(f32, 4)],
+        "moe_gemm_i8": lambda: [T(i8, 4, 256), T(f32, 4), T(i32, 2), 4, 1, 64, 256, T(i8, 64, 256), T(f32, 64), T(bf, 4, 64)],
+        "moe_expert_ffn_i8": lambda: [T(i8, 4, 512), T(f32, 4), T(i32, 3), 4, *matrices(), T(bf, 4, 512)],
+        "moe_layer_forward_i8": lambda: [T(bf, 4, 512), T(i8, 4, 512), T(f32, 4), T(f32, 512, 2), T(f32, 2), *matrices(), 4,
+                                         T(bf, 4, 512)],
+    }[name]()
+
+
+@pytest.mark.parametrize("name", ["moe_rmsnorm_i8", "moe_quantize_i8", "moe_gemm_i8", "moe_expert_ffn_i8", "moe_layer_forward_i8"])
+def test_tensors_and_streams_of_another_gpu_are_refused(calls, name):
+    """Kernels run on the current GPU, the context's: memory of another one need not be mapped there."""
+    from types import SimpleNamespace
+    from paper_2605_17889_amd import binding
+    context = [SimpleNamespace(_h=None, device=0, d_model=512, d_ff=128, E=2)] if "norm" not in name and "quant" not in name else []
+    call = getattr(binding, name)
+    call(*context, *arguments_of(name))
+    call(*context, *arguments_of(name), stream=Stream(0))
+    assert calls == [name] * 2
+    for i, a in enumerate(arguments_of(name)):
+        if isinstance(a, Tensor):
+            other = arguments_of(name)
+            other[i] = Tensor(a.dtype, *a.shape, device=1)
+            with pytest.raises(binding.MoeError):
+                call(*context, *other)
+    with pytest.raises(binding.MoeError):
+        call(*context, *arguments_of(name), stream=Stream(1))
+    assert calls == [name] * 2
