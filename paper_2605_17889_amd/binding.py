@@ -326,6 +326,8 @@ def _addr(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, device: i
 
 def _rows_addr(t: torch.Tensor, device: int, what: str):
     """-> (address, row stride) of a 2-D bf16 tensor on that GPU whose rows are contiguous and do not overlap."""
+    if t is None:
+        raise MoeError(f"{what}: missing")
     if t.dtype is not torch.bfloat16 or t.dim() != 2 or t.get_device() != device or (t.shape[1] > 1 and t.stride(1) != 1):
         raise MoeError(f"{what}: expected a 2-D tensor of {torch.bfloat16} with contiguous rows on cuda:{device}, got "
                        f"{t.dtype} on {t.device}, shape={tuple(t.shape)}, strides={t.stride()}")

@@ -140,3 +140,11 @@ def test_tensors_and_streams_of_another_gpu_are_refused(calls, name):
     with pytest.raises(binding.MoeError):
         call(*context, *arguments_of(name), stream=Stream(1))
     assert calls == [name] * 2
+
+
+def test_rows_that_are_missing_are_refused(calls):
+    from paper_2605_17889_amd import binding
+    for name in ("moe_rmsnorm_i8", "moe_quantize_i8"):
+        with pytest.raises(binding.MoeError):
+            getattr(binding, name)(None, *arguments_of(name)[1:])
+    assert not calls
