@@ -61,16 +61,16 @@ int launch_select_hist_permute(const float* logits, int T, int E, int k, int32_t
                                int32_t* seg_tables, hipStream_t s);
 int launch_gather(const moe_bf16* x, const int32_t* perm, const int32_t* offsets, int R, int d,
                   int k, int E, moe_bf16* x_perm, hipStream_t s);
-// Memory that is zero between launches: counters from which persistent workgroups draw their tiles, then the sums and counters
-// of split reductions. A context takes a set of its device's 64 and gives it back; set -1: there is none left (the caller
-// then zeroes memory of its own). The calling thread's current device must be `device`.
+// Counters from which persistent workgroups draw their tiles, kTileCounterBytes that are zero between launches.
+// A context takes a set of its device's 64 and gives it back; set -1: there is none left (the caller then zeroes
+// memory of its own). The calling thread's current device must be `device`.
 constexpr size_t kTileCounterBytes = kXcds * 128;
+int32_t* take_tile_counters(int device, int* set);
+void give_tile_counters(int device, int set);
+// Sums of split reductions, in memory that a context allocates for its first call that may split one.
 constexpr int kPartSums = 6 << 18;        // 6 MB of them
 constexpr int kSplitTiles = 128;
 constexpr size_t kSplitSumBytes = kSplitTiles * (256 + 1) * sizeof(int32_t);   // of 256 sums and a counter each
-constexpr size_t kZeroedBytes = kTileCounterBytes + kSplitSumBytes;
-int32_t* take_tile_counters(int device, int* set);
-void give_tile_counters(int device, int set);
 // Where and how a context launches its expert GEMMs: its device, its tile counters and the tuning knobs of
 // moe_set_gemm_config (all settings give identical bits).
 struct GemmEnv {
@@ -81,8 +81,8 @@ struct GemmEnv {
     bool split_last_round = true;     // large tiles: halve the tiles of a last round under half full
     int large_tile_waves = 0;         // 0: automatic; 4 / 8: wavefronts of the 256 x 256 tile
     int32_t* tile_counters = nullptr; // kTileCounterBytes, zero between launches
-    int32_t* split_sums = nullptr;    // kSplitSumBytes, zero between launches: 8-bit products of few rows, split reductions
-    int32_t* part_sums = nullptr;     // kPartSums: the same of more rows, parts that a second launch joins
+    int32_t* split_sums = nullptr;    // kSplitSumBytes, zero between launches: 8-bit products of few rows through one matrix
+    int32_t* part_sums = nullptr;     // kPartSums: of more rows without offsets, parts that a second launch joins
 };
 int launch_gateup(const GemmEnv& env, const moe_bf16* a, const int32_t* row_index, int index_div,
                   const int32_t* offsets, int R, int R_hint, int d, int f, int E,

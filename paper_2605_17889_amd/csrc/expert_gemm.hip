@@ -18,7 +18,7 @@
 namespace moe {
 
 constexpr int kCounterSets = 64;
-static __device__ __align__(256) int32_t tile_counter_sets[kCounterSets][kZeroedBytes / sizeof(int32_t)];
+static __device__ __align__(256) int32_t tile_counter_sets[kCounterSets][kTileCounterBytes / sizeof(int32_t)];
 static std::atomic<uint64_t> counter_sets_taken[64];         // one bit per set and device
 static std::atomic<int32_t*> counter_sets_at[64];
 
@@ -39,7 +39,7 @@ int32_t* take_tile_counters(int device, int* set) {
         const int n = __builtin_ctzll(~taken);
         if (counter_sets_taken[device].compare_exchange_weak(taken, taken | (1ull << n), std::memory_order_acq_rel)) {
             *set = n;
-            return base + n * (kZeroedBytes / sizeof(int32_t));
+            return base + n * (kTileCounterBytes / sizeof(int32_t));
         }
     }
     return nullptr;

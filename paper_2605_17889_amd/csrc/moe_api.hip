@@ -69,7 +69,7 @@ bool on_own_device(const moe_ctx* c) {
 }
 
 struct Layout {
-    size_t topk_idx, topk_w, counts, offsets, perm, inv_perm, scratch, logits, x_perm, H, y_perm, counters, part_sums, total;
+    size_t topk_idx, topk_w, counts, offsets, perm, inv_perm, scratch, logits, x_perm, H, y_perm, counters, total;
 };
 
 Layout layout_for(const moe_shape* s) {
@@ -88,8 +88,7 @@ Layout layout_for(const moe_shape* s) {
     L.x_perm = take(R * s->d_model * 2);
     L.H = take(R * s->d_ff * 2);
     L.y_perm = take(R * s->d_model * 2);
-    L.counters = take(kZeroedBytes);
-    L.part_sums = take(kPartSums * sizeof(int32_t));
+    L.counters = take(kTileCounterBytes);
     L.total = off ? off : 256;
     return L;
 }
@@ -188,7 +187,30 @@ int forward_chunk(moe_ctx* c, const moe_bf16* x, const float* w_router, const fl
     });
 }
 
+// Memory of split reductions (products of one matrix), its zeros by a copy of the host's, which has ended when it returns.
+int ensure_sums(moe_ctx* c) {
+    if (c->gemm.split_sums) return MOE_OK;
+    void* p = nullptr;
+    if (hipMalloc(&p, kSplitSumBytes + kPartSums * sizeof(int32_t)) != hipSuccess) {
+        (void)hipGetLastError();
+        return MOE_ERR_WORKSPACE;
+    }
+    static const unsigned char zeros[kSplitSumBytes] = {};
+    if (hipMemcpy(p, zeros, sizeof(zeros), hipMemcpyHostToDevice) != hipSuccess) {
+        (void)hipGetLastError();
+        (void)hipFree(p);
+        return MOE_ERR_HIP;
+    }
+    c->gemm.split_sums = static_cast<int32_t*>(p);
+    c->gemm.part_sums = c->gemm.split_sums + kSplitSumBytes / sizeof(int32_t);
+    return MOE_OK;
+}
+
 int ensure_i8(moe_ctx* c) {
+    if (c->shape.E == 1) {                           // the down projection is then a product of one matrix
+        const int rc = ensure_sums(c);
+        if (rc != MOE_OK) return rc;
+    }
     if (c->h_i8) return MOE_OK;
     const size_t rows = static_cast<size_t>(c->shape.T_max) * c->shape.k, bytes = align_up(rows * c->shape.d_ff);
     void* p = nullptr;
@@ -315,7 +337,7 @@ int moe_create(moe_ctx** out, const moe_shape* shape, int device_id) {
     if (err == hipSuccess) err = hipMalloc(&p, L.total);
     int32_t* counters = err == hipSuccess ? take_tile_counters(device_id, &c->counter_set) : nullptr;
     if (err == hipSuccess && counters == nullptr) {          // a copy of the host's: it has ended when it returns
-        static const unsigned char zeros[kZeroedBytes] = {};
+        static const unsigned char zeros[kTileCounterBytes] = {};
         counters = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(p) + L.counters);
         err = hipMemcpy(counters, zeros, sizeof(zeros), hipMemcpyHostToDevice);
     }
@@ -343,8 +365,6 @@ int moe_create(moe_ctx** out, const moe_shape* shape, int device_id) {
     c->h_i8 = nullptr;
     c->h_scale = c->x_scale = nullptr;
     c->gemm.tile_counters = counters;
-    c->gemm.split_sums = counters + kTileCounterBytes / sizeof(int32_t);
-    c->gemm.part_sums = reinterpret_cast<int32_t*>(c->base + L.part_sums);
     c->prof_armed = false;
     c->prof_max_calls = c->prof_calls = 0;
     for (auto& v : c->prof_launches) v = 0;
@@ -371,6 +391,7 @@ int moe_destroy(moe_ctx* c) {
     if (c->slot[0] && hipFree(c->slot[0]) != hipSuccess) rc = MOE_ERR_HIP;
     if (c->y_perm_f32 && hipFree(c->y_perm_f32) != hipSuccess) rc = MOE_ERR_HIP;
     if (c->h_i8 && hipFree(c->h_i8) != hipSuccess) rc = MOE_ERR_HIP;
+    if (c->gemm.split_sums && hipFree(c->gemm.split_sums) != hipSuccess) rc = MOE_ERR_HIP;
     if (c->base && hipFree(c->base) != hipSuccess) rc = MOE_ERR_HIP;
     give_tile_counters(c->device, c->counter_set);
     delete c;
@@ -717,6 +738,10 @@ int moe_gemm_i8(moe_ctx* c, const moe_i8* x, const float* x_scale, const int32_t
     if (E > kMaxExperts || N % 16 != 0 || N < 32 || N > kMaxDimI8 || K % 128 != 0 || K > kMaxSumI8) return MOE_ERR_UNSUPPORTED_SHAPE;
     if (R == 0) return MOE_OK;
     if (!x || !x_scale || !W || !w_scale || !out || !at_16_bytes(x, W, out)) return MOE_ERR_INVALID_ARG;
+    if (E == 1) {
+        const int rc = ensure_sums(c);
+        if (rc != MOE_OK) return rc;
+    }
     return launch_product_i8(c->gemm, x, x_scale, offsets, R, N, K, E, W, w_scale, out, out_type == MOE_OUT_FP32,
                              static_cast<hipStream_t>(stream));
 }

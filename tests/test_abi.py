@@ -93,3 +93,12 @@ def test_binding_fails_loudly_without_gpu():
         pytest.skip("a GPU is present")
     with pytest.raises(binding.MoeError):
         binding.MoeContext(16, 512, 1024, 8, 2)
+
+
+def test_workspace_of_a_small_context_is_small(lib):
+    """What only 8-bit products need (6 MB of partial sums) is not part of every context: one token's tables, rows and
+    the tile counters are each rounded up to 256 bytes."""
+    from paper_2605_17889_amd.binding import MoeShape
+    one = MoeShape(1, 512, 128, 1, 1)
+    rows = 512 * 2 + 128 * 2 + 512 * 2
+    assert rows < lib.moe_workspace_bytes(C.byref(one)) <= rows + 12 * 256 + 8 * 128 + 16 * 1024

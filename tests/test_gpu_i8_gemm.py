@@ -630,3 +630,28 @@ def test_ties_of_h_go_to_even(rows):
         q = y.double() * 127 / peak                  # off by y's rounding, 2^-8 of up to 127: less than half a step
         assert ((q - want).abs() <= 0.51)[lo == hi].all() and (lo == hi).double().mean() > 0.99
     ctx.close()
+
+
+def test_split_reductions_of_many_contexts():
+    """More contexts at once than a device has sets of counters; each has sums of its own, made by its first call, zero then and
+    after every call. One matrix, and the expert FFN of a context of one expert, whose down projection splits too."""
+    d, f = 512, 8192
+    g = gen(9)
+    x, xs, w, ws = whole(g, 40, f), positive(g, 40), whole(g, d, f), positive(g, d)
+    q, qs = whole(g, 3, d), positive(g, 3)
+    up = [t for _ in range(2) for t in (whole(g, 1, f, d), positive(g, 1, f) / 20)]
+    want = {T: product64(x[:T], xs[:T], w, ws) for T in (3, 16, 40)}
+    for _ in range(2):
+        ctxs = [B.MoeContext(40, d, f, 1, 1) for _ in range(70)]
+        ffn = []
+        for c in (0, 1, 63, 64, 69, 1, 69):
+            for T in (3, 40, 16, 3):
+                out = torch.empty((T, d), device="cuda")
+                B.moe_gemm_i8(ctxs[c], x[:T], xs[:T], None, T, 1, d, f, w, ws, out)
+                assert_near(out, want[T], 0.0)
+            y = torch.empty((3, d), dtype=torch.bfloat16, device="cuda")
+            B.moe_expert_ffn_i8(ctxs[c - 2], q, qs, groups([3]), 3, *up, w[None], ws[None], y)
+            ffn.append(y)
+        assert all(torch.equal(ffn[0], y) for y in ffn[1:]) and ffn[0].isfinite().all()
+        for c in ctxs:
+            c.close()
