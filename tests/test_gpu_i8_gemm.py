@@ -655,3 +655,13 @@ def test_split_reductions_of_many_contexts():
         assert all(torch.equal(ffn[0], y) for y in ffn[1:]) and ffn[0].isfinite().all()
         for c in ctxs:
             c.close()
+
+
+@pytest.mark.parametrize("T,N,K", [(17, 256, 16384), (30, 272, 8192), (32, 2048, 8192), (33, 1024, 14336), (60, 272, 16384),
+                                   (64, 528, 12288), (20, 2048, 2048), (64, 4096, 4096)])
+def test_split_reductions_from_k_steps_in_turn(T, N, K):
+    """One row tile at pitches of whole 4 KB (and 2 KB): every part starts at a k-step of its own and goes round. The parts'
+    sums are whole numbers, so the bits are those of a reduction that is not split, with offsets."""
+    for dtype in (torch.bfloat16, torch.float32):
+        a = gemm_case([T], N, K, dtype, seed=T, dense=True)
+        assert torch.equal(a, gemm_case([T], N, K, dtype, seed=T))
