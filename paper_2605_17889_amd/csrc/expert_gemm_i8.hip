@@ -6,6 +6,7 @@
 // The kernels and the rules by which tiles are chosen are those of the bf16 products, with rows of half as many 16-bit
 // units (expert_gemm_kernel.h). The sums are whole numbers: every tile and order of them gives the same bits.
 #include "expert_gemm_launch.h"
+#include "i8_tile_rules.h"
 #include "rows_i8.h"
 
 namespace moe {
@@ -421,29 +422,6 @@ bool many_short_tiles(const Call& c) {
     return c.env.forced_config < 0 && c.K <= 1024 && touched(c) * (c.N / 128) >= 2.9 * compute_units(c.env.device);
 }
 
-// Whether the groups mostly fit 128 rows, 1.5 standard deviations above the mean, in reductions from 4096 elements on with tiles for
-// all compute units: a second tile for the largest costs less than 256-row ones for all, of half the height too. 256- -> 128-row tiles, 110 rows each, us, groups alike | as skewed as rank^-0.5: gate/up, 8
-// experts of 4096 x 14336 217 -> 200 | 246 -> 215, 8192 x 8192 225 -> 202 | 249 -> 229, 6144 x 16384 318 -> 313 | 351 -> 342, 5120 x 10240
-// 200 -> 196 | 213 -> 228, 16 of 4096 x 4096 129 -> 113 | 137 -> 125; down at 4096 x 14336 120 -> 96 | 117 -> 152, 8192 x 8192 129 -> 102 |
-// 139 -> 141, 16 of 4096 x 4096 72 -> 55 | 79 -> 79. With fewer tiles two experts of 4096 x 14336 59 -> 74, down at 5120 x 10240 99 ->
-// 107. 130 rows, 4096 x 14336: gate/up 223 -> 245 | 238 -> 234, down 121 -> 157 | 117 -> 148.
-bool most_fit_128_rows(const Call& c, int mid_n_tiles) {
-    const double avg = static_cast<double>(c.R) / c.E;
-    return c.K >= 2048 && static_cast<double>(c.E) * mid_n_tiles >= compute_units(c.env.device) &&
-           avg + 1.5 * std::sqrt(avg) <= 128.0;
-}
-
-// Gate/up reductions from 4096 elements on: 128- instead of 64- and 96-row tiles from 46 rows a group on, us, groups alike | as
-// skewed as rank^-0.5: 46 rows for each of 8 experts of 4096 x 14336 166 -> 171 | 183 -> 176, 6144 x 16384 280 -> 267 | 311 -> 277, 8192 x
-// 8192 173 -> 174 | 200 -> 173, 5120 x 10240 157 -> 164 | 179 -> 169, 16 of 6144 x 6144 211 -> 201 | 230 -> 205; 34 rows 156 -> 167 | 161 ->
-// 170, 264 -> 264 | 273 -> 260, 171 -> 174 | 174 -> 172, 149 -> 159 | 151 -> 161, 198 -> 196 | 220 -> 202; 58 rows, of 96 179 -> 179 | 207
-// -> 184, 283 -> 282 | 331 -> 289, 177 -> 175 | 218 -> 175, 167 -> 172 | 205 -> 178, 210 -> 208 | 237 -> 241.
-bool gateup_of_128_rows(const Call& c, int config) {
-    if (config == 0) return most_fit_128_rows(c, c.N / 128);
-    return (config == 2 || config == 4) && c.K >= 2048 && c.R >= 46.0 * c.E &&
-           static_cast<double>(c.E) * (c.N / 128) >= compute_units(c.env.device);
-}
-
 template <class Cfg>
 int converted(const Call& c) {
     static std::atomic<uint64_t> attr_set[2];
@@ -458,7 +436,7 @@ int gateup(const Call& c) {
     if (few_rows_fits(c)) return few_rows<true, false>(c);
     int config = pick_config(c.env, c.R, c.E, gateup_tiles(c.E, c.K, c.N));
     if (config == 0 && !large_takes(c.N, c.K)) config = 1;
-    if (c.env.forced_config < 0 && gateup_of_128_rows(c, config)) config = 1;
+    if (c.env.forced_config < 0) config = i8_gateup_config(config, c.R, c.E, c.N, c.K, compute_units(c.env.device));
     switch (config) {
         case 0: return large<GateUp1W>(c);
         case 1: return grouped<GateUpMid, GateUpMidS>(c);
@@ -568,29 +546,6 @@ int priced(const Call& c) {
     return grouped<Out<F32, PlainSmall>>(c);
 }
 
-// Long reductions whose weights stream past groups of few rows: a tile with rows to spare takes the time of one that just
-// holds the mean, and a group that outgrows its tile costs a second tile's stream, often a second round. From 4096 elements on:
-// 96- and 128-row tiles where their rounds (one, or two full ones) leave few compute units idle; 32- or 64-row tiles -> so, us,
-// groups alike | as skewed as rank^-0.5: 8 experts of 4096 x 14336, 20 rows each 72 -> 76 | 99 -> 73, 38 77 -> 77 | 116 -> 77, 52 114
-// -> 78 | 108 -> 84, of 6144 x 16384 20 127 -> 122 | 151 -> 124, 52 166 -> 127 | 163 -> 131, of 5120 x 10240 38 84 -> 80 | 95 -> 84, of
-// 8192 x 8192 20 88 -> 85 | 98 -> 82, 52 110 -> 82 | 111 -> 86, 16 of 4096 x 4096 20 45 -> 45 | 49 -> 45, 52 58 -> 44 | 58 -> 48, of
-// 2048 x 4096 20 24 -> 25 | 28 -> 25, 52 32 -> 25 | 33 -> 27. With half of them idle small tiles stay (8 of 2048 x 8192, 28 rows 22,
-// 96-row tiles 34), and with a round and a half (16 of 6144 x 6144, 20 rows 96, 114 | 101, 106). Elsewhere 64- instead of 32-row tiles
-// (8 of 2048 x 8192, 18 rows 27 -> 27 | 33 -> 27; below 4096 elements 60 of 1536 x 1536, 14 rows 26.0, 28.2 | 25.5, 29.9) and 128-
-// instead of 96-row ones (72 rows, 16 of 6144 x 6144 119 -> 120 | 120 -> 119, 8 of 8192 x 8192 84 -> 85 | 130 -> 88; below, 64 of 2048 x
-// 1408 43, 45 | 51, 55).
-int tiles_of_uneven_groups(const Call& c, int config, int mid_n_tiles) {
-    const double avg = static_cast<double>(c.R) / c.E;
-    if (config == 0) return most_fit_128_rows(c, mid_n_tiles) ? 1 : 0;
-    if (config == 1 || avg < 16.0) return config;
-    const int cus = compute_units(c.env.device);
-    const double mid = static_cast<double>(c.E) * mid_n_tiles;
-    if (c.K < 2048) return config;
-    if (mid >= 0.6 * cus && mid <= 2.0 * cus && (mid <= cus || last_round_use(mid, cus) >= 0.95)) return avg <= 32.0 ? 4 : 1;
-    if (config == 3 && static_cast<double>(c.E) * (c.N / 64) >= cus) return 2;
-    return config == 4 ? 1 : config;
-}
-
 template <bool F32>
 int product(const Call& c) {
     if (few_rows_fits(c)) return few_rows<false, F32>(c);
@@ -603,7 +558,7 @@ int product(const Call& c) {
     if (config == 0 && (!large_takes(d, c.K) || d < 256)) config = 1;
     if ((config == 1 || config == 4) && d < 128) config = 2;
     if (config == 2 && d < 64) config = 3;
-    if (c.env.forced_config < 0) config = tiles_of_uneven_groups(c, config, wide_mid ? d / 256 : d / 128);
+    if (c.env.forced_config < 0) config = i8_product_config(config, c.R, c.E, d, c.K, wide_mid ? d / 256 : d / 128, cus);
     // Reductions of up to 1024 elements over many tiles: the pipelined 64 x 128 tile, two on a compute unit. Grouped forms -> so,
     // through 8 of 128 experts of 2048 x 768: 120 tokens 113 -> 111 us, 300 122 -> 115, 600 132 -> 122, 1000 140 -> 131 (all with
     // gate/up); 1408 elements, 600 tokens through 6 of 64 119 -> 122.
