@@ -66,25 +66,34 @@ int spread_steps(int R, int E, int N, int K, bool dual) {
     return K < 6144 || bytes < 0.8e9 ? 0 : K % 16384 == 0 ? 2 : 1;
 }
 
-// Whether the n-tiles of a product of whole numbers start at k-steps of their own (gemm::first_kstep) instead of together or
-// late: at pitches of whole 4 KB, where weight rows fall on few memory channels. Expert FFN and its down projection alone,
-// together -> so, us: 12 rows for each of 8 experts of 8192 x 8192 271 and 92 -> 257 and 85, 64 317 and 116 -> 260 and 84, 4 of
-// 16 of 4096 x 4096 151 and 49 -> 133 and 44, 64 190 and 67 -> 148 and 48, 24 of 8 of 6144 x 16384 (late before) 397 and 127 -> 389
-// and 120; one matrix of 8192 x 8192, 37 rows 20.3 -> 17.8. 96- and 128-row tiles at all longer pitches: 90 rows, 8 of 4096 x 14336,
-// down turned too 290 -> 275, 16 of 6144 x 6144 367 -> 347, 8 of 5120 x 10240 290 -> 280. Lower ones lose at others (down at 14336
-// bytes 70 -> 72; gate/up at 7168 67 -> 69.5), and those of 16 rows at all (8192 x 2048, one row 19.6 -> 22). At 2 KB gate/up of
-// many n-tiles gains (8 of 2048 x 8192, 12 rows 56 -> 50), of few not (64 of 2048 x 1408, 24 rows 69 -> 72), nor does down
-// (7168 x 2048 22 -> 23). Pipelined tiles turn for one row tile: several share an n-tile's weights, but each n-tile then asks for
-// rows of its own (14336 x 4096, 1003 rows 68 -> 75, 8192 x 8192, 512 40 -> 44; 2048 x 32000, 37 rows 17 -> 15).
+// Whether weight rows that far apart in bytes, streamed at the same k by workgroups that started together, fall on few memory
+// channels: a multiple of 4 KB, or a divisor of it, with which every few rows come round to the same place.
+bool rows_on_few_channels(int pitch) { return pitch % 4096 == 0 || 4096 % pitch == 0; }
+
+// Whether the n-tiles of a product of whole numbers start at k-steps of their own (gemm::first_kstep) instead of together or late:
+//   - rows 4 KB or a multiple apart;
+//   - gate/up of 32 n-tiles and more, rows a divisor of 4 KB apart;
+//   - 96- and 128-row tiles, rows more than 4 KB apart.
+// Never 16-row tiles (8192 x 2048, one row 19.6 -> 22 us). Together -> so, us, other weights for every call. Multiples: expert FFN
+// of 8 experts of 8192 x 8192, 12 rows each 271 -> 257, 64 317 -> 260. Divisors, gate/up: 6 rows for each of 8 of 2048 x 8192 53.5 ->
+// 44.3, 32 of 2048 x 2048 55 -> 46, 8 of 1024 x 16384 53.8 -> 52.6, of 512 x 16384 32.5 -> 31.8 (at worst 24 for each of 32 of 1024 x 2048
+// 27.5 -> 28.3); fewer n-tiles, 24 for each of 64 of 2048 x 1408 65 -> 67; down, 7168 x 2048 22 -> 23. Others: gate/up at 1536 and
+// 10240 within 1 %, 2560 57 -> 58, 3584 76 -> 77, 14336 563 -> 568, but all longer ones of 96- and 128-row tiles, whose workgroups are
+// the fewest, gain: 90 rows, 8 of 4096 x 14336, down turned too 290 -> 275.
 template <class Cfg>
 bool turned_ksteps(int N, int K) {
     if (!gemm::operands_i8<Cfg>::value || Cfg::BM == 16) return false;
     const int pitch = 2 * K;
-    return pitch % 4096 == 0 || (Cfg::BM >= 96 && pitch > 4096) || (pitch == 2048 && Cfg::DUAL && N >= 32 * Cfg::BN_OUT);
+    return pitch % 4096 == 0 || (Cfg::BM >= 96 && pitch > 4096) ||
+           (Cfg::DUAL && N >= 32 * Cfg::BN_OUT && rows_on_few_channels(pitch));
 }
+// The same of the pipelined tiles: for one matrix and one row tile (several share an n-tile's weights, but each n-tile then asks
+// for rows of its own: 14336 x 4096, 1003 rows 68 -> 75) at both kinds of distance. us, 37 rows, 32000 columns, other weights for
+// every call: of 1024 10.4 -> 10.0, 2048 18.2 -> 16.1, 4096 31.2 -> 27.7, 8192 57 -> 51; between them 1536 13.7 -> 13.5, 2560 21.6 ->
+// 21.5, 3584 25.8 -> 26.2, 5120 37.4 -> 36.7, 7168 46.4 -> 47.3; 16384 columns of 14336 45 -> 47. 4096 columns: within 1 %.
 template <class Cfg>
 bool turned_ksteps_of_one(int R, int E, int K) {
-    return E == 1 && R <= Cfg::BM && (2 * K % 4096 == 0 || 2 * K == 2048);
+    return E == 1 && R <= Cfg::BM && rows_on_few_channels(2 * K);
 }
 
 // Whether tiles of Cfg::BN_OUT columns cover N of them (gemm::n_tiles).

@@ -665,3 +665,17 @@ def test_split_reductions_from_k_steps_in_turn(T, N, K):
     for dtype in (torch.bfloat16, torch.float32):
         a = gemm_case([T], N, K, dtype, seed=T, dense=True)
         assert torch.equal(a, gemm_case([T], N, K, dtype, seed=T))
+
+
+@pytest.mark.parametrize("T,N,K", [(17, 4096, 512), (64, 2064, 512), (33, 8192, 1024), (64, 1040, 1024), (20, 32000, 2048), (129, 4096, 1024)])
+def test_one_matrix_from_k_steps_in_turn(T, N, K):
+    for dtype in (torch.bfloat16, torch.float32):
+        a = gemm_case([T], N, K, dtype, seed=T, dense=True)
+        assert torch.equal(a, gemm_case([T], N, K, dtype, seed=T, config=1))
+
+
+@pytest.mark.parametrize("counts", [[1, 0, 2, 1], [2, 0, 17, 40], [33, 64, 5, 20], [70, 100, 3, 90]])
+@pytest.mark.parametrize("d,f", [(512, 8192), (1024, 4096), (2048, 4096)])
+def test_gateup_from_k_steps_in_turn(counts, d, f):
+    want = ffn_case(counts, d, f, seed=d)
+    assert torch.equal(want, ffn_case(counts, d, f, seed=d, config=0, check=False))

@@ -57,3 +57,13 @@ def test_long_reductions_of_few_rows(say):
         assert int(say("product", config, 8 * rows, 8, 4096, 14336, 32)) == want
     assert int(say("product", ROWS32, 8 * 18, 8, 2048, 8192, 16)) == ROWS64      # half the compute units idle with 128 columns
     assert int(say("product", ROWS96, 64 * 72, 64, 2048, 1408, 16)) == ROWS96
+
+
+@pytest.mark.parametrize("K,gateup,down,mid,one", [
+    (512, 1, 0, 0, 1), (1024, 1, 0, 0, 1), (1536, 0, 0, 0, 0), (2048, 1, 0, 0, 1), (2560, 0, 0, 0, 0), (4096, 1, 1, 1, 1), (5120, 0, 0, 1, 0),
+    (6144, 0, 0, 1, 0), (8192, 1, 1, 1, 1), (14336, 0, 0, 1, 0)])
+def test_k_steps_in_turn_where_rows_fall_on_few_channels(say, K, gateup, down, mid, one):
+    """Weight rows a multiple or a divisor of 4 KB apart, whichever; gate/up of divisors with 32 n-tiles and more."""
+    assert say("turned", 0, 8192, K) == f"{gateup}{down}{mid}00"
+    assert say("turned", 0, 1408, K)[0] == str(int(K % 4096 == 0))
+    assert int(say("one", 37, 1, K)) == one and int(say("one", 65, 1, K)) == 0 and int(say("one", 37, 2, K)) == 0
