@@ -351,9 +351,10 @@ enum { MOE_OUT_BF16 = 0, MOE_OUT_FP32 = 1 };
  * (one matrix for all tokens). x [R,K]; x_scale [R]; W [E,N,K]; w_scale [E,N]; out [R,N] of out_type.
  * x, W and out start at multiples of 16 bytes (else MOE_ERR_INVALID_ARG). R <= T_max * k of the context, whose
  * d_model, d_ff and E play no part here. E <= 256; K a multiple of 128 up to 130944 (the sums
- * fit 32 bits); N a multiple of 16, 32 <= N <= 2^23; else MOE_ERR_UNSUPPORTED_SHAPE. The first call with E == 1
- * allocates 6.4 MB for the sums of split reductions, kept until moe_destroy (MOE_ERR_WORKSPACE if that fails): make one
- * before recording such calls into a HIP graph. */
+ * fit 32 bits); N a multiple of 16, 32 <= N <= 2^23; else MOE_ERR_UNSUPPORTED_SHAPE. A long
+ * reduction over few rows through one matrix is split over workgroups: the context's first such call allocates 6.4 MB for
+ * the sums, kept until moe_destroy. Where that fails, or the stream is being captured, the reduction is not split: the same
+ * bits, later. */
 int moe_gemm_i8(moe_ctx* ctx, const moe_i8* x, const float* x_scale, const int32_t* offsets,
                 int32_t R, int32_t E, int32_t N, int32_t K, const moe_i8* W, const float* w_scale,
                 void* out, int out_type, void* stream);
@@ -366,7 +367,7 @@ int moe_gemm_i8(moe_ctx* ctx, const moe_i8* x, const float* x_scale, const int32
  * x_perm [R,d_model]; x_scale [R]; W1, W3 [E,d_ff,d_model], their scales [E,d_ff]; W2
  * [E,d_model,d_ff], w2_scale [E,d_model]; y_perm [R,d_model] bf16 out; R <= T_max * k; x_perm, the
  * weights and y_perm start at multiples of 16 bytes (else MOE_ERR_INVALID_ARG). d_ff <= 65536. The first call allocates
- * T_max * k * (d_ff + 8) bytes, of a context with E == 1 moe_gemm_i8's 6.4 MB too, kept until moe_destroy (MOE_ERR_WORKSPACE if that fails): make one
+ * T_max * k * (d_ff + 8) bytes, kept until moe_destroy (MOE_ERR_WORKSPACE if that fails): make one
  * before recording such calls into a HIP graph. */
 int moe_expert_ffn_i8(moe_ctx* ctx, const moe_i8* x_perm, const float* x_scale,
                       const int32_t* offsets, int32_t R, const moe_i8* W1, const float* w1_scale,

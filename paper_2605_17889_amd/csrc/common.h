@@ -67,7 +67,7 @@ int launch_gather(const moe_bf16* x, const int32_t* perm, const int32_t* offsets
 constexpr size_t kTileCounterBytes = kXcds * 128;
 int32_t* take_tile_counters(int device, int* set);
 void give_tile_counters(int device, int set);
-// Sums of split reductions, in memory that a context allocates for its first call that may split one.
+// Sums of split reductions, in memory that a context allocates for its first call that splits one.
 constexpr int kPartSums = 6 << 18;        // 6 MB of them
 constexpr int kSplitTiles = 128;
 constexpr size_t kSplitSumBytes = kSplitTiles * (256 + 1) * sizeof(int32_t);   // of 256 sums and a counter each
@@ -83,6 +83,7 @@ struct GemmEnv {
     int32_t* tile_counters = nullptr; // kTileCounterBytes, zero between launches
     int32_t* split_sums = nullptr;    // kSplitSumBytes, zero between launches: 8-bit products of few rows through one matrix
     int32_t* part_sums = nullptr;     // kPartSums: of more rows without offsets, parts that a second launch joins
+    bool whole_reductions = false;    // split none (there is no such memory, and none can be had)
 };
 int launch_gateup(const GemmEnv& env, const moe_bf16* a, const int32_t* row_index, int index_div,
                   const int32_t* offsets, int R, int R_hint, int d, int f, int E,
@@ -113,6 +114,8 @@ int launch_gateup_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, 
 bool down_converts(const GemmEnv& env, int R, int d, int f, int E);
 int launch_down_converting_i8(const GemmEnv& env, const moe_bf16* H, const int32_t* offsets, int R, int d, int f, int E,
                               const moe_i8* W2, const float* w2_scale, void* y, bool y_f32, hipStream_t s);
+// kNeedsSums: nothing was enqueued; the reduction would be split, and env has no memory for its sums.
+constexpr int kNeedsSums = 1;
 int launch_product_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, int N, int K,
                       int E, const moe_i8* W, const float* w_scale, void* out, bool out_f32, hipStream_t s);
 

@@ -396,7 +396,7 @@ bool few_rows_fits(const Call& c) {
 // by 1 -> as here: 16384 x 256 12.3 -> 6.1 us (8), 8192 x 1024 7.7 -> 5.9 (4), 8192 x 2048 7.9 -> 6.9 (2); joining costs about 1 us,
 // 4096 x 512 4.9 -> 5.1 (2), 2048 x 1024 3.8 -> 4.6, and more with more parts (16384 x 256 in 16 7.0).
 int few_rows_splits(const Call& c) {
-    if (c.E != 1 || c.K < 3 * 1024) return 1;        // K counts pairs of elements
+    if (c.E != 1 || c.K < 3 * 1024 || c.env.whole_reductions) return 1;      // K counts pairs of elements
     const int tiles = c.N / 16;
     if (tiles > kSplitTiles) return 1;
     return std::max(1, std::min(compute_units(c.env.device) / tiles, c.K / 1024));
@@ -404,6 +404,7 @@ int few_rows_splits(const Call& c) {
 template <bool DUAL, bool F32>
 int few_rows(const Call& c) {
     const int splits = DUAL ? 1 : few_rows_splits(c);
+    if (splits > 1 && c.env.split_sums == nullptr) return kNeedsSums;
     const long long grid = (most_row_tiles(c.R, c.E, kFewRows) * (c.N / 16) * splits + kXcds - 1) / kXcds * kXcds;
     if (grid > 0x7fffffffLL) return MOE_ERR_UNSUPPORTED_SHAPE;
     hipLaunchKernelGGL((few_rows_i8_kernel<DUAL, F32>), dim3(static_cast<unsigned>(grid)), dim3(kFewWaves * kWave), 0, c.s,
@@ -495,7 +496,7 @@ Plan price(const Call& c) {
         if (c.N < t.cols || c.K / 64 < t.stages || (t.tile == Tile::large && !large_takes(c.N, c.K))) continue;
         const double row_tiles_of = c.E == 1 ? std::ceil(c.R / static_cast<double>(t.rows)) : row_tiles(c.R, c.E, t.rows);
         const double tiles = row_tiles_of * ((c.N + t.cols - 1) / t.cols);
-        const bool can_split = c.offsets == nullptr && t.tile <= Tile::t64x128;
+        const bool can_split = c.offsets == nullptr && t.tile <= Tile::t64x128 && !c.env.whole_reductions;
         for (int s = 1; s <= (can_split ? 16 : 1); ++s) {
             if (c.K / 64 / s < t.stages || (s > 1 && static_cast<double>(s) * c.R * c.N > kPartSums)) break;
             const double n = tiles * s, each = std::ceil(n / cus);           // workgroups of a compute unit
@@ -530,6 +531,7 @@ bool is_priced(const Call& c) {
 template <bool F32>
 int priced(const Call& c) {
     const Plan plan = price(c);
+    if (plan.splits > 1 && c.env.part_sums == nullptr) return kNeedsSums;
     switch (plan.tile) {
         case Tile::t64x64: return one_tile<F32, Piped64x64>(c, plan.splits);
         case Tile::t64x128: return one_tile<F32, Piped64x128>(c, plan.splits);

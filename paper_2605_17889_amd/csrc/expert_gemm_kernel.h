@@ -32,7 +32,7 @@
 // Operands of 8-bit integers (OperandsI8) run through the same kernels: 16 bytes of a row are a lane's operand of
 // v_mfma_i32_16x16x64_i8 as they are one of v_mfma_f32_16x16x32_bf16, in the same cycles, so a row of K integers is loaded,
 // staged and read as K / 2 units of 16 bits, which is what K, BK and offsets along k count here. The sums are exact
-// (int32, |q| <= 127: up to 133000 products), so they are the same in every tile and order; the epilogue turns them into
+// (int32, |q| <= 128: up to 130944 products), so they are the same in every tile and order; the epilogue turns them into
 // fp32 and multiplies by the row's scale, then by the column's.
 #pragma once
 #include <type_traits>

@@ -187,30 +187,40 @@ int forward_chunk(moe_ctx* c, const moe_bf16* x, const float* w_router, const fl
     });
 }
 
-// Memory of split reductions (products of one matrix), its zeros by a copy of the host's, which has ended when it returns.
-int ensure_sums(moe_ctx* c) {
-    if (c->gemm.split_sums) return MOE_OK;
-    void* p = nullptr;
-    if (hipMalloc(&p, kSplitSumBytes + kPartSums * sizeof(int32_t)) != hipSuccess) {
-        (void)hipGetLastError();
-        return MOE_ERR_WORKSPACE;
-    }
+// Memory of split reductions, its zeros by a copy of the host's, which has ended when it returns. Whether there is such memory
+// then: a stream that is being captured is left alone, and its calls split no reduction.
+bool ensure_sums(moe_ctx* c, hipStream_t s) {
     static const unsigned char zeros[kSplitSumBytes] = {};
+    hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
+    void* p = nullptr;
+    if (hipStreamIsCapturing(s, &capturing) != hipSuccess || capturing != hipStreamCaptureStatusNone ||
+        hipMalloc(&p, kSplitSumBytes + kPartSums * sizeof(int32_t)) != hipSuccess) {
+        (void)hipGetLastError();
+        return false;
+    }
     if (hipMemcpy(p, zeros, sizeof(zeros), hipMemcpyHostToDevice) != hipSuccess) {
         (void)hipGetLastError();
         (void)hipFree(p);
-        return MOE_ERR_HIP;
+        return false;
     }
     c->gemm.split_sums = static_cast<int32_t*>(p);
     c->gemm.part_sums = c->gemm.split_sums + kSplitSumBytes / sizeof(int32_t);
-    return MOE_OK;
+    return true;
+}
+
+int product_i8(moe_ctx* c, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, int N, int K, int E,
+               const moe_i8* W, const float* w_scale, void* out, bool out_f32, hipStream_t s) {
+    auto with = [&](const GemmEnv& env) {
+        return launch_product_i8(env, x, x_scale, offsets, R, N, K, E, W, w_scale, out, out_f32, s);
+    };
+    const int rc = with(c->gemm);
+    if (rc != kNeedsSums) return rc;
+    GemmEnv env = c->gemm;
+    env.whole_reductions = true;
+    return with(ensure_sums(c, s) ? c->gemm : env);
 }
 
 int ensure_i8(moe_ctx* c) {
-    if (c->shape.E == 1) {                           // the down projection is then a product of one matrix
-        const int rc = ensure_sums(c);
-        if (rc != MOE_OK) return rc;
-    }
     if (c->h_i8) return MOE_OK;
     const size_t rows = static_cast<size_t>(c->shape.T_max) * c->shape.k, bytes = align_up(rows * c->shape.d_ff);
     void* p = nullptr;
@@ -254,7 +264,7 @@ int expert_ffn_i8(moe_ctx* c, const moe_i8* x, const float* x_scale, const int32
     return run_stage(c, MOE_STAGE_DOWN, 2, s, [&] {
         const int rc = launch_quantize_i8(c->H, sh.d_ff, R, sh.d_ff, c->h_i8, c->h_scale, s);
         if (rc != MOE_OK) return rc;
-        return launch_product_i8(c->gemm, c->h_i8, c->h_scale, offsets, R, sh.d_model, sh.d_ff, sh.E, w.w2, w.s2, y, y_f32, s);
+        return product_i8(c, c->h_i8, c->h_scale, offsets, R, sh.d_model, sh.d_ff, sh.E, w.w2, w.s2, y, y_f32, s);
     });
 }
 
@@ -738,12 +748,8 @@ int moe_gemm_i8(moe_ctx* c, const moe_i8* x, const float* x_scale, const int32_t
     if (E > kMaxExperts || N % 16 != 0 || N < 32 || N > kMaxDimI8 || K % 128 != 0 || K > kMaxSumI8) return MOE_ERR_UNSUPPORTED_SHAPE;
     if (R == 0) return MOE_OK;
     if (!x || !x_scale || !W || !w_scale || !out || !at_16_bytes(x, W, out)) return MOE_ERR_INVALID_ARG;
-    if (E == 1) {
-        const int rc = ensure_sums(c);
-        if (rc != MOE_OK) return rc;
-    }
-    return launch_product_i8(c->gemm, x, x_scale, offsets, R, N, K, E, W, w_scale, out, out_type == MOE_OUT_FP32,
-                             static_cast<hipStream_t>(stream));
+    return product_i8(c, x, x_scale, offsets, R, N, K, E, W, w_scale, out, out_type == MOE_OUT_FP32,
+                      static_cast<hipStream_t>(stream));
 }
 
 int moe_expert_ffn_i8(moe_ctx* c, const moe_i8* x_perm, const float* x_scale, const int32_t* offsets, int32_t R,

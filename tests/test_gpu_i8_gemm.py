@@ -679,3 +679,36 @@ def test_one_matrix_from_k_steps_in_turn(T, N, K):
 def test_gateup_from_k_steps_in_turn(counts, d, f):
     want = ffn_case(counts, d, f, seed=d)
     assert torch.equal(want, ffn_case(counts, d, f, seed=d, config=0, check=False))
+
+
+@pytest.mark.parametrize("T,N,K", [(3, 512, 8192), (40, 272, 16384)])
+def test_a_first_call_that_is_captured_splits_nothing(T, N, K):
+    """Reductions that an ordinary call would split: recorded by a context's first call, and after one, each replayed with other
+    rows between eager calls, give the same bits."""
+    g = gen(T)
+    x, xs, w, ws = whole(g, T, K), positive(g, T), whole(g, N, K), positive(g, N)
+    ctx, warm = B.MoeContext(T, 512, 128, 1, 1), B.MoeContext(T, 512, 128, 1, 1)
+    out = [torch.empty((T, N), device="cuda") for _ in range(3)]
+
+    def call(c, y, offsets=None):
+        B.moe_gemm_i8(c, x, xs, offsets, T, 1, N, K, w, ws, y)
+
+    call(warm, out[0])                                   # the kernels' first launches, split and not
+    call(warm, out[0], groups([T]))
+    torch.cuda.synchronize()
+    graphs = []
+    for i, c in enumerate((ctx, warm)):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            call(c, out[i])
+    for seed in range(4):
+        x.copy_(whole(gen(seed), T, K))
+        want = product64(x, xs, w, ws)
+        for i, c in enumerate((ctx, warm)):
+            graphs[i].replay()
+            call(c, out[2])
+            torch.cuda.synchronize()
+            assert_near(out[2], want, 0.0)
+            assert torch.equal(out[i], out[2])
+    ctx.close()
+    warm.close()
