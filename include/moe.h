@@ -320,8 +320,9 @@ enum { MOE_RESIDUAL_BF16 = 0, MOE_RESIDUAL_FP32 = 1 };
  *   h = x + residual (x where residual is NULL),   residual_out = h rounded to its type,
  *   v = h * weight / sqrt(mean_i h[i]^2 + eps),    y = v rounded to bf16,
  *   q_scale[t] = max_i |v[t,i]| / 127,             q = v / q_scale[t] to the nearest integer
- * (ties to even: an element that is half the largest one gives 64), -127..127; h, v and the sums are fp32, neither
- * rounding enters the other outputs. A row of zeros has scale 0 and q 0. A row whose v holds a NaN or an infinity has scale
+ * (ties to even: an element that is half the largest one gives 64), -127..127; h, v and the sums are
+ * fp32 (h * weight is formed first and has to stay in range), neither rounding enters the other
+ * outputs. A row of zeros has scale 0 and q 0. A row whose v holds a NaN or an infinity has scale
  * NaN and q 0, so that what is computed from it is NaN, and other rows are what they are.
  * x [T,d] bf16, rows x_stride elements apart (x_stride >= d; x may be part of a wider tensor);
  * residual [T,d] of residual_type (MOE_RESIDUAL_*) or NULL; weight [d] bf16; residual_out [T,d] of
