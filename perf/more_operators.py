@@ -116,12 +116,12 @@ def _randn(gen, *shape):
 
 
 def _arranged(scale):
-    """Scales of blocks [rows, blocks] as the operators hold them: 16 blocks (512 elements) of a row side by side,
-    block 4 * t + g of them at 4 * g + t; 0 behind the last block."""
+    """Scales of blocks [rows, blocks] as the operators hold them: 8 blocks (256 elements) of a row side by side,
+    block 4 * t + g of them at 2 * g + t; 0 behind the last block."""
     rows, blocks = scale.shape
-    whole = torch.zeros((rows, -(-blocks // 16) * 16), dtype=torch.uint8, device=scale.device)
+    whole = torch.zeros((rows, -(-blocks // 8) * 8), dtype=torch.uint8, device=scale.device)
     whole[:, :blocks] = scale
-    return whole.view(rows, -1, 4, 4).permute(1, 0, 3, 2).reshape(-1, rows, 16).contiguous()
+    return whole.view(rows, -1, 2, 4).permute(1, 0, 3, 2).reshape(-1, rows, 8).contiguous()
 
 
 def _packed(rows):
@@ -143,7 +143,7 @@ def _tokens(gen, R, d):
 
 def _matrices(gen, E, N, K):
     q = torch.empty((E, N, K // 2), dtype=torch.uint8, device="cuda")
-    scale = torch.empty((E, -(-K // 512), N, 16), dtype=torch.uint8, device="cuda")
+    scale = torch.empty((E, -(-K // 256), N, 8), dtype=torch.uint8, device="cuda")
     for e in range(E):
         q[e], scale[e] = _packed(_randn(gen, N, K) * 0.02)
     return q, scale
@@ -208,7 +208,7 @@ def prepare(case, seed):
         s["x"] = _tokens(gen, T, d + case["gap"]).to(torch.bfloat16)[:, :d]
         if own:
             s["q"] = torch.empty((T, d // 2), dtype=torch.uint8, device="cuda")
-            s["scale"] = torch.empty((-(-d // 512), T, 16), dtype=torch.uint8, device="cuda")
+            s["scale"] = torch.empty((-(-d // 256), T, 8), dtype=torch.uint8, device="cuda")
             s["y"] = torch.empty((T, d), dtype=torch.bfloat16, device="cuda")
         return s
     if case["op"] == "gemm":
@@ -272,12 +272,12 @@ def _in_4_bits(v):
 
 
 def _numbers(q, scale):
-    """Packed rows [.., rows, K / 2] and arranged scales [.., chunks, rows, 16] as the fp32 numbers they stand for."""
+    """Packed rows [.., rows, K / 2] and arranged scales [.., chunks, rows, 8] as the fp32 numbers they stand for."""
     table = torch.tensor(_VALUES + tuple(-v for v in _VALUES), device=q.device)
     v = table[torch.stack((q & 15, q >> 4), dim=-1).int()].flatten(-2)
     K = v.shape[-1]
     lead = scale.shape[:-3]
-    by_block = scale.view(*lead, *scale.shape[-3:-1], 4, 4).transpose(-1, -2).movedim(-4, -3).reshape(*v.shape[:-1], -1)
+    by_block = scale.view(*lead, *scale.shape[-3:-1], 4, 2).transpose(-1, -2).movedim(-4, -3).reshape(*v.shape[:-1], -1)
     power = by_block[..., :K // 32].to(torch.int32) - 127
     return torch.ldexp(v.view(*v.shape[:-1], -1, 32), power[..., None]).flatten(-2)
 
@@ -363,7 +363,7 @@ def _decoded(q, scale):
     value = torch.where(exponent == 0, fraction / 2, (1 + fraction / 2) * torch.pow(2.0, (exponent - 1).double()))
     value = torch.where(code >= 8, -value, value)
     block = torch.arange(value.shape[1], device=q.device) // 32
-    byte = scale[block // 16, :, 4 * (block % 4) + block % 16 // 4].t()
+    byte = scale[block // 8, :, 2 * (block % 4) + block % 8 // 4].t()
     return value * torch.pow(2.0, byte.double() - 127)
 
 
