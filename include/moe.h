@@ -210,7 +210,7 @@ int moe_last_routing(moe_ctx* ctx, int32_t T, int32_t* topk_idx, float* topk_w, 
 
 /* Per-stage device timing for measurement. moe_profile_begin() arms up to `max_calls`
  * subsequent moe_layer_forward / moe_layer_forward_microbatched / moe_layer_forward_streamed / moe_layer_forward_i8 /
- * moe_expert_ffn / moe_expert_ffn_i8 calls: each records HIP events on the caller's stream between stages (the
+ * moe_layer_forward_mx4 / moe_expert_ffn / moe_expert_ffn_i8 / moe_expert_ffn_mx4 calls: each records HIP events on the caller's stream between stages (the
  * two GEMM stages for moe_expert_ffn). moe_profile_end() waits for those events and
  * writes, per stage, the total milliseconds (stage_ms[MOE_NUM_STAGES], host), the number of
  * kernel launches (stage_launches[MOE_NUM_STAGES], host) and the number of layer calls
@@ -384,6 +384,98 @@ int moe_layer_forward_i8(moe_ctx* ctx, const moe_bf16* x, const moe_i8* x_i8, co
                          const float* w_router, const float* bias, const moe_i8* W1,
                          const float* w1_scale, const moe_i8* W3, const float* w3_scale,
                          const moe_i8* W2, const float* w2_scale, int32_t T, moe_bf16* y, void* stream);
+
+/* ---- routers that score every expert --------------------------------------------------------
+ * What layers with many experts select by: a score for each expert, a correction for balance that takes part in the choice
+ * only, groups of experts of which a token may use the best few. */
+enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
+
+typedef struct {
+    int32_t score;                  /* MOE_SCORE_*: softmax over all E logits, or 1 / (1 + exp(-logit)) */
+    int32_t groups;                 /* equal ranges of experts: group g is experts g*E/groups ..; 1: no groups */
+    int32_t top_groups;             /* groups that a token may use */
+    int32_t group_best;             /* 1: a group is worth its largest c, 2: the sum of its two largest (its one, if it has one) */
+    int32_t renormalise;            /* non-zero: the weights are divided by their sum (0 where that is 0) */
+    float scale;                    /* of the weights */
+} moe_scoring;
+
+/* Router by scores. Logits as for moe_route (x, w_router, bias), then for every token
+ *   s[e] = score of logit e,   c[e] = s[e] + correction[e] (s[e] where correction is NULL),
+ *   the top_groups groups of largest value (ties -> lower group); of their experts
+ *   topk_idx[t,j] = expert with the (j+1)-th largest c (ties -> lower index),
+ *   topk_w[t,j]   = scale * s[idx] / (renormalise ? sum over the k : 1).
+ * All in fp32; a token's results do not depend on T. A NaN logit counts as -infinity; a softmax whose largest logit is
+ * infinite (of either sign) is shared by the logits that equal it; a c (or a group's value) that is NaN counts as -infinity,
+ * and a correction of -infinity leaves its expert to the end. Experts of other groups are never selected.
+ * scoring (HOST): 1 <= groups <= 64 dividing E, 1 <= top_groups <= groups, k <= top_groups * E / groups, group_best 1 or 2, a
+ * finite scale, else MOE_ERR_INVALID_ARG (MOE_ERR_UNSUPPORTED_SHAPE for more than 64 groups). correction [E] fp32 or NULL;
+ * the other arguments as for moe_route. Uses the context's workspace. */
+int moe_route_scored(moe_ctx* ctx, const moe_bf16* x, const float* w_router, const float* bias,
+                     const float* correction, const moe_scoring* scoring, int32_t T, int32_t* topk_idx,
+                     float* topk_w, float* logits_out, void* stream);
+
+/* The same selection and weights from caller-supplied logits [T,E] fp32. */
+int moe_route_scored_from_logits(moe_ctx* ctx, const float* logits, const float* correction,
+                                 const moe_scoring* scoring, int32_t T, int32_t* topk_idx, float* topk_w,
+                                 void* stream);
+
+/* ---- the 4-bit path -----------------------------------------------------------------------
+ * Activations and weights in microscaled 4-bit floating point: blocks of 32 consecutive elements of a row with a power of two
+ * each. An element's 4 bits are a sign (bit 3) and 0, 0.5, 1, 1.5, 2, 3, 4, 6 for 0..7; a block's scale is a byte s, the element
+ * stands for 2^(s - 127) times that, and for NaN where s is 255.
+ *   codes  [rows, K/2] bytes, element 2i in the low half of byte i, element 2i+1 in the high half;
+ *   scales [ceil(K/256), rows, 8] bytes: the 8 blocks of a run of 256 elements side by side for each row, block 4t+g of the run
+ *          (t = 0,1, g = 0..3) at byte 2g+t; bytes of blocks behind the row's last one are 0.
+ * From scales S [rows, K/32] in the order of the blocks (as checkpoints hold them), padded with zeros to a multiple of 8:
+ * S.view(rows, K/256, 2, 4) with its axes permuted to (1, 0, 3, 2). Matrices [E, N, K] have codes [E, N, K/2] and scales
+ * [E, ceil(K/256), N, 8]. */
+typedef uint8_t moe_mx4;            /* two codes */
+typedef uint8_t moe_e8m0;           /* a scale */
+
+/* Rows of bf16 in 4 bits: with 2^m the largest power of two up to the block's largest |element|, its scale is
+ * 2^max(m - 2, -127) and an element is brought to the nearest code of element / scale (ties to the even code), above 6 to 6.
+ * A block of zeros has scale byte 0; a block that holds a NaN or an infinity has scale byte 255 and codes 0. Writes the
+ * scales of blocks behind the row's end too.
+ * x [T,d], rows x_stride >= d elements apart, d a multiple of 32 up to 2^22 (else MOE_ERR_UNSUPPORTED_SHAPE); q [T,d/2];
+ * scale [ceil(d/256),T,8]. Tokens, or one matrix (T = N output channels of d = K). No context. */
+int moe_quantize_mx4(const moe_bf16* x, int64_t x_stride, int32_t T, int32_t d, moe_mx4* q,
+                     moe_e8m0* scale, void* stream);
+
+/* The numbers that such rows stand for, rounded to bf16 (exact from 2^-133 on): y [T,d] out. */
+int moe_dequantize_mx4(const moe_mx4* q, const moe_e8m0* scale, int32_t T, int32_t d, moe_bf16* y,
+                       void* stream);
+
+/* Matrix product of such operands: for offsets[e] <= p < offsets[e+1],
+ *   out[p,n] = sum_k x[p,k] * W[e,n,k]
+ * of the numbers that they stand for, summed in fp32 on the matrix cores (products of normal fp32 size are exact; their order
+ * depends on R, E, N and K) and rounded to out's type. offsets [E+1] int32 (device), or NULL with E == 1: all R rows are one
+ * group. x [R,K/2] with x_scale [ceil(K/256),R,8]; W [E,N,K/2] with w_scale [E,ceil(K/256),N,8]; out [R,N] of out_type
+ * (MOE_OUT_*). x, W and out start at multiples of 16 bytes, the scales at multiples of 8 (else MOE_ERR_INVALID_ARG).
+ * R <= T_max * k of the context, whose d_model, d_ff and E play no part here. E <= 256; K a multiple of 32 up to 2^22; N a
+ * multiple of 16 up to 2^23; else MOE_ERR_UNSUPPORTED_SHAPE. Rows that no group holds are left as they were. */
+int moe_gemm_mx4(moe_ctx* ctx, const moe_mx4* x, const moe_e8m0* x_scale, const int32_t* offsets,
+                 int32_t R, int32_t E, int32_t N, int32_t K, const moe_mx4* W, const moe_e8m0* w_scale,
+                 void* out, int out_type, void* stream);
+
+/* moe_expert_ffn in 4 bits: for offsets[e] <= p < offsets[e+1]
+ *   H[p,:]      = SiLU(g) (.) u in fp32, brought to 4 bits as by moe_quantize_mx4,  g and u the products with W1 and W3,
+ *   y_perm[p,:] = bf16 product of that with W2.
+ * x_perm [R,d_model/2] with x_scale [d_model/256,R,8]; W1, W3 [E,d_ff,d_model/2], W2 [E,d_model,d_ff/2] and their scales as
+ * above; y_perm [R,d_model] bf16 out; R = offsets[E] <= T_max * k; addresses and limits as for moe_gemm_mx4. Needs no memory beyond
+ * the context's. */
+int moe_expert_ffn_mx4(moe_ctx* ctx, const moe_mx4* x_perm, const moe_e8m0* x_scale,
+                       const int32_t* offsets, int32_t R, const moe_mx4* W1, const moe_e8m0* w1_scale,
+                       const moe_mx4* W3, const moe_e8m0* w3_scale, const moe_mx4* W2,
+                       const moe_e8m0* w2_scale, moe_bf16* y_perm, void* stream);
+
+/* moe_layer_forward with its experts in 4 bits: the router reads the tokens x [T,d_model] in bf16, the experts the same tokens
+ * as moe_quantize_mx4 brings them to 4 bits; route -> permute -> rows in 4 bits, grouped -> expert FFN as in
+ * moe_expert_ffn_mx4 -> combine. scoring NULL: the router is moe_route's (correction is NULL then), else moe_route_scored's with
+ * correction [E] or NULL. Weights as above; moe_set_expert_output_fp32 and moe_last_routing as for moe_layer_forward. */
+int moe_layer_forward_mx4(moe_ctx* ctx, const moe_bf16* x, const float* w_router, const float* bias,
+                          const float* correction, const moe_scoring* scoring, const moe_mx4* W1,
+                          const moe_e8m0* w1_scale, const moe_mx4* W3, const moe_e8m0* w3_scale,
+                          const moe_mx4* W2, const moe_e8m0* w2_scale, int32_t T, moe_bf16* y, void* stream);
 
 #ifdef __cplusplus
 }

@@ -25,7 +25,8 @@ EXPORTS = (
     "moe_set_gemm_config", "moe_estimate_expert_stage", "moe_layer_forward_streamed",
     "moe_estimate_streamed_stage", "moe_permute_static", "moe_set_expert_output_fp32",
     "moe_profile_end_per_call", "moe_rmsnorm_i8", "moe_quantize_i8", "moe_gemm_i8", "moe_expert_ffn_i8",
-    "moe_layer_forward_i8",
+    "moe_layer_forward_i8", "moe_route_scored", "moe_route_scored_from_logits", "moe_quantize_mx4", "moe_dequantize_mx4",
+    "moe_gemm_mx4", "moe_expert_ffn_mx4", "moe_layer_forward_mx4",
 )
 
 
@@ -51,15 +52,34 @@ class MoeStreamedEstimate(C.Structure):
                 ("t_sum_s", C.c_double), ("t_overlap_s", C.c_double)]
 
 
-# Argument types of the 8-bit calls: ctypes then converts plain numbers by itself. Host time of a call, with an object for every
+class MoeScoring(C.Structure):
+    """How a router scores, groups and weighs experts (moe_scoring in include/moe.h): score "sigmoid" or "softmax"."""
+    _fields_ = [("score", C.c_int32), ("groups", C.c_int32), ("top_groups", C.c_int32), ("group_best", C.c_int32),
+                ("renormalise", C.c_int32), ("scale", C.c_float)]
+
+    def __init__(self, score: str, groups: int = 1, top_groups: int = 1, group_best: int = 2, renormalise: bool = True,
+                 scale: float = 1.0):
+        if score not in ("softmax", "sigmoid"):
+            raise MoeError(f"score: expected 'softmax' or 'sigmoid', got {score!r}")
+        super().__init__(1 if score == "sigmoid" else 0, groups, top_groups, group_best, int(renormalise), scale)
+
+
+# Argument types of the calls with many arguments: ctypes then converts plain numbers by itself. Host time of a call, with an object for every
 # argument and for the stream -> so: moe_rmsnorm_i8 11.5 -> 7.4 us, moe_gemm_i8 10.3 -> 6.5, moe_expert_ffn_i8 18.5 -> 11.7.
 _P, _I, _L, _F = C.c_void_p, C.c_int32, C.c_int64, C.c_float
-_I8_ARGUMENTS = {
+_ARGUMENTS = {
     "moe_rmsnorm_i8": (_P, _L, _P, _I, _P, _F, _I, _I, _P, _P, _P, _P, _P),
     "moe_quantize_i8": (_P, _L, _I, _I, _P, _P, _P),
     "moe_gemm_i8": (_P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _I, _P),
     "moe_expert_ffn_i8": (_P, _P, _P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _P),
     "moe_layer_forward_i8": (_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _P),
+    "moe_route_scored": (_P, _P, _P, _P, _P, _P, _I, _P, _P, _P, _P),
+    "moe_route_scored_from_logits": (_P, _P, _P, _P, _I, _P, _P, _P),
+    "moe_quantize_mx4": (_P, _L, _I, _I, _P, _P, _P),
+    "moe_dequantize_mx4": (_P, _P, _I, _I, _P, _P),
+    "moe_gemm_mx4": (_P, _P, _P, _P, _I, _I, _I, _I, _P, _P, _P, _I, _P),
+    "moe_expert_ffn_mx4": (_P, _P, _P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _P),
+    "moe_layer_forward_mx4": (_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _P),
 }
 
 
@@ -87,7 +107,7 @@ def lib():
             getattr(L, name).restype = C.c_int
         L.moe_workspace_bytes.restype = C.c_size_t
         L.moe_status_string.restype = C.c_char_p
-        for name, types in _I8_ARGUMENTS.items():
+        for name, types in _ARGUMENTS.items():
             getattr(L, name).argtypes = types
         _lib = L
     return _lib
@@ -422,3 +442,112 @@ def moe_layer_forward_i8(ctx: MoeContext, x, x_i8, x_scale, w_router, bias, W1, 
                                       _addr(bias, torch.float32, (E,), device, "bias"), w1, s1, w3, s3, w2, s2, T,
                                       _addr(y, torch.bfloat16, (T, d), device, "y"), _stream_addr(stream, device)),
            "moe_layer_forward_i8")
+
+
+def _scoring(scoring):
+    if scoring is not None and not isinstance(scoring, MoeScoring):
+        raise MoeError(f"scoring: expected a MoeScoring, got {type(scoring).__name__}")
+    return None if scoring is None else C.addressof(scoring)
+
+
+def moe_route_scored(ctx: MoeContext, x, w_router, bias, correction, scoring, T, topk_idx, topk_w, logits_out=None,
+                     stream=None):
+    """Router by scores: x [T,d] bf16, w_router [d,E] fp32, bias and correction [E] fp32 or None, scoring a MoeScoring ->
+    topk_idx [T,k] int32, topk_w [T,k] fp32 (, logits_out [T,E] fp32)."""
+    d, E, k, device = ctx.d_model, ctx.E, ctx.k, ctx.device
+    _check(lib().moe_route_scored(ctx._h, _addr(x, torch.bfloat16, (T, d), device, "x"),
+                                  _addr(w_router, torch.float32, (d, E), device, "w_router"),
+                                  _addr(bias, torch.float32, (E,), device, "bias"),
+                                  _addr(correction, torch.float32, (E,), device, "correction"), _scoring(scoring), T,
+                                  _addr(topk_idx, torch.int32, (T, k), device, "topk_idx"),
+                                  _addr(topk_w, torch.float32, (T, k), device, "topk_w"),
+                                  _addr(logits_out, torch.float32, (T, E), device, "logits_out"),
+                                  _stream_addr(stream, device)), "moe_route_scored")
+
+
+def moe_route_scored_from_logits(ctx: MoeContext, logits, correction, scoring, T, topk_idx, topk_w, stream=None):
+    """The same from logits [T,E] fp32."""
+    E, k, device = ctx.E, ctx.k, ctx.device
+    _check(lib().moe_route_scored_from_logits(ctx._h, _addr(logits, torch.float32, (T, E), device, "logits"),
+                                              _addr(correction, torch.float32, (E,), device, "correction"),
+                                              _scoring(scoring), T, _addr(topk_idx, torch.int32, (T, k), device, "topk_idx"),
+                                              _addr(topk_w, torch.float32, (T, k), device, "topk_w"),
+                                              _stream_addr(stream, device)), "moe_route_scored_from_logits")
+
+
+def _runs(K: int) -> int:
+    return (K + 255) // 256
+
+
+def moe_quantize_mx4(x, q, scale, stream=None):
+    """x [T,d] bf16 (rows may be strided) -> q [T,d/2] uint8, scale [ceil(d/256),T,8] uint8. One matrix: T = N rows of d = K."""
+    device = torch.cuda.current_device()
+    ptr, stride = _rows_addr(x, device, "x")
+    T, d = x.shape
+    _check(lib().moe_quantize_mx4(ptr, stride, T, d, _addr(q, torch.uint8, (T, d // 2), device, "q"),
+                                  _addr(scale, torch.uint8, (_runs(d), T, 8), device, "scale"), _stream_addr(stream, device)),
+           "moe_quantize_mx4")
+
+
+def moe_dequantize_mx4(q, scale, y, stream=None):
+    """q [T,d/2] uint8, scale [ceil(d/256),T,8] uint8 -> y [T,d] bf16."""
+    device = torch.cuda.current_device()
+    if y is None or y.dim() != 2:
+        raise MoeError("y: expected a 2-D tensor")
+    T, d = y.shape
+    _check(lib().moe_dequantize_mx4(_addr(q, torch.uint8, (T, d // 2), device, "q"),
+                                    _addr(scale, torch.uint8, (_runs(d), T, 8), device, "scale"), T, d,
+                                    _addr(y, torch.bfloat16, (T, d), device, "y"), _stream_addr(stream, device)),
+           "moe_dequantize_mx4")
+
+
+def _matrices_mx4(E: int, N: int, K: int, device: int, W, scale, what: str):
+    """Addresses of matrices [E,N,K] in 4 bits and their scales; of one matrix also without the axis of the experts."""
+    one = E == 1 and W is not None and W.dim() == 2
+    one_scale = E == 1 and scale is not None and scale.dim() == 3
+    return (_addr(W, torch.uint8, (N, K // 2) if one else (E, N, K // 2), device, what),
+            _addr(scale, torch.uint8, (_runs(K), N, 8) if one_scale else (E, _runs(K), N, 8), device, what + "_scale"))
+
+
+def moe_gemm_mx4(ctx: MoeContext, x, x_scale, offsets, R, E, N, K, W, w_scale, out, stream=None):
+    """out[p,n] = sum_k x[p,k] W[e,n,k] for the rows p of expert e; offsets None: one matrix for all rows. x [R,K/2] and
+    W [E,N,K/2] uint8 with scales [ceil(K/256),R,8] and [E,ceil(K/256),N,8], out [R,N] bf16 or fp32."""
+    device = ctx.device
+    w, ws = _matrices_mx4(E, N, K, device, W, w_scale, "W")
+    kind = torch.float32 if out is not None and out.dtype is torch.float32 else torch.bfloat16
+    _check(lib().moe_gemm_mx4(ctx._h, _addr(x, torch.uint8, (R, K // 2), device, "x"),
+                              _addr(x_scale, torch.uint8, (_runs(K), R, 8), device, "x_scale"),
+                              _addr(offsets, torch.int32, (E + 1,), device, "offsets"), R, E, N, K, w, ws,
+                              _addr(out, kind, (R, N), device, "out"), 1 if kind is torch.float32 else 0,
+                              _stream_addr(stream, device)), "moe_gemm_mx4")
+
+
+def moe_expert_ffn_mx4(ctx: MoeContext, x_perm, x_scale, offsets, R, W1, w1_scale, W3, w3_scale, W2, w2_scale, y_perm,
+                       stream=None):
+    """moe_expert_ffn over rows and weights in 4 bits: x_perm [R,d/2], W1, W3 [E,f,d/2] and W2 [E,d,f/2] uint8 with their
+    scales, y_perm [R,d] bf16."""
+    d, f, E, device = ctx.d_model, ctx.d_ff, ctx.E, ctx.device
+    w1, s1 = _matrices_mx4(E, f, d, device, W1, w1_scale, "W1")
+    w3, s3 = _matrices_mx4(E, f, d, device, W3, w3_scale, "W3")
+    w2, s2 = _matrices_mx4(E, d, f, device, W2, w2_scale, "W2")
+    _check(lib().moe_expert_ffn_mx4(ctx._h, _addr(x_perm, torch.uint8, (R, d // 2), device, "x_perm"),
+                                    _addr(x_scale, torch.uint8, (_runs(d), R, 8), device, "x_scale"),
+                                    _addr(offsets, torch.int32, (E + 1,), device, "offsets"), R, w1, s1, w3, s3, w2, s2,
+                                    _addr(y_perm, torch.bfloat16, (R, d), device, "y_perm"), _stream_addr(stream, device)),
+           "moe_expert_ffn_mx4")
+
+
+def moe_layer_forward_mx4(ctx: MoeContext, x, w_router, bias, correction, scoring, W1, w1_scale, W3, w3_scale, W2, w2_scale,
+                          T, y, stream=None):
+    """moe_layer_forward with experts in 4 bits: x, y [T,d] bf16, scoring a MoeScoring (or None: moe_route's router, without
+    a correction), weights as for moe_expert_ffn_mx4."""
+    d, f, E, device = ctx.d_model, ctx.d_ff, ctx.E, ctx.device
+    w1, s1 = _matrices_mx4(E, f, d, device, W1, w1_scale, "W1")
+    w3, s3 = _matrices_mx4(E, f, d, device, W3, w3_scale, "W3")
+    w2, s2 = _matrices_mx4(E, d, f, device, W2, w2_scale, "W2")
+    _check(lib().moe_layer_forward_mx4(ctx._h, _addr(x, torch.bfloat16, (T, d), device, "x"),
+                                       _addr(w_router, torch.float32, (d, E), device, "w_router"),
+                                       _addr(bias, torch.float32, (E,), device, "bias"),
+                                       _addr(correction, torch.float32, (E,), device, "correction"), _scoring(scoring),
+                                       w1, s1, w3, s3, w2, s2, T, _addr(y, torch.bfloat16, (T, d), device, "y"),
+                                       _stream_addr(stream, device)), "moe_layer_forward_mx4")

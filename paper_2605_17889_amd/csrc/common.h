@@ -12,6 +12,8 @@ constexpr int kMaxExperts = 256; // four experts per lane in the permutation and
 constexpr int kMaxRowI8 = 65536; // a row in the registers of a workgroup (norm.hip)
 constexpr int kMaxSumI8 = 130944; // products of -128 .. 127 whose sum stays below 2^31, a multiple of 128
 constexpr int kMaxDimI8 = 1 << 23; // widths of outputs, for 32-bit offsets inside a tile
+constexpr int kMaxDimMx4 = 1 << 22; // lengths of rows in 4 bits: 256 rows of a tile stay below 2^30 bytes
+constexpr int kMaxGroups = 64;   // of experts: a lane each
 constexpr int kXcds = 8;         // workgroups are dealt round-robin to the 8 XCDs (own L2 each)
 
 __device__ __forceinline__ float bf16_to_f32(uint16_t b) {
@@ -118,5 +120,20 @@ int launch_down_converting_i8(const GemmEnv& env, const moe_bf16* H, const int32
 constexpr int kNeedsSums = 1;
 int launch_product_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, int N, int K,
                       int E, const moe_i8* W, const float* w_scale, void* out, bool out_f32, hipStream_t s);
+// Scores, groups and weights from logits; sc is checked.
+int launch_route_scored(const float* logits, const float* correction, const moe_scoring& sc, int T, int E, int k,
+                        int32_t* topk_idx, float* topk_w, hipStream_t s);
+// Rows in microscaled 4-bit floating point (mx4.h), d a multiple of 32.
+int launch_quantize_mx4(const moe_bf16* x, long long x_stride, int T, int d, moe_mx4* q, moe_e8m0* scale, hipStream_t s);
+// Token rows to their k places in the rows grouped by expert.
+int launch_quantize_grouped_mx4(const moe_bf16* x, const int32_t* inv_perm, int T, int d, int k, moe_mx4* q, moe_e8m0* scale,
+                                hipStream_t s);
+int launch_dequantize_mx4(const moe_mx4* q, const moe_e8m0* scale, int T, int d, moe_bf16* y, hipStream_t s);
+// Products of such rows (expert_gemm_mx4.hip). Without offsets they are one group. H's scales have a pitch of R rows.
+int launch_gateup_mx4(const GemmEnv& env, const moe_mx4* x, const moe_e8m0* x_scale, const int32_t* offsets, int R, int d, int f,
+                      int E, const moe_mx4* W1, const moe_e8m0* w1_scale, const moe_mx4* W3, const moe_e8m0* w3_scale,
+                      moe_mx4* H, moe_e8m0* h_scale, hipStream_t s);
+int launch_product_mx4(const GemmEnv& env, const moe_mx4* x, const moe_e8m0* x_scale, const int32_t* offsets, int R, int N,
+                       int K, int E, const moe_mx4* W, const moe_e8m0* w_scale, void* out, bool out_f32, hipStream_t s);
 
 }  // namespace moe

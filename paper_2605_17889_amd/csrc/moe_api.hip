@@ -268,6 +268,54 @@ int expert_ffn_i8(moe_ctx* c, const moe_i8* x, const float* x_scale, const int32
     });
 }
 
+int scoring_status(const moe_scoring* sc, const moe_shape& sh) {
+    if (!sc || (sc->score != MOE_SCORE_SOFTMAX && sc->score != MOE_SCORE_SIGMOID)) return MOE_ERR_INVALID_ARG;
+    if (sc->groups < 1 || sh.E % sc->groups != 0 || sc->top_groups < 1 || sc->top_groups > sc->groups) return MOE_ERR_INVALID_ARG;
+    if (sc->group_best != 1 && sc->group_best != 2) return MOE_ERR_INVALID_ARG;
+    if (sh.k > sc->top_groups * (sh.E / sc->groups) || !std::isfinite(sc->scale)) return MOE_ERR_INVALID_ARG;
+    return sc->groups > kMaxGroups ? MOE_ERR_UNSUPPORTED_SHAPE : MOE_OK;
+}
+
+// Logits, then the selection by scores. Without a caller's tensor the logits lie in the context's own or, where it has none (up to
+// 16 experts), in y_perm's memory, which a layer call fills later: 1 KB and more for each token.
+int route_scored(moe_ctx* c, const moe_bf16* x, const float* w_router, const float* bias, const float* correction,
+                 const moe_scoring& scoring, int T, int32_t* topk_idx, float* topk_w, float* logits_out, hipStream_t s) {
+    const moe_shape& sh = c->shape;
+    float* logits = logits_out ? logits_out : c->logits ? c->logits : reinterpret_cast<float*>(c->y_perm);
+    const int rc = sh.E > 16 ? launch_route_logits(x, w_router, bias, T, sh.d_model, sh.E, logits, s)
+                             : launch_route(x, w_router, bias, T, sh.d_model, sh.E, sh.k, topk_idx, topk_w, logits, nullptr, s);
+    if (rc != MOE_OK) return rc;
+    return launch_route_scored(logits, correction, scoring, T, sh.E, sh.k, topk_idx, topk_w, s);
+}
+
+template <class... Ptr>
+bool at_8_bytes(Ptr... p) {
+    return ((reinterpret_cast<uintptr_t>(p) | ...) & 7) == 0;
+}
+
+struct ExpertsMx4 {
+    const moe_mx4 *w1, *w3, *w2;
+    const moe_e8m0 *s1, *s3, *s2;
+    bool complete() const { return w1 && w3 && w2 && s1 && s3 && s2; }
+    bool aligned() const { return at_16_bytes(w1, w3, w2) && at_8_bytes(s1, s3, s2); }
+};
+
+// Expert FFN over grouped rows in 4 bits. H's codes and scales lie in the memory of the bf16 H, of which they take little more than
+// a quarter (a row of 128 elements and more: d_ff / 2 and up to d_ff / 16 bytes of 2 d_ff).
+int expert_ffn_mx4(moe_ctx* c, const moe_mx4* x, const moe_e8m0* x_scale, const int32_t* offsets, int R, const ExpertsMx4& w,
+                   void* y, bool y_f32, hipStream_t s) {
+    const moe_shape& sh = c->shape;
+    moe_mx4* H = reinterpret_cast<moe_mx4*>(c->H);
+    moe_e8m0* h_scale = H + static_cast<size_t>(R) * (sh.d_ff / 2);
+    const int rc = run_stage(c, MOE_STAGE_GATEUP, 1, s, [&] {
+        return launch_gateup_mx4(c->gemm, x, x_scale, offsets, R, sh.d_model, sh.d_ff, sh.E, w.w1, w.s1, w.w3, w.s3, H, h_scale, s);
+    });
+    if (rc != MOE_OK) return rc;
+    return run_stage(c, MOE_STAGE_DOWN, 1, s, [&] {
+        return launch_product_mx4(c->gemm, H, h_scale, offsets, R, sh.d_model, sh.d_ff, sh.E, w.w2, w.s2, y, y_f32, s);
+    });
+}
+
 int ensure_streaming(moe_ctx* c) {
     if (c->copy_stream) return MOE_OK;
     const size_t bytes = static_cast<size_t>(3) * c->shape.d_model * c->shape.d_ff * sizeof(moe_bf16);
@@ -794,6 +842,117 @@ int moe_layer_forward_i8(moe_ctx* c, const moe_bf16* x, const moe_i8* x_i8, cons
     });
     if (rc != MOE_OK) return rc;
     rc = expert_ffn_i8(c, grouped, c->x_scale, c->offsets, R, w, expert_out(c), c->y_perm_f32 != nullptr, s);
+    if (rc != MOE_OK) return rc;
+    return run_stage(c, MOE_STAGE_COMBINE, 1, s, [&] {
+        return launch_combine(expert_out(c), c->y_perm_f32 != nullptr, c->inv_perm, c->topk_w, T, sh.d_model, sh.k, y, s);
+    });
+}
+
+// ---- routers that score every expert ----
+int moe_route_scored(moe_ctx* c, const moe_bf16* x, const float* w_router, const float* bias, const float* correction,
+                     const moe_scoring* scoring, int32_t T, int32_t* topk_idx, float* topk_w, float* logits_out, void* stream) {
+    if (!c || T < 0 || T > c->shape.T_max) return MOE_ERR_INVALID_ARG;
+    if (!on_own_device(c)) return MOE_ERR_INVALID_ARG;
+    const int rc = scoring_status(scoring, c->shape);
+    if (rc != MOE_OK || T == 0) return rc;
+    if (!x || !w_router || !topk_idx || !topk_w) return MOE_ERR_INVALID_ARG;
+    return route_scored(c, x, w_router, bias, correction, *scoring, T, topk_idx, topk_w, logits_out,
+                        static_cast<hipStream_t>(stream));
+}
+
+int moe_route_scored_from_logits(moe_ctx* c, const float* logits, const float* correction, const moe_scoring* scoring, int32_t T,
+                                 int32_t* topk_idx, float* topk_w, void* stream) {
+    if (!c || T < 0 || T > c->shape.T_max) return MOE_ERR_INVALID_ARG;
+    if (!on_own_device(c)) return MOE_ERR_INVALID_ARG;
+    const int rc = scoring_status(scoring, c->shape);
+    if (rc != MOE_OK || T == 0) return rc;
+    if (!logits || !topk_idx || !topk_w) return MOE_ERR_INVALID_ARG;
+    return launch_route_scored(logits, correction, *scoring, T, c->shape.E, c->shape.k, topk_idx, topk_w,
+                               static_cast<hipStream_t>(stream));
+}
+
+// ---- the 4-bit path ----
+int moe_quantize_mx4(const moe_bf16* x, int64_t x_stride, int32_t T, int32_t d, moe_mx4* q, moe_e8m0* scale, void* stream) {
+    if (T < 0 || d < 1 || x_stride < d) return MOE_ERR_INVALID_ARG;
+    if (d % 32 != 0 || d > kMaxDimMx4) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (T == 0) return MOE_OK;
+    if (!x || !q || !scale) return MOE_ERR_INVALID_ARG;
+    return launch_quantize_mx4(x, x_stride, T, d, q, scale, static_cast<hipStream_t>(stream));
+}
+
+int moe_dequantize_mx4(const moe_mx4* q, const moe_e8m0* scale, int32_t T, int32_t d, moe_bf16* y, void* stream) {
+    if (T < 0 || d < 1) return MOE_ERR_INVALID_ARG;
+    if (d % 32 != 0 || d > kMaxDimMx4) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (T == 0) return MOE_OK;
+    if (!q || !scale || !y) return MOE_ERR_INVALID_ARG;
+    return launch_dequantize_mx4(q, scale, T, d, y, static_cast<hipStream_t>(stream));
+}
+
+int moe_gemm_mx4(moe_ctx* c, const moe_mx4* x, const moe_e8m0* x_scale, const int32_t* offsets, int32_t R, int32_t E, int32_t N,
+                 int32_t K, const moe_mx4* W, const moe_e8m0* w_scale, void* out, int out_type, void* stream) {
+    if (!c || R < 0 || static_cast<long long>(R) > static_cast<long long>(c->shape.T_max) * c->shape.k)
+        return MOE_ERR_INVALID_ARG;
+    if (!on_own_device(c) || E < 1 || N < 1 || K < 1 || (!offsets && E != 1)) return MOE_ERR_INVALID_ARG;
+    if (out_type != MOE_OUT_BF16 && out_type != MOE_OUT_FP32) return MOE_ERR_INVALID_ARG;
+    if (E > kMaxExperts || N % 16 != 0 || N > kMaxDimI8 || K % 32 != 0 || K > kMaxDimMx4) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (R == 0) return MOE_OK;
+    if (!x || !x_scale || !W || !w_scale || !out) return MOE_ERR_INVALID_ARG;
+    if (!at_16_bytes(x, W, out) || !at_8_bytes(x_scale, w_scale)) return MOE_ERR_INVALID_ARG;
+    return launch_product_mx4(c->gemm, x, x_scale, offsets, R, N, K, E, W, w_scale, out, out_type == MOE_OUT_FP32,
+                              static_cast<hipStream_t>(stream));
+}
+
+int moe_expert_ffn_mx4(moe_ctx* c, const moe_mx4* x_perm, const moe_e8m0* x_scale, const int32_t* offsets, int32_t R,
+                       const moe_mx4* W1, const moe_e8m0* w1_scale, const moe_mx4* W3, const moe_e8m0* w3_scale,
+                       const moe_mx4* W2, const moe_e8m0* w2_scale, moe_bf16* y_perm, void* stream) {
+    if (!c || R < 0 || static_cast<long long>(R) > static_cast<long long>(c->shape.T_max) * c->shape.k)
+        return MOE_ERR_INVALID_ARG;
+    if (!on_own_device(c)) return MOE_ERR_INVALID_ARG;
+    if (c->shape.d_model > kMaxDimMx4 || c->shape.d_ff > kMaxDimMx4) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (R == 0) return MOE_OK;
+    const ExpertsMx4 w{W1, W3, W2, w1_scale, w3_scale, w2_scale};
+    if (!x_perm || !x_scale || !offsets || !w.complete() || !y_perm) return MOE_ERR_INVALID_ARG;
+    if (!at_16_bytes(x_perm, y_perm) || !at_8_bytes(x_scale) || !w.aligned()) return MOE_ERR_INVALID_ARG;
+    if (c->prof_armed) ++c->prof_calls;
+    return expert_ffn_mx4(c, x_perm, x_scale, offsets, R, w, y_perm, false, static_cast<hipStream_t>(stream));
+}
+
+int moe_layer_forward_mx4(moe_ctx* c, const moe_bf16* x, const float* w_router, const float* bias, const float* correction,
+                          const moe_scoring* scoring, const moe_mx4* W1, const moe_e8m0* w1_scale, const moe_mx4* W3,
+                          const moe_e8m0* w3_scale, const moe_mx4* W2, const moe_e8m0* w2_scale, int32_t T, moe_bf16* y,
+                          void* stream) {
+    if (!c || T < 0 || T > c->shape.T_max) return MOE_ERR_INVALID_ARG;
+    if (!on_own_device(c)) return MOE_ERR_INVALID_ARG;
+    const moe_shape& sh = c->shape;
+    int rc = scoring ? scoring_status(scoring, sh) : correction ? MOE_ERR_INVALID_ARG : MOE_OK;
+    if (rc != MOE_OK) return rc;
+    if (sh.d_model > kMaxDimMx4 || sh.d_ff > kMaxDimMx4) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (T == 0) return MOE_OK;
+    const ExpertsMx4 w{W1, W3, W2, w1_scale, w3_scale, w2_scale};
+    if (!x || !w_router || !w.complete() || !y || !w.aligned()) return MOE_ERR_INVALID_ARG;
+    if (c->prof_armed) ++c->prof_calls;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int R = T * sh.k;
+    if (scoring == nullptr) {
+        rc = route_and_permute(c, x, w_router, bias, T, s);
+    } else {
+        rc = run_stage(c, MOE_STAGE_ROUTE, sh.E > 16 ? 2 : route_launches(sh.E) + 1, s, [&] {
+            return route_scored(c, x, w_router, bias, correction, *scoring, T, c->topk_idx, c->topk_w, nullptr, s);
+        });
+        if (rc != MOE_OK) return rc;
+        rc = run_stage(c, MOE_STAGE_PERMUTE, permute_launches(R), s, [&] {
+            return launch_permute(c->topk_idx, R, sh.E, c->counts, c->offsets, c->perm, c->inv_perm, c->scratch, s);
+        });
+    }
+    if (rc != MOE_OK) return rc;
+    // grouped rows in the memory of x_perm, a quarter of it and a bit: codes, then scales
+    moe_mx4* grouped = reinterpret_cast<moe_mx4*>(c->x_perm);
+    moe_e8m0* grouped_scale = grouped + static_cast<size_t>(R) * (sh.d_model / 2);
+    rc = run_stage(c, MOE_STAGE_GATHER, 1, s, [&] {
+        return launch_quantize_grouped_mx4(x, c->inv_perm, T, sh.d_model, sh.k, grouped, grouped_scale, s);
+    });
+    if (rc != MOE_OK) return rc;
+    rc = expert_ffn_mx4(c, grouped, grouped_scale, c->offsets, R, w, expert_out(c), c->y_perm_f32 != nullptr, s);
     if (rc != MOE_OK) return rc;
     return run_stage(c, MOE_STAGE_COMBINE, 1, s, [&] {
         return launch_combine(expert_out(c), c->y_perm_f32 != nullptr, c->inv_perm, c->topk_w, T, sh.d_model, sh.k, y, s);
