@@ -128,9 +128,9 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_rows_kernel(Operands op
 // Upper bound on the number of row tiles of E groups with R rows in all.
 long long most_row_tiles(int R, int E, int BM) { return R / BM + std::min(E, R); }
 
-template <class Kernel>
+template <class Kernel, class... Args>
 int launch(const GemmEnv& env, std::atomic<uint64_t>& attr_set, Kernel kern, int smem, int threads, long long grid,
-           const Operands& op, const Outputs& out, hipStream_t s) {
+           hipStream_t s, Args... args) {
     if (env.device < 0 || env.device >= 64) return MOE_ERR_INVALID_ARG;
     const uint64_t bit = 1ull << env.device;         // the attribute belongs to the kernel on one device
     if (smem > 0 && !(attr_set.load(std::memory_order_acquire) & bit)) {
@@ -140,7 +140,7 @@ int launch(const GemmEnv& env, std::atomic<uint64_t>& attr_set, Kernel kern, int
     }
     grid = (grid + kXcds - 1) / kXcds * kXcds;       // every XCD's range of tiles is as long
     if (grid > 0x7fffffffLL) return MOE_ERR_UNSUPPORTED_SHAPE;
-    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid)), dim3(threads), smem, s, op, out);
+    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid)), dim3(threads), smem, s, args...);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
@@ -148,14 +148,34 @@ template <class Cfg>
 int ring(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
     static std::atomic<uint64_t> attr_set{0};
     return launch(env, attr_set, mx4::ring_kernel<Cfg>, Cfg::SMEM, Cfg::NTHREADS,
-                  most_row_tiles(op.R, op.E, Cfg::BM) * ((op.N + Cfg::BN_OUT - 1) / Cfg::BN_OUT), op, out, s);
+                  most_row_tiles(op.R, op.E, Cfg::BM) * ((op.N + Cfg::BN_OUT - 1) / Cfg::BN_OUT), s, op, out);
+}
+
+using GateUpLarge = mx4::Mx4<gemm::Config<256, 256, 64, 2, 2, 2, true>>;
+template <bool F32>
+using PlainLarge = mx4::Mx4<std::conditional_t<F32, gemm::F32Out<gemm::Config<256, 256, 64, 2, 2, 2, false>>,
+                                               gemm::Config<256, 256, 64, 2, 2, 2, false>>>;
+template <class Cfg, bool ODD>
+int large_of(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
+    static std::atomic<uint64_t> attr_set{0};
+    const int cus = compute_units(env.device);
+    // tiles, and the halves that the last round's are cut into
+    const long long grid = most_row_tiles(op.R, op.E, 256) * gemm::n_tiles<Cfg>(op.N) + kXcds * ((cus / 2 + kXcds - 1) / kXcds + 1);
+    return launch(env, attr_set, mx4::large_kernel<Cfg, ODD>, mx4::Large<Cfg>::SMEM, 256, grid, s, op, out, cus);
+}
+template <class Cfg>
+bool large_fits(const Operands& op) { return op.K > 512 && op.N >= Cfg::BN_OUT; }
+template <class Cfg>
+int large(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
+    if (!large_fits<Cfg>(op)) return MOE_ERR_UNSUPPORTED_SHAPE;
+    return mx_runs(op.K) & 1 ? large_of<Cfg, true>(env, op, out, s) : large_of<Cfg, false>(env, op, out, s);
 }
 
 template <bool DUAL, bool F32>
 int few_rows(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
     static std::atomic<uint64_t> attr_set{0};
     return launch(env, attr_set, few_rows_kernel<DUAL, F32>, 0, kFewWaves * kWave,
-                  most_row_tiles(op.R, op.E, kFewRows) * (op.N / (DUAL ? 32 : 16)), op, out, s);
+                  most_row_tiles(op.R, op.E, kFewRows) * (op.N / (DUAL ? 32 : 16)), s, op, out);
 }
 
 // Rows of a group: the average and two standard deviations of a uniform routing.
@@ -169,7 +189,8 @@ int product(const GemmEnv& env, const Operands& op, const Outputs& out, hipStrea
     const double rows = upper_rows(op.R, op.E);
     if (rows <= 16.0) return few_rows<false, F32>(env, op, out, s);
     if (rows <= 64.0) return ring<Plain32<F32>>(env, op, out, s);
-    return ring<Plain128<F32>>(env, op, out, s);
+    if (rows <= 128.0 || !large_fits<PlainLarge<F32>>(op)) return ring<Plain128<F32>>(env, op, out, s);
+    return large<PlainLarge<F32>>(env, op, out, s);
 }
 
 }  // namespace
@@ -182,7 +203,8 @@ int launch_gateup_mx4(const GemmEnv& env, const moe_mx4* x, const moe_e8m0* x_sc
     const double rows = upper_rows(R, E);
     if (rows <= 16.0) return few_rows<true, false>(env, op, out, s);
     if (rows <= 64.0) return ring<GateUp32>(env, op, out, s);
-    return ring<GateUp128>(env, op, out, s);
+    if (rows <= 128.0 || !large_fits<GateUpLarge>(op)) return ring<GateUp128>(env, op, out, s);
+    return large<GateUpLarge>(env, op, out, s);
 }
 
 int launch_product_mx4(const GemmEnv& env, const moe_mx4* x, const moe_e8m0* x_scale, const int32_t* offsets, int R, int N,

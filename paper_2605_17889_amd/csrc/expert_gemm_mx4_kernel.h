@@ -55,18 +55,19 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const void* base, uin
 }
 
 // Direct-to-LDS loads through a resource: 64 lanes x 16 (or 4) bytes land contiguously at LDS byte offset lds_off. The
-// kernels place their own waits (see dma16 in expert_gemm_kernel.h).
+// kernels place their own waits (see dma16 in expert_gemm_kernel.h). A scalar register that the vector unit has written may be
+// read by a vector memory instruction five instructions later; the compiler does not see that this is one.
 template <bool STREAM = false>
 __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t from, uint32_t voff, uint32_t soff, uint32_t lds_off) {
     if constexpr (STREAM)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds"
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds"
                      :: "s"(lds_off), "v"(voff), "s"(from), "s"(soff) : "memory", "m0");
     else
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                      :: "s"(lds_off), "v"(voff), "s"(from), "s"(soff) : "memory", "m0");
 }
 __device__ __forceinline__ void dma4(__amdgpu_buffer_rsrc_t from, uint32_t voff, uint32_t lds_off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
                  :: "s"(lds_off), "v"(voff), "s"(from) : "memory", "m0");
 }
 
@@ -298,5 +299,342 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void ring_kernel(Operands op, Output
     store_tile<Cfg>(acc, op, tc, out, wm, wn, frag_row, g);
 }
 
+// ---- large tiles: one wavefront per SIMD, hand-placed pipeline -------------------------------------------------------------
+// 256 x 256 outputs, 128 x 128 to a wavefront, as grouped_gemm_1w_kernel has them (expert_gemm_kernel.h): two half-steps of one
+// instruction of 128 elements each, every LDS read, direct-to-LDS load and scalar update behind an MFMA of its own, the barrier
+// of a k-step between its halves. LDS does not hold that kernel's five stages of 32 KB and the scales, so the B ring holds two and a
+// half: five halves of 128 rows, of which k-step kt has numbers 2 kt and 2 kt + 1 modulo 5. In the first half of k-step kt go out
+// the loads of the first B half of kt + 2, into the place that has been idle since the barrier of kt - 1, and its scales (a
+// ring of four k-steps), in the second half the loads of its A rows and second B half, into the places that the barrier of kt
+// has freed: at that barrier only the first half's loads may still be on their way. The scales of k-step kt + 1 are read from
+// LDS in the second half of kt, 16 bits for each fragment's row and lane group: one byte for each half-step.
+// Loads go through resources that advance by a k-step at a time and end where the tile's rows do; those of k-steps that there
+// are not are empty: the loads then bring zeros and read nothing, and every k-step runs the same code.
+template <class Cfg>
+struct Mx4 : Cfg {
+    static constexpr bool ANY_WIDTH = true;
+};
+template <class Cfg>
+struct Large {
+    static constexpr uint32_t AB = 256 * 128, HB = 128 * 128, A_RING = 2 * AB, B_RING = 5 * HB, SCALES = A_RING + B_RING;
+    static constexpr uint32_t SA = 256 * 8, SS = 2 * SA, SMEM = SCALES + 4 * SS;      // a k-step's scales: of A, then of B
+    static_assert(SMEM <= 160 * 1024 && Cfg::BM == 256 && Cfg::BN == 256 && Cfg::NW == 4, "256 x 256");
+};
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// A resource in four scalar registers: address, bytes, format.
+__device__ __forceinline__ u32x4 resource_words(const void* base, uint32_t bytes) {
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    return u32x4{static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at))),
+                 static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(at >> 32))),
+                 static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(bytes)), 0x00027000u};
+}
+__device__ __forceinline__ void advance(u32x4& r, uint64_t by) {
+    const uint64_t at = (r[0] | static_cast<uint64_t>(r[1]) << 32) + by;
+    r[0] = static_cast<uint32_t>(at);
+    r[1] = static_cast<uint32_t>(at >> 32);
+}
+template <int BYTES>
+__device__ __forceinline__ void dma(const u32x4& from, uint32_t voff, uint32_t lds_off) {
+    if constexpr (BYTES == 16)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     :: "s"(lds_off), "v"(voff), "s"(from) : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                     :: "s"(lds_off), "v"(voff), "s"(from) : "memory", "m0");
+}
+
+// acc += W_frag * X_frag with the accumulator pinned to AGPRs (see mma16_agpr), and the same with one direct-to-LDS load behind
+// it, whose LDS address goes to M0 in front.
+template <int H>
+__device__ __forceinline__ void mma_agpr(const i32x4& w, const i32x4& x, f32x4& acc, int ws, int xs) {
+    if constexpr (H == 0)
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4"
+                     : "+a"(acc) : "v"(w), "v"(x), "v"(ws), "v"(xs));
+    else
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4"
+                     : "+a"(acc) : "v"(w), "v"(x), "v"(ws), "v"(xs));
+}
+template <int H, int BYTES, int LDS_OFF>
+__device__ __forceinline__ void mma_then_dma(const i32x4& w, const i32x4& x, f32x4& acc, int ws, int xs, uint32_t lds_base,
+                                             uint32_t voff, const u32x4& from) {
+#define MOE_MX4_STEP(SEL, LOAD)                                                                                        \
+    asm volatile("s_add_u32 m0, %5, %6\n\t"                                                                            \
+                 "v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:" SEL " op_sel_hi:[0,0,0] cbsz:4 blgp:4\n\t" \
+                 LOAD " %7, %8, 0 offen lds"                                                                           \
+                 : "+a"(acc)                                                                                           \
+                 : "v"(w), "v"(x), "v"(ws), "v"(xs), "s"(lds_base), "n"(LDS_OFF), "v"(voff), "s"(from)                 \
+                 : "memory", "m0", "scc")
+    if constexpr (H == 0 && BYTES == 16) MOE_MX4_STEP("[0,0,0]", "buffer_load_dwordx4");
+    else if constexpr (H == 0) MOE_MX4_STEP("[0,0,0]", "buffer_load_dword");
+    else if constexpr (BYTES == 16) MOE_MX4_STEP("[1,1,0]", "buffer_load_dwordx4");
+    else MOE_MX4_STEP("[1,1,0]", "buffer_load_dword");
+#undef MOE_MX4_STEP
+}
+
+// Loads of a tile: A load i of wavefront w is tile rows 8 (4 i + w) .. + 7, so that the first TM loads of all wavefronts are the
+// rows of a tile of TM * 32 rows; B load i of half b is B-tile rows 128 b + 32 w + 8 i .. + 7 (with DUAL 32 rows of one matrix).
+template <class Cfg>
+struct LargeLoads {
+    u32x4 a, b, sa, sb[Cfg::DUAL ? 2 : 1];
+    uint32_t a_voff[8], b_voff[8], sa_voff, sb_voff;           // of the first scale loads; the second ones are 256 bytes on
+    uint64_t sa_step, sb_step;
+    int left;                                                  // k-steps from the one whose loads are next to the last
+    __device__ __forceinline__ void init(const Operands& op, const TileCoord& tc, int wave, int lane) {
+        const uint32_t pitch = static_cast<uint32_t>(op.K) / 2;
+        const int col0 = gemm::first_column<Cfg>(tc, op.N);
+        const size_t first = static_cast<size_t>(tc.expert) * op.N + col0;
+        const size_t first_scale = (static_cast<size_t>(tc.expert) * mx_runs(op.K) * op.N + col0) * kMxRunBytes;
+        left = mx_runs(op.K);
+        a = resource_words(op.a + static_cast<size_t>(tc.row0) * pitch, tc.rows * pitch);
+        b = resource_words((Cfg::DUAL && (wave & 1) ? op.b[1] : op.b[0]) + first * pitch, Cfg::BN_OUT * pitch);
+        sa = resource_words(op.a_scale + static_cast<size_t>(tc.row0) * kMxRunBytes, tc.rows * kMxRunBytes);
+#pragma unroll
+        for (int m = 0; m < (Cfg::DUAL ? 2 : 1); ++m) sb[m] = resource_words(op.b_scale[m] + first_scale, Cfg::BN_OUT * kMxRunBytes);
+        sa_step = static_cast<uint64_t>(op.R) * kMxRunBytes;
+        sb_step = static_cast<uint64_t>(op.N) * kMxRunBytes;
+        const int lrow = lane >> 3;
+        const uint32_t achunk = ((lane & 7) ^ gemm::swz<64>(8 * wave + lrow)) * 16;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            a_voff[i] = (8 * (4 * i + wave) + lrow) * pitch + achunk;
+            const int row = 128 * (i >> 2) + 32 * wave + 8 * (i & 3) + lrow;
+            b_voff[i] = (Cfg::DUAL ? row / 64 * 32 + row % 32 : row) * pitch + ((lane & 7) ^ gemm::swz<64>(row)) * 16;
+        }
+        sa_voff = wave * 512 + lane * 4;
+        sb_voff = (Cfg::DUAL ? wave * 256 : wave * 512) + lane * 4;
+    }
+    // to the next k-step; the resources of one that there is not are empty
+    __device__ __forceinline__ void next_scales() {
+        advance(sa, sa_step);
+        sa[2] = left > 1 ? sa[2] : 0u;
+#pragma unroll
+        for (int m = 0; m < (Cfg::DUAL ? 2 : 1); ++m) {
+            advance(sb[m], sb_step);
+            sb[m][2] = left > 1 ? sb[m][2] : 0u;
+        }
+    }
+    __device__ __forceinline__ void next_rows() {
+        advance(a, 128);
+        a[2] = left > 1 ? a[2] - 128u : 0u;
+        advance(b, 128);
+        b[2] = left > 1 ? b[2] - 128u : 0u;
+        --left;
+    }
+    __device__ __forceinline__ u32x4 scale_source(int m) const { return sb[Cfg::DUAL ? m : 0]; }
+    static constexpr uint32_t sb_second = Cfg::DUAL ? 0 : 256;
+};
+
+struct LargeState {
+    uint32_t sa, s0, ss;             // LDS offsets of k-step kt: A stage, first B half's place, scales (of its ring)
+};
+
+// One k-step. On entry f[0] holds its first-half fragments and sc its scales; on return those of k-step kt + 1 are in f[0] and
+// nsc. pa, pb, psa, psb: the wavefront's fragment and scale addresses in a first stage.
+template <class Cfg, class Full>
+__device__ __forceinline__ void large_kstep(f32x4 (&acc)[Cfg::TM][8], i32x4 (&fa)[2][Cfg::TM], i32x4 (&fb)[2][8],
+                                            const int (&sca)[Cfg::TM], const int (&scb)[8], int (&nsa)[Cfg::TM], int (&nsb)[8],
+                                            LargeState& st, LargeLoads<Full>& lp, int wave, int wn, const unsigned char* pa0,
+                                            const unsigned char* pa1, const unsigned char* pb0, const unsigned char* pb1,
+                                            const unsigned char* psa, const unsigned char* psb) {
+    using L = Large<Full>;
+    constexpr int TM = Cfg::TM, NM = TM * 8, NR = TM + 8;
+    constexpr int STRIDE1 = NM / 8, NL2 = TM + 4, STRIDE2 = NM / NL2;
+    constexpr int SPAN1 = (3 * NR <= NM - 4) ? 3 * NR : 2 * NR;
+    static_assert(TM >= 4 && TM <= 8, "64 to 128 rows of a wavefront");
+    auto wrap = [](uint32_t v) { return v >= L::B_RING ? v - L::B_RING : v; };
+    const uint32_t own = wrap(st.s0 + wn * L::HB);                       // the wavefront's columns
+    const uint32_t s0n = wrap(st.s0 + 2 * L::HB), own_n = wrap(s0n + wn * L::HB);
+    const uint32_t idle = wrap(st.s0 + 4 * L::HB);                       // place of the first B half of kt + 2
+    const uint32_t ssn = (st.ss + L::SS) & (4 * L::SS - 1);
+    const uint32_t scales_to = L::SCALES + ((st.ss + 2 * L::SS) & (4 * L::SS - 1)) + wave * 512;
+    const uint32_t b0_to = L::A_RING + idle + wave * 4096, b1_to = L::A_RING + st.s0 + wave * 4096, a_to = st.sa + wave * 1024;
+    const unsigned char *pa_h1 = pa1 + st.sa, *pb_h1 = pb1 + own, *pa_n0 = pa0 + (st.sa ^ L::AB), *pb_n0 = pb0 + own_n;
+    const unsigned char *psa_n = psa + ssn, *psb_n = psb + ssn;
+    // ---- first half: MFMAs on f[0]; read f[1]; four B loads, four scale loads
+    auto first = [&](auto mtag) {
+        constexpr int m = decltype(mtag)::value, i = m >> 3, j = m & 7, n = m / STRIDE1;
+        if constexpr (m % STRIDE1 == STRIDE1 - 1 && n < 4)
+            mma_then_dma<0, 16, n * 1024>(fb[0][j], fa[0][i], acc[i][j], scb[j], sca[i], b0_to, lp.b_voff[n], lp.b);
+        else if constexpr (m % STRIDE1 == STRIDE1 - 1 && n < 6)
+            mma_then_dma<0, 4, (n - 4) * 256>(fb[0][j], fa[0][i], acc[i][j], scb[j], sca[i], scales_to, lp.sa_voff + (n - 4) * 256, lp.sa);
+        else if constexpr (m % STRIDE1 == STRIDE1 - 1)
+            mma_then_dma<0, 4, L::SA + (n - 6) * 256>(fb[0][j], fa[0][i], acc[i][j], scb[j], sca[i], scales_to,
+                                                      lp.sb_voff + (n - 6) * LargeLoads<Full>::sb_second, lp.scale_source(n - 6));
+        else
+            mma_agpr<0>(fb[0][j], fa[0][i], acc[i][j], scb[j], sca[i]);
+        MOE_FENCE();
+        constexpr int r = (m * NR + SPAN1 - 1) / SPAN1;
+        if constexpr (r < NR && (r * SPAN1) / NR == m) {
+            if constexpr (r < 8) fb[1][r] = *reinterpret_cast<const i32x4*>(pb_h1 + r * 2048);
+            else fa[1][r - 8] = *reinterpret_cast<const i32x4*>(pa_h1 + (r - 8) * 2048);
+            MOE_FENCE();
+        }
+    };
+    // ---- second half: MFMAs on f[1]; read f[0] and the scales of kt + 1; the A loads and four B loads
+    auto second = [&](auto mtag) {
+        constexpr int m = decltype(mtag)::value, i = m >> 3, j = m & 7, n = m / STRIDE2;
+        if constexpr (m % STRIDE2 == STRIDE2 - 1 && n < 4)
+            mma_then_dma<1, 16, n * 1024>(fb[1][j], fa[1][i], acc[i][j], scb[j], sca[i], b1_to, lp.b_voff[4 + n], lp.b);
+        else if constexpr (m % STRIDE2 == STRIDE2 - 1 && n < NL2)
+            mma_then_dma<1, 16, (n - 4) * 4096>(fb[1][j], fa[1][i], acc[i][j], scb[j], sca[i], a_to, lp.a_voff[n - 4], lp.a);
+        else
+            mma_agpr<1>(fb[1][j], fa[1][i], acc[i][j], scb[j], sca[i]);
+        MOE_FENCE();
+        constexpr int r = (m * 2 * NR + NM - 1) / NM;                    // read r behind MFMA r * NM / (2 NR)
+        if constexpr (r < 2 * NR && (r * NM) / (2 * NR) == m) {
+            if constexpr (r % 2 == 0) {
+                if constexpr (r / 2 < 8) fb[0][r / 2] = *reinterpret_cast<const i32x4*>(pb_n0 + r / 2 * 2048);
+                else fa[0][r / 2 - 8] = *reinterpret_cast<const i32x4*>(pa_n0 + (r / 2 - 8) * 2048);
+            } else {
+                if constexpr (r / 2 < 8) nsb[r / 2] = *reinterpret_cast<const uint16_t*>(psb_n + r / 2 * 128);
+                else nsa[r / 2 - 8] = *reinterpret_cast<const uint16_t*>(psa_n + (r / 2 - 8) * 128);
+            }
+            MOE_FENCE();
+        }
+    };
+    gemm::static_for<NM>(first);
+    lp.next_scales();
+    asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();      // k-step kt + 1 complete in LDS; this k-step's stages are free
+    MOE_FENCE();
+    gemm::static_for<NM>(second);
+    lp.next_rows();
+    st.sa ^= L::AB;
+    st.s0 = s0n;
+    st.ss = ssn;
+}
+
+// H's columns of a wavefront, two blocks of 32: straight from the accumulators.
+template <class Cfg>
+__device__ __forceinline__ void store_blocks(const f32x4 (&acc)[Cfg::TM][8], const Operands& op, const TileCoord& tc,
+                                             const Outputs& out, int wm, int wn, int lane) {
+    const int frag_row = lane & 15, g = lane >> 4;
+    const int col0 = tc.nt * Cfg::BN_OUT + wn * 64;
+#pragma unroll
+    for (int i = 0; i < Cfg::TM; ++i) {
+        const int r = wm * Cfg::WTM + i * 16 + frag_row;
+        const size_t row = static_cast<size_t>(tc.row0) + r;
+        uint32_t codes[2], scale[2];
+        int part = 0;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            float v[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                v[q] = gemm::silu(gemm::read_acc(acc[i][4 * b + q / 4], q & 3)) * gemm::read_acc(acc[i][4 * b + 2 + q / 4], q & 3);
+            codes[b] = block_codes(v, g, scale[b], part);
+        }
+        if (r < tc.rows) {
+            uint8_t* at = static_cast<uint8_t*>(out.c) + row * (op.N / 2) + col0 / 2 + part * 4;
+            *reinterpret_cast<uint32_t*>(at) = codes[0];
+            *reinterpret_cast<uint32_t*>(at + 16) = codes[1];
+            if (g < 2) store_scale(out.scale, op.R, row, col0 / 32 + g, op.N / 32, g ? scale[1] : scale[0]);
+        }
+        MOE_FENCE();
+    }
+}
+
+// One tile, from its first load to its last store. At least two k-steps, three if ODD.
+template <class Cfg, class Full, bool ODD>
+__device__ __forceinline__ void large_tile(const Operands& op, const Outputs& out, const TileCoord& tc, unsigned char* smem,
+                                           int wave, int lane) {
+    using L = Large<Full>;
+    constexpr int TM = Cfg::TM;
+    const int wm = wave / Cfg::WN, wn = wave % Cfg::WN, frag_row = lane & 15, g = lane >> 4;
+    LargeLoads<Full> lp;
+    lp.init(op, tc, wave, lane);
+    const int KT = mx_runs(op.K);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {                    // k-step 1 may be one that there is not
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dma<16>(lp.b, lp.b_voff[i], L::A_RING + (2 * s + (i >> 2)) * L::HB + wave * 4096 + (i & 3) * 1024);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) dma<16>(lp.a, lp.a_voff[i], s * L::AB + wave * 1024 + i * 4096);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            dma<4>(lp.sa, lp.sa_voff + i * 256, L::SCALES + s * L::SS + wave * 512 + i * 256);
+            dma<4>(lp.scale_source(i), lp.sb_voff + i * LargeLoads<Full>::sb_second, L::SCALES + s * L::SS + L::SA + wave * 512 + i * 256);
+        }
+        lp.next_scales();
+        lp.next_rows();
+    }
+    gemm::FragPlan<Cfg> fp;
+    fp.init(lane, wm, wn);
+    const unsigned char* pa[2] = {smem + fp.a_off[0], smem + fp.a_off[1]};
+    // B-tile rows of a wavefront from the start of its half
+    const unsigned char* pb[2] = {smem + L::A_RING + (fp.b_off[0] - Cfg::A_BYTES - wn * L::HB),
+                                  smem + L::A_RING + (fp.b_off[1] - Cfg::A_BYTES - wn * L::HB)};
+    const unsigned char* psa = smem + L::SCALES + (wm * Cfg::WTM + frag_row) * 8 + 2 * g;
+    const unsigned char* psb = smem + L::SCALES + L::SA + (wn * 128 + frag_row) * 8 + 2 * g;
+    gemm::wait_vmcnt<8 + TM + 4>();                  // k-step 0 landed
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    i32x4 fa[2][TM], fb[2][8];
+    int sa[2][TM], sb[2][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        fb[0][j] = *reinterpret_cast<const i32x4*>(pb[0] + wn * L::HB + j * 2048);
+        sb[0][j] = *reinterpret_cast<const uint16_t*>(psb + j * 128);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        fa[0][i] = *reinterpret_cast<const i32x4*>(pa[0] + i * 2048);
+        sa[0][i] = *reinterpret_cast<const uint16_t*>(psa + i * 128);
+    }
+    MOE_FENCE();
+    f32x4 acc[TM][8];
+    gemm::zero_accumulators(acc);
+    LargeState st{0, 0, 0};
+    auto step = [&](auto from) {
+        constexpr int S = decltype(from)::value;
+        large_kstep<Cfg, Full>(acc, fa, fb, sa[S], sb[S], sa[S ^ 1], sb[S ^ 1], st, lp, wave, wn, pa[0], pa[1], pb[0], pb[1], psa, psb);
+    };
+    if constexpr (ODD) step(std::integral_constant<int, 0>{});
+    for (int n = KT / 2;;) {                         // at least one pair: no path joins behind the loop
+        step(std::integral_constant<int, ODD ? 1 : 0>{});
+        step(std::integral_constant<int, ODD ? 0 : 1>{});
+        if (--n == 0) break;
+    }
+    gemm::mfma_drain(acc[TM - 1]);
+    if constexpr (Cfg::DUAL) {
+        store_blocks<Cfg>(acc, op, tc, out, wm, wn, lane);
+        gemm::wait_vmcnt<0>();                       // nothing is on its way to LDS when it is given back
+    } else {
+        gemm::wait_vmcnt<0>();
+        __builtin_amdgcn_s_barrier();                // of no wavefront: LDS is free for the outputs
+        asm volatile("" ::: "memory");
+        gemm::store_tile_via_lds<Cfg>(acc, tc, fp, wave, lane, smem + wave * gemm::kEpilogueBytes, static_cast<uint16_t*>(out.c),
+                                      op.N, gemm::KeptScales<Cfg>{}, [] {});
+    }
+}
+
+template <class Cfg, bool ODD>
+__global__ __launch_bounds__(256) void large_kernel(Operands op, Outputs out, int split_cus) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const int NT = gemm::n_tiles<Cfg>(op.N);
+    const gemm::Cut cut = op.K < 4 * gemm::kLongK ? gemm::Cut::kAlways : gemm::Cut::kLong;
+    const TileCoord tc = op.offsets == nullptr ? gemm::locate_tile_of_one<256>(op.R, NT, split_cus, cut)
+                                               : gemm::locate_tile<256>(op.offsets, op.E, NT, split_cus, cut);
+    if (tc.expert < 0) return;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    auto run = [&](auto tag) {
+        using TileCfg = typename decltype(tag)::type;
+        large_tile<TileCfg, Cfg, ODD>(op, out, tc, smem, wave, lane);
+    };
+    switch (tc.height) {
+        case 128: run(gemm::type_tag<gemm::AtHeight<Cfg, 128>>{}); break;
+        case 160: run(gemm::type_tag<gemm::AtHeight<Cfg, 160>>{}); break;
+        case 192: run(gemm::type_tag<gemm::AtHeight<Cfg, 192>>{}); break;
+        case 224: run(gemm::type_tag<gemm::AtHeight<Cfg, 224>>{}); break;
+        default: run(gemm::type_tag<Cfg>{}); break;
+    }
+}
+
 }  // namespace mx4
+namespace gemm {
+template <class Cfg, int H>
+struct WithHeight<mx4::Mx4<Cfg>, H> { using type = mx4::Mx4<typename WithHeight<Cfg, H>::type>; };
+}  // namespace gemm
 }  // namespace moe
