@@ -155,13 +155,23 @@ using GateUpLarge = mx4::Mx4<gemm::Config<256, 256, 64, 2, 2, 2, true>>;
 template <bool F32>
 using PlainLarge = mx4::Mx4<std::conditional_t<F32, gemm::F32Out<gemm::Config<256, 256, 64, 2, 2, 2, false>>,
                                                gemm::Config<256, 256, 64, 2, 2, 2, false>>>;
+// Workgroups that run one tile after the other where there are tiles for more than a round. A workgroup per tile -> so: 8192 rows
+// of 2048 x 16384 columns 175 -> 170 us, 6144 x 16384 379 -> 375, 16384 x 16384 867 -> 857, experts of 8 x 6144 x 16384 with 8192
+// tokens 2213 -> 2180, 5003 skewed tokens through 64 of 2048 x 1408 229 -> 223. What they gain is bounded by the board's power: the
+// clock falls from 1.9 to 1.6 GHz as the matrix units get busier (8192 x 16384 x 16384: busy 70 % of the time, 5.1 PFLOP/s; the
+// same without a load or an LDS read, 8.0).
 template <class Cfg, bool ODD>
 int large_of(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
-    static std::atomic<uint64_t> attr_set{0};
-    const int cus = compute_units(env.device);
+    static std::atomic<uint64_t> attr_set[2];
+    const int cus = compute_units(env.device), nt = gemm::n_tiles<Cfg>(op.N);
     // tiles, and the halves that the last round's are cut into
-    const long long grid = most_row_tiles(op.R, op.E, 256) * gemm::n_tiles<Cfg>(op.N) + kXcds * ((cus / 2 + kXcds - 1) / kXcds + 1);
-    return launch(env, attr_set, mx4::large_kernel<Cfg, ODD>, mx4::Large<Cfg>::SMEM, 256, grid, s, op, out, cus);
+    const long long slots = most_row_tiles(op.R, op.E, 256) * nt + kXcds * ((cus / 2 + kXcds - 1) / kXcds + 1);
+    const double tiles = static_cast<double>(op.R) / 256 * nt;
+    if (tiles > 1.5 * cus)
+        return launch(env, attr_set[0], mx4::large_kernel<Cfg, true, ODD>, mx4::Large<Cfg>::SMEM, 256, std::min<long long>(slots, cus), s,
+                      op, out, cus, env.tile_counters);
+    return launch(env, attr_set[1], mx4::large_kernel<Cfg, false, ODD>, mx4::Large<Cfg>::SMEM, 256, slots, s, op, out, cus,
+                  env.tile_counters);
 }
 template <class Cfg>
 bool large_fits(const Operands& op) { return op.K > 512 && op.N >= Cfg::BN_OUT; }

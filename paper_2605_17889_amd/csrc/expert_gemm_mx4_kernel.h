@@ -308,8 +308,9 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void ring_kernel(Operands op, Output
 // ring of four k-steps), in the second half the loads of its A rows and second B half, into the places that the barrier of kt
 // has freed: at that barrier only the first half's loads may still be on their way. The scales of k-step kt + 1 are read from
 // LDS in the second half of kt, 16 bits for each fragment's row and lane group: one byte for each half-step.
-// Loads go through resources that advance by a k-step at a time and end where the tile's rows do; those of k-steps that there
-// are not are empty: the loads then bring zeros and read nothing, and every k-step runs the same code.
+// Loads go through resources that advance by a k-step at a time and end where the tile's rows do. In the last two k-steps of a
+// tile they stand on the next one, or are empty where there is none: they then bring zeros and read nothing, and every k-step
+// runs the same code.
 template <class Cfg>
 struct Mx4 : Cfg {
     static constexpr bool ANY_WIDTH = true;
@@ -376,21 +377,13 @@ __device__ __forceinline__ void mma_then_dma(const i32x4& w, const i32x4& x, f32
 // rows of a tile of TM * 32 rows; B load i of half b is B-tile rows 128 b + 32 w + 8 i .. + 7 (with DUAL 32 rows of one matrix).
 template <class Cfg>
 struct LargeLoads {
-    u32x4 a, b, sa, sb[Cfg::DUAL ? 2 : 1];
-    uint32_t a_voff[8], b_voff[8], sa_voff, sb_voff;           // of the first scale loads; the second ones are 256 bytes on
+    u32x4 a, b, sa, sb[Cfg::DUAL ? 2 : 1];           // at the k-step whose loads are next
+    uint32_t a_voff[8], b_voff[8], sa_voff, sb_voff; // of the first scale loads; the second ones are 256 bytes on
     uint64_t sa_step, sb_step;
-    int left;                                                  // k-steps from the one whose loads are next to the last
-    __device__ __forceinline__ void init(const Operands& op, const TileCoord& tc, int wave, int lane) {
+    uint32_t shorter;                                // what a and b lose with a k-step: nothing where they are empty
+    // what is the same for every tile
+    __device__ __forceinline__ void init(const Operands& op, int wave, int lane) {
         const uint32_t pitch = static_cast<uint32_t>(op.K) / 2;
-        const int col0 = gemm::first_column<Cfg>(tc, op.N);
-        const size_t first = static_cast<size_t>(tc.expert) * op.N + col0;
-        const size_t first_scale = (static_cast<size_t>(tc.expert) * mx_runs(op.K) * op.N + col0) * kMxRunBytes;
-        left = mx_runs(op.K);
-        a = resource_words(op.a + static_cast<size_t>(tc.row0) * pitch, tc.rows * pitch);
-        b = resource_words((Cfg::DUAL && (wave & 1) ? op.b[1] : op.b[0]) + first * pitch, Cfg::BN_OUT * pitch);
-        sa = resource_words(op.a_scale + static_cast<size_t>(tc.row0) * kMxRunBytes, tc.rows * kMxRunBytes);
-#pragma unroll
-        for (int m = 0; m < (Cfg::DUAL ? 2 : 1); ++m) sb[m] = resource_words(op.b_scale[m] + first_scale, Cfg::BN_OUT * kMxRunBytes);
         sa_step = static_cast<uint64_t>(op.R) * kMxRunBytes;
         sb_step = static_cast<uint64_t>(op.N) * kMxRunBytes;
         const int lrow = lane >> 3;
@@ -404,22 +397,36 @@ struct LargeLoads {
         sa_voff = wave * 512 + lane * 4;
         sb_voff = (Cfg::DUAL ? wave * 256 : wave * 512) + lane * 4;
     }
-    // to the next k-step; the resources of one that there is not are empty
+    // to the first k-step of a tile; one without rows loads nothing
+    __device__ __forceinline__ void start(const Operands& op, const TileCoord& tc, int wave) {
+        const uint32_t pitch = static_cast<uint32_t>(op.K) / 2;
+        const int col0 = gemm::first_column<Cfg>(tc, op.N), cols = tc.rows > 0 ? Cfg::BN_OUT : 0;
+        const size_t first = static_cast<size_t>(tc.expert) * op.N + col0;
+        const size_t first_scale = (static_cast<size_t>(tc.expert) * mx_runs(op.K) * op.N + col0) * kMxRunBytes;
+        shorter = tc.rows > 0 ? 128u : 0u;
+        a = resource_words(op.a + static_cast<size_t>(tc.row0) * pitch, tc.rows * pitch);
+        b = resource_words((Cfg::DUAL && (wave & 1) ? op.b[1] : op.b[0]) + first * pitch, cols * pitch);
+        sa = resource_words(op.a_scale + static_cast<size_t>(tc.row0) * kMxRunBytes, tc.rows * kMxRunBytes);
+#pragma unroll
+        for (int m = 0; m < (Cfg::DUAL ? 2 : 1); ++m) sb[m] = resource_words(op.b_scale[m] + first_scale, cols * kMxRunBytes);
+    }
+    // from here on nothing is loaded: zeros go to LDS
+    __device__ __forceinline__ void stop() {
+        a[2] = b[2] = sa[2] = shorter = 0;
+#pragma unroll
+        for (int m = 0; m < (Cfg::DUAL ? 2 : 1); ++m) sb[m][2] = 0;
+    }
+    // to the next k-step
     __device__ __forceinline__ void next_scales() {
         advance(sa, sa_step);
-        sa[2] = left > 1 ? sa[2] : 0u;
 #pragma unroll
-        for (int m = 0; m < (Cfg::DUAL ? 2 : 1); ++m) {
-            advance(sb[m], sb_step);
-            sb[m][2] = left > 1 ? sb[m][2] : 0u;
-        }
+        for (int m = 0; m < (Cfg::DUAL ? 2 : 1); ++m) advance(sb[m], sb_step);
     }
     __device__ __forceinline__ void next_rows() {
         advance(a, 128);
-        a[2] = left > 1 ? a[2] - 128u : 0u;
+        a[2] -= shorter;
         advance(b, 128);
-        b[2] = left > 1 ? b[2] - 128u : 0u;
-        --left;
+        b[2] -= shorter;
     }
     __device__ __forceinline__ u32x4 scale_source(int m) const { return sb[Cfg::DUAL ? m : 0]; }
     static constexpr uint32_t sb_second = Cfg::DUAL ? 0 : 256;
@@ -505,10 +512,10 @@ __device__ __forceinline__ void large_kstep(f32x4 (&acc)[Cfg::TM][8], i32x4 (&fa
     st.ss = ssn;
 }
 
-// H's columns of a wavefront, two blocks of 32: straight from the accumulators.
-template <class Cfg>
+// H's columns of a wavefront, two blocks of 32: straight from the accumulators. `before_stores` runs once, ahead of the first.
+template <class Cfg, class Before>
 __device__ __forceinline__ void store_blocks(const f32x4 (&acc)[Cfg::TM][8], const Operands& op, const TileCoord& tc,
-                                             const Outputs& out, int wm, int wn, int lane) {
+                                             const Outputs& out, int wm, int wn, int lane, Before&& before_stores) {
     const int frag_row = lane & 15, g = lane >> 4;
     const int col0 = tc.nt * Cfg::BN_OUT + wn * 64;
 #pragma unroll
@@ -525,6 +532,7 @@ __device__ __forceinline__ void store_blocks(const f32x4 (&acc)[Cfg::TM][8], con
                 v[q] = gemm::silu(gemm::read_acc(acc[i][4 * b + q / 4], q & 3)) * gemm::read_acc(acc[i][4 * b + 2 + q / 4], q & 3);
             codes[b] = block_codes(v, g, scale[b], part);
         }
+        if (i == 0) before_stores();
         if (r < tc.rows) {
             uint8_t* at = static_cast<uint8_t*>(out.c) + row * (op.N / 2) + col0 / 2 + part * 4;
             *reinterpret_cast<uint32_t*>(at) = codes[0];
@@ -535,30 +543,18 @@ __device__ __forceinline__ void store_blocks(const f32x4 (&acc)[Cfg::TM][8], con
     }
 }
 
-// One tile, from its first load to its last store. At least two k-steps, three if ODD.
-template <class Cfg, class Full, bool ODD>
-__device__ __forceinline__ void large_tile(const Operands& op, const Outputs& out, const TileCoord& tc, unsigned char* smem,
-                                           int wave, int lane) {
+// One tile of at least two k-steps, three if ODD. On entry its first two are in the rings, at the places of `st`, and every
+// wavefront knows it; on return those of the next tile are, and the stores of this one are on their way.
+//   lp     loads of this tile at k-step 2, then of the next one; last: there is none
+//   draw   called once in each wavefront two k-steps before the end; drawn() before the first store, when all loads of the
+//          wavefront have landed
+template <class Cfg, class Full, bool ODD, class Draw, class Drawn>
+__device__ __forceinline__ void large_tile(const Operands& op, const Outputs& out, const TileCoord& tc, const TileCoord& nxt,
+                                           bool last, LargeLoads<Full>& lp, LargeState& st, unsigned char* smem, int wave, int lane,
+                                           Draw&& draw, Drawn&& drawn) {
     using L = Large<Full>;
     constexpr int TM = Cfg::TM;
     const int wm = wave / Cfg::WN, wn = wave % Cfg::WN, frag_row = lane & 15, g = lane >> 4;
-    LargeLoads<Full> lp;
-    lp.init(op, tc, wave, lane);
-    const int KT = mx_runs(op.K);
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {                    // k-step 1 may be one that there is not
-#pragma unroll
-        for (int i = 0; i < 8; ++i) dma<16>(lp.b, lp.b_voff[i], L::A_RING + (2 * s + (i >> 2)) * L::HB + wave * 4096 + (i & 3) * 1024);
-#pragma unroll
-        for (int i = 0; i < TM; ++i) dma<16>(lp.a, lp.a_voff[i], s * L::AB + wave * 1024 + i * 4096);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            dma<4>(lp.sa, lp.sa_voff + i * 256, L::SCALES + s * L::SS + wave * 512 + i * 256);
-            dma<4>(lp.scale_source(i), lp.sb_voff + i * LargeLoads<Full>::sb_second, L::SCALES + s * L::SS + L::SA + wave * 512 + i * 256);
-        }
-        lp.next_scales();
-        lp.next_rows();
-    }
     gemm::FragPlan<Cfg> fp;
     fp.init(lane, wm, wn);
     const unsigned char* pa[2] = {smem + fp.a_off[0], smem + fp.a_off[1]};
@@ -567,68 +563,169 @@ __device__ __forceinline__ void large_tile(const Operands& op, const Outputs& ou
                                   smem + L::A_RING + (fp.b_off[1] - Cfg::A_BYTES - wn * L::HB)};
     const unsigned char* psa = smem + L::SCALES + (wm * Cfg::WTM + frag_row) * 8 + 2 * g;
     const unsigned char* psb = smem + L::SCALES + L::SA + (wn * 128 + frag_row) * 8 + 2 * g;
-    gemm::wait_vmcnt<8 + TM + 4>();                  // k-step 0 landed
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
     i32x4 fa[2][TM], fb[2][8];
     int sa[2][TM], sb[2][8];
+    const uint32_t own = st.s0 + wn * L::HB >= L::B_RING ? st.s0 + wn * L::HB - L::B_RING : st.s0 + wn * L::HB;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        fb[0][j] = *reinterpret_cast<const i32x4*>(pb[0] + wn * L::HB + j * 2048);
-        sb[0][j] = *reinterpret_cast<const uint16_t*>(psb + j * 128);
+        fb[0][j] = *reinterpret_cast<const i32x4*>(pb[0] + own + j * 2048);
+        sb[0][j] = *reinterpret_cast<const uint16_t*>(psb + st.ss + j * 128);
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        fa[0][i] = *reinterpret_cast<const i32x4*>(pa[0] + i * 2048);
-        sa[0][i] = *reinterpret_cast<const uint16_t*>(psa + i * 128);
+        fa[0][i] = *reinterpret_cast<const i32x4*>(pa[0] + st.sa + i * 2048);
+        sa[0][i] = *reinterpret_cast<const uint16_t*>(psa + st.ss + i * 128);
     }
     MOE_FENCE();
     f32x4 acc[TM][8];
     gemm::zero_accumulators(acc);
-    LargeState st{0, 0, 0};
     auto step = [&](auto from) {
         constexpr int S = decltype(from)::value;
         large_kstep<Cfg, Full>(acc, fa, fb, sa[S], sb[S], sa[S ^ 1], sb[S ^ 1], st, lp, wave, wn, pa[0], pa[1], pb[0], pb[1], psa, psb);
     };
     if constexpr (ODD) step(std::integral_constant<int, 0>{});
-    for (int n = KT / 2;;) {                         // at least one pair: no path joins behind the loop
+    for (int left = mx_runs(op.K) - 2 - ODD;; left -= 2) {         // k-steps whose loads are this tile's
+        if (left == 0) {
+            if (last) {
+                lp.stop();
+            } else {
+                lp.start(op, nxt, wave);
+                draw();
+            }
+        }
         step(std::integral_constant<int, ODD ? 1 : 0>{});
         step(std::integral_constant<int, ODD ? 0 : 1>{});
-        if (--n == 0) break;
+        if (left == 0) break;
     }
     gemm::mfma_drain(acc[TM - 1]);
+    // rows of a higher next tile that this one's loads did not reach, of both its k-steps: lp is two k-steps on
+    if constexpr (TM < 8) {
+        if (!last && nxt.height > Cfg::BM) {
+            u32x4 first = lp.a, second = lp.a;
+            const uint32_t bytes = nxt.rows * (static_cast<uint32_t>(op.K) / 2);
+            advance(first, -256ll);
+            advance(second, -128ll);
+            first[2] = bytes;
+            second[2] = bytes - 128u;
+#pragma unroll
+            for (int i = TM; i < 8; ++i) {
+                dma<16>(first, lp.a_voff[i], st.sa + wave * 1024 + i * 4096);
+                dma<16>(second, lp.a_voff[i], (st.sa ^ L::AB) + wave * 1024 + i * 4096);
+            }
+        }
+    }
+    auto before = [&] {
+        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): the next tile's first loads, and what draw() asked for
+        drawn();
+    };
     if constexpr (Cfg::DUAL) {
-        store_blocks<Cfg>(acc, op, tc, out, wm, wn, lane);
-        gemm::wait_vmcnt<0>();                       // nothing is on its way to LDS when it is given back
+        store_blocks<Cfg>(acc, op, tc, out, wm, wn, lane, before);
     } else {
-        gemm::wait_vmcnt<0>();
-        __builtin_amdgcn_s_barrier();                // of no wavefront: LDS is free for the outputs
-        asm volatile("" ::: "memory");
-        gemm::store_tile_via_lds<Cfg>(acc, tc, fp, wave, lane, smem + wave * gemm::kEpilogueBytes, static_cast<uint16_t*>(out.c),
-                                      op.N, gemm::KeptScales<Cfg>{}, [] {});
+        // through the B half that is idle: every wavefront had read it at the last barrier, and the next load into it is the next
+        // tile's first
+        const uint32_t idle = st.s0 + 4 * L::HB >= L::B_RING ? st.s0 + 4 * L::HB - L::B_RING : st.s0 + 4 * L::HB;
+        static_assert(4 * gemm::kEpilogueBytes <= L::HB, "room for the outputs");
+        gemm::store_tile_via_lds<Cfg>(acc, tc, fp, wave, lane, smem + L::A_RING + idle + wave * gemm::kEpilogueBytes,
+                                      static_cast<uint16_t*>(out.c), op.N, gemm::KeptScales<Cfg>{}, before);
     }
 }
 
-template <class Cfg, bool ODD>
-__global__ __launch_bounds__(256) void large_kernel(Operands op, Outputs out, int split_cus) {
+// PERSISTENT: a workgroup runs one tile after the other, as grouped_gemm_1w_kernel's do (slots, draws and their counter are
+// described there): the next tile's first two k-steps are loaded in the last two of this one and arrive under its stores.
+template <class Cfg, bool PERSISTENT, bool ODD>
+__global__ __launch_bounds__(256) void large_kernel(Operands op, Outputs out, int split_cus, int32_t* __restrict__ counters) {
+    using L = Large<Cfg>;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int xcd = blockIdx.x % kXcds, workgroups = gridDim.x / kXcds;
+    int32_t* counter = counters + xcd * gemm::kCounterInts;
     const int NT = gemm::n_tiles<Cfg>(op.N);
     const gemm::Cut cut = op.K < 4 * gemm::kLongK ? gemm::Cut::kAlways : gemm::Cut::kLong;
-    const TileCoord tc = op.offsets == nullptr ? gemm::locate_tile_of_one<256>(op.R, NT, split_cus, cut)
-                                               : gemm::locate_tile<256>(op.offsets, op.E, NT, split_cus, cut);
-    if (tc.expert < 0) return;
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    auto run = [&](auto tag) {
-        using TileCfg = typename decltype(tag)::type;
-        large_tile<TileCfg, Cfg, ODD>(op, out, tc, smem, wave, lane);
+    gemm::TileTable<256> table;                      // kept over the tiles: a lookup then reads no memory
+    const uint32_t magic = gemm::division_magic(lane);
+    TileCoord tc;
+    if constexpr (PERSISTENT) {
+        if (op.offsets == nullptr) table.init_one(op.R, NT, split_cus, xcd, lane);
+        else table.init(op.offsets, op.E, NT, split_cus, xcd, lane);
+        tc = gemm::uniform_tile(table.find(NT, cut, blockIdx.x / kXcds, magic));
+        if (tc.expert == gemm::kNoTile) return;      // the same for the whole workgroup
+    } else {
+        tc = op.offsets == nullptr ? gemm::locate_tile_of_one<256>(op.R, NT, split_cus, cut)
+                                   : gemm::locate_tile<256>(op.offsets, op.E, NT, split_cus, cut);
+        if (tc.expert < 0) return;
+    }
+    // an empty slot is a tile without rows: it loads and stores nothing
+    const TileCoord none{0, 0, 0, 0, 128};
+    if (tc.expert == gemm::kEmptySlot) tc = none;
+    bool last = !PERSISTENT, drew = false;
+    int ahead = 0;                                   // lane 0 of wavefront 0: the latest draw
+    LargeState st{0, 0, 0};
+    // the scales of the tile's last k-step are no longer read when it is drawn, and overwritten in the next one's second k-step
+    auto draw_at = [&] { return reinterpret_cast<int*>(smem + L::SCALES + ((st.ss + 3 * L::SS) & (4 * L::SS - 1))); };
+    auto draw = [&] {
+        if (PERSISTENT && threadIdx.x == 0) {
+            int at = 0;                              // an address that the compiler does not know to be uniform
+            asm volatile("" : "+v"(at));
+            ahead = __hip_atomic_fetch_add(counter + at, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
     };
-    switch (tc.height) {
-        case 128: run(gemm::type_tag<gemm::AtHeight<Cfg, 128>>{}); break;
-        case 160: run(gemm::type_tag<gemm::AtHeight<Cfg, 160>>{}); break;
-        case 192: run(gemm::type_tag<gemm::AtHeight<Cfg, 192>>{}); break;
-        case 224: run(gemm::type_tag<gemm::AtHeight<Cfg, 224>>{}); break;
-        default: run(gemm::type_tag<Cfg>{}); break;
+    auto drawn = [&] {
+        if (PERSISTENT && wave == 0) {
+            const int v = __builtin_amdgcn_readfirstlane(ahead);
+            if (lane == 0) *draw_at() = v;
+        }
+    };
+    LargeLoads<Cfg> lp;
+    lp.init(op, wave, lane);
+    lp.start(op, tc, wave);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dma<16>(lp.b, lp.b_voff[i], L::A_RING + (2 * s + (i >> 2)) * L::HB + wave * 4096 + (i & 3) * 1024);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dma<16>(lp.a, lp.a_voff[i], s * L::AB + wave * 1024 + i * 4096);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            dma<4>(lp.sa, lp.sa_voff + i * 256, L::SCALES + s * L::SS + wave * 512 + i * 256);
+            dma<4>(lp.scale_source(i), lp.sb_voff + i * LargeLoads<Cfg>::sb_second, L::SCALES + s * L::SS + L::SA + wave * 512 + i * 256);
+        }
+        lp.next_scales();
+        lp.next_rows();
+    }
+    gemm::wait_vmcnt<20>();                          // k-step 0 landed
+    int slot = blockIdx.x / kXcds + workgroups;      // of the next tile
+    while (true) {
+        // lane-dependent addresses are formed anew for every tile: kept over the loop they would take the registers of fragments
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(lane) :: "memory");
+        __builtin_amdgcn_s_barrier();                // the tile's first k-step has landed for every wavefront
+        asm volatile("" ::: "memory");
+        TileCoord nxt = tc;
+        if constexpr (PERSISTENT) {
+            if (drew) slot = 2 * workgroups + __builtin_amdgcn_readfirstlane(*draw_at());
+            const TileCoord found = gemm::uniform_tile(table.find(NT, cut, slot, magic));
+            last = found.expert == gemm::kNoTile;
+            if (found.expert == gemm::kEmptySlot)
+                nxt = none;
+            else if (!last)
+                nxt = found;
+            else if (drew && slot == table.range.slots + workgroups - 1 && threadIdx.x == 0)
+                __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        auto run = [&](auto tag) {
+            using TileCfg = typename decltype(tag)::type;
+            large_tile<TileCfg, Cfg, ODD>(op, out, tc, nxt, last, lp, st, smem, wave, lane, draw, drawn);
+        };
+        switch (tc.height) {
+            case 128: run(gemm::type_tag<gemm::AtHeight<Cfg, 128>>{}); break;
+            case 160: run(gemm::type_tag<gemm::AtHeight<Cfg, 160>>{}); break;
+            case 192: run(gemm::type_tag<gemm::AtHeight<Cfg, 192>>{}); break;
+            case 224: run(gemm::type_tag<gemm::AtHeight<Cfg, 224>>{}); break;
+            default: run(gemm::type_tag<Cfg>{}); break;
+        }
+        if (last) break;
+        tc = nxt;
+        drew = true;
     }
 }
 
