@@ -10,6 +10,7 @@
 #include <cmath>
 
 #include "expert_gemm_mx4_kernel.h"
+#include "mx4_tile_rules.h"
 
 namespace moe {
 namespace {
@@ -18,67 +19,59 @@ using mx4::Operands;
 using mx4::Outputs;
 using mx4::Tile;
 
-//                     BM   BN  WM WN NSTAGE DUAL
-using GateUp128 = Tile<128, 128, 2, 2, 4, true>;
-using GateUp32  = Tile<32, 128, 2, 2, 5, true>;
-template <bool F32> using Plain128 = Tile<128, 128, 2, 2, 4, false, false, F32>;
-template <bool F32> using Plain32 = Tile<32, 64, 2, 2, 6, false, false, F32>;
+//                       BM   BN  WM WN NSTAGE DUAL STREAM_B
+using GateUp32     = Tile<32, 128, 2, 2, 3, true, true>;
+using GateUp64     = Tile<64, 128, 2, 2, 3, true, true>;
+using GateUp128    = Tile<128, 256, 2, 4, 3, true>;
+template <bool F32> using Plain16x64 = Tile<16, 64, 1, 4, 6, false, true, F32>;
+template <bool F32> using Plain32x64Deep = Tile<32, 64, 2, 2, 6, false, true, F32>;
+template <bool F32> using Plain32x64 = Tile<32, 64, 2, 2, 3, false, true, F32>;
+template <bool F32> using Plain64x64 = Tile<64, 64, 2, 2, 4, false, true, F32>;
+template <bool F32> using Plain64x128 = Tile<64, 128, 2, 2, 3, false, true, F32>;
+template <bool F32> using Plain128x128 = Tile<128, 128, 2, 2, 4, false, false, F32>;
+template <bool F32> using Plain128x128Pair = Tile<128, 128, 2, 2, 2, false, false, F32>;
 
-// ---- a few rows: weights straight to registers, the reduction shared by the wavefronts of a workgroup -----------------------
-// A tile is 16 rows and 16 output columns (with DUAL a block of 32, of both matrices). Its eight wavefronts take contiguous parts
-// of the reduction; the fp32 parts are added in LDS in their order, which K alone decides.
+// ---- a few rows and few tiles: weights straight to registers, the reduction shared by the wavefronts of a workgroup ---------
+// A tile is 16 rows and 16 output columns, so that a projection of a few thousand columns has a workgroup for every compute unit.
+// Its eight wavefronts take contiguous parts of the reduction, two k-steps in flight each; the fp32 parts are added in LDS in
+// their order, which K alone decides. Bound by latency: one row, 14336 x 4096, weights from memory 8.8 us (31 MB, of which 4.8 at
+// 6.5 TB/s), with 16 x 64 tiles 15.3; four k-steps in flight or sixteen wavefronts 8.8 to 9.2, 32 columns 14.5.
 constexpr int kFewWaves = 8, kFewRows = 16;
 
-template <bool DUAL, bool F32>
+template <bool F32>
 __global__ __launch_bounds__(kFewWaves * kWave) void few_rows_kernel(Operands op, Outputs out) {
     using namespace mx4;
-    constexpr int NB = DUAL ? 4 : 1, COLS = DUAL ? 32 : 16;      // weight fragments: 32 columns of W1, the same of W3
-    __shared__ f32x4 part[kFewWaves][NB][kWave];
-    const int NT = op.N / COLS;
+    __shared__ f32x4 part[kFewWaves][kWave];
+    const int NT = op.N / 16;
     const TileCoord tc =
         op.offsets ? gemm::locate_tile<kFewRows>(op.offsets, op.E, NT) : gemm::locate_tile_of_one<kFewRows>(op.R, NT);
     if (tc.expert < 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int frag_row = lane & 15, g = lane >> 4;
     const uint32_t pitch = static_cast<uint32_t>(op.K) / 2;
-    const int runs = mx_runs(op.K), col0 = tc.nt * COLS;
+    const int runs = mx_runs(op.K), col0 = tc.nt * 16;
     const int first = wave * runs / kFewWaves, last = (wave + 1) * runs / kFewWaves;
 
     const __amdgpu_buffer_rsrc_t a = resource(op.a + static_cast<size_t>(tc.row0) * pitch, tc.rows * pitch);
-    __amdgpu_buffer_rsrc_t b[NB];
-    const uint8_t* b_scale[NB];
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
-        const int m = DUAL ? j >> 1 : 0, col = col0 + (DUAL ? (j & 1) * 16 : 0);
-        b[j] = resource(op.b[m] + (static_cast<size_t>(tc.expert) * op.N + col) * pitch, 16 * pitch);
-        b_scale[j] = op.b_scale[m] + (static_cast<size_t>(tc.expert) * runs * op.N + col) * kMxRunBytes;
-    }
+    const __amdgpu_buffer_rsrc_t b = resource(op.b[0] + (static_cast<size_t>(tc.expert) * op.N + col0) * pitch, 16 * pitch);
+    const uint8_t* a_scale = op.a_scale + static_cast<size_t>(tc.row0) * kMxRunBytes;
+    const uint8_t* b_scale = op.b_scale[0] + (static_cast<size_t>(tc.expert) * runs * op.N + col0) * kMxRunBytes;
     const uint32_t voff = frag_row * pitch + g * 16, soff = frag_row * kMxRunBytes + 2 * g;
     const bool row_in = frag_row < tc.rows;
 
-    f32x4 acc[NB];
-#pragma unroll
-    for (int j = 0; j < NB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    struct Run { i32x4 a[2], b[NB][2]; int as, bs[NB]; } held[2];
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    struct Run { i32x4 a[2], b[2]; int as, bs; } held[2];
     auto load = [&](Run& r, int run) {
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                r.b[j][h] = __builtin_amdgcn_raw_buffer_load_b128(b[j], voff + h * 64, run * 128, 2);
-            r.bs[j] = *reinterpret_cast<const uint16_t*>(b_scale[j] + static_cast<size_t>(run) * op.N * kMxRunBytes + soff);
-        }
+        for (int h = 0; h < 2; ++h) r.b[h] = __builtin_amdgcn_raw_buffer_load_b128(b, voff + h * 64, run * 128, 2);
+        r.bs = *reinterpret_cast<const uint16_t*>(b_scale + static_cast<size_t>(run) * op.N * kMxRunBytes + soff);
 #pragma unroll
         for (int h = 0; h < 2; ++h) r.a[h] = __builtin_amdgcn_raw_buffer_load_b128(a, voff + h * 64, run * 128, 0);
-        r.as = row_in ? *reinterpret_cast<const uint16_t*>(
-                            op.a_scale + (static_cast<size_t>(run) * op.R + tc.row0) * kMxRunBytes + soff) : 0;
+        r.as = row_in ? *reinterpret_cast<const uint16_t*>(a_scale + static_cast<size_t>(run) * op.R * kMxRunBytes + soff) : 0;
     };
     auto multiply = [&](const Run& r) {
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            acc[j] = mma<0>(r.b[j][0], r.a[0], acc[j], r.bs[j], r.as);
-            acc[j] = mma<1>(r.b[j][1], r.a[1], acc[j], r.bs[j], r.as);
-        }
+        acc = mma<0>(r.b[0], r.a[0], acc, r.bs, r.as);
+        acc = mma<1>(r.b[1], r.a[1], acc, r.bs, r.as);
     };
     if (first < last) load(held[0], first);
     for (int p = first; p < last; p += 2) {
@@ -88,39 +81,20 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_rows_kernel(Operands op
         if (p + 2 < last) load(held[0], p + 2);
         multiply(held[1]);
     }
-#pragma unroll
-    for (int j = 0; j < NB; ++j) part[wave][j][lane] = acc[j];
+    part[wave][lane] = acc;
     __syncthreads();
-    if (wave != 0) return;
-    f32x4 sum[NB];
+    if (wave != 0 || !row_in) return;
+    f32x4 sum = part[0][lane];
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-        sum[j] = part[0][j][lane];
-#pragma unroll
-        for (int w = 1; w < kFewWaves; ++w) sum[j] += part[w][j][lane];
-    }
-    const size_t row = static_cast<size_t>(tc.row0) + frag_row;
-    if constexpr (DUAL) {
-        float v[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = gemm::silu(sum[q / 4][q & 3]) * sum[2 + q / 4][q & 3];
-        uint32_t scale;
-        int at;
-        const uint32_t codes = block_codes(v, g, scale, at);
-        if (!row_in) return;
-        *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(out.c) + row * (op.N / 2) + col0 / 2 + at * 4) = codes;
-        if (g == 0) store_scale(out.scale, op.R, row, col0 / 32, op.N / 32, scale);
+    for (int w = 1; w < kFewWaves; ++w) sum += part[w][lane];
+    const size_t at = (static_cast<size_t>(tc.row0) + frag_row) * op.N + col0 + 4 * g;
+    if constexpr (F32) {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(out.c) + at) = sum;
     } else {
-        if (!row_in) return;
-        const size_t at = row * op.N + col0 + 4 * g;
-        if constexpr (F32) {
-            *reinterpret_cast<f32x4*>(static_cast<float*>(out.c) + at) = sum[0];
-        } else {
-            gemm::bf16x4 o;
+        gemm::bf16x4 o;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) o[q] = static_cast<__bf16>(sum[0][q]);
-            *reinterpret_cast<gemm::bf16x4*>(static_cast<uint16_t*>(out.c) + at) = o;
-        }
+        for (int q = 0; q < 4; ++q) o[q] = static_cast<__bf16>(sum[q]);
+        *reinterpret_cast<gemm::bf16x4*>(static_cast<uint16_t*>(out.c) + at) = o;
     }
 }
 
@@ -174,33 +148,30 @@ int large_of(const GemmEnv& env, const Operands& op, const Outputs& out, hipStre
                   env.tile_counters);
 }
 template <class Cfg>
-bool large_fits(const Operands& op) { return op.K > 512 && op.N >= Cfg::BN_OUT; }
-template <class Cfg>
 int large(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
-    if (!large_fits<Cfg>(op)) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (op.K <= 512 || op.N < Cfg::BN_OUT) return MOE_ERR_UNSUPPORTED_SHAPE;
     return mx_runs(op.K) & 1 ? large_of<Cfg, true>(env, op, out, s) : large_of<Cfg, false>(env, op, out, s);
 }
 
-template <bool DUAL, bool F32>
+template <bool F32>
 int few_rows(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
     static std::atomic<uint64_t> attr_set{0};
-    return launch(env, attr_set, few_rows_kernel<DUAL, F32>, 0, kFewWaves * kWave,
-                  most_row_tiles(op.R, op.E, kFewRows) * (op.N / (DUAL ? 32 : 16)), s, op, out);
-}
-
-// Rows of a group: the average and two standard deviations of a uniform routing.
-double upper_rows(int R, int E) {
-    const double avg = static_cast<double>(R) / E;
-    return E == 1 ? avg : avg + 2.0 * std::sqrt(avg);
+    return launch(env, attr_set, few_rows_kernel<F32>, 0, kFewWaves * kWave, most_row_tiles(op.R, op.E, kFewRows) * (op.N / 16), s, op, out);
 }
 
 template <bool F32>
 int product(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
-    const double rows = upper_rows(op.R, op.E);
-    if (rows <= 16.0) return few_rows<false, F32>(env, op, out, s);
-    if (rows <= 64.0) return ring<Plain32<F32>>(env, op, out, s);
-    if (rows <= 128.0 || !large_fits<PlainLarge<F32>>(op)) return ring<Plain128<F32>>(env, op, out, s);
-    return large<PlainLarge<F32>>(env, op, out, s);
+    switch (mx_plain_tile(op.R, op.E, op.N, op.K, compute_units(env.device))) {
+        case kMxFew: return few_rows<F32>(env, op, out, s);
+        case kMx16x64: return ring<Plain16x64<F32>>(env, op, out, s);
+        case kMx32x64Deep: return ring<Plain32x64Deep<F32>>(env, op, out, s);
+        case kMx32x64: return ring<Plain32x64<F32>>(env, op, out, s);
+        case kMx64x64: return ring<Plain64x64<F32>>(env, op, out, s);
+        case kMx64x128: return ring<Plain64x128<F32>>(env, op, out, s);
+        case kMx128x128: return ring<Plain128x128<F32>>(env, op, out, s);
+        case kMx128x128Pair: return ring<Plain128x128Pair<F32>>(env, op, out, s);
+        default: return large<PlainLarge<F32>>(env, op, out, s);
+    }
 }
 
 }  // namespace
@@ -210,11 +181,12 @@ int launch_gateup_mx4(const GemmEnv& env, const moe_mx4* x, const moe_e8m0* x_sc
                       moe_mx4* H, moe_e8m0* h_scale, hipStream_t s) {
     const Operands op{x, x_scale, {W1, W3}, {w1_scale, w3_scale}, offsets, R, E, f, d};
     const Outputs out{H, h_scale};
-    const double rows = upper_rows(R, E);
-    if (rows <= 16.0) return few_rows<true, false>(env, op, out, s);
-    if (rows <= 64.0) return ring<GateUp32>(env, op, out, s);
-    if (rows <= 128.0 || !large_fits<GateUpLarge>(op)) return ring<GateUp128>(env, op, out, s);
-    return large<GateUpLarge>(env, op, out, s);
+    switch (mx_gateup_tile(R, E, f, d, compute_units(env.device))) {
+        case kMxGate32: return ring<GateUp32>(env, op, out, s);
+        case kMxGate64: return ring<GateUp64>(env, op, out, s);
+        case kMxGate128: return ring<GateUp128>(env, op, out, s);
+        default: return large<GateUpLarge>(env, op, out, s);
+    }
 }
 
 int launch_product_mx4(const GemmEnv& env, const moe_mx4* x, const moe_e8m0* x_scale, const int32_t* offsets, int R, int N,

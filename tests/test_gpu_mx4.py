@@ -20,15 +20,18 @@ def cuda(a):
     return torch.from_numpy(np.ascontiguousarray(a)).cuda()
 
 
-def rows_of(rng, R, K, spread=3):
-    """Rows in 4 bits with blocks of different magnitudes: (codes, scales by block, numbers)."""
+def rows_of(rng, R, K, spread=3, random=False):
+    """Rows in 4 bits with blocks of different magnitudes: (codes, scales by block, numbers); random: codes at random."""
+    if random:
+        q, s = rng.integers(0, 256, (R, K // 2), np.uint8), rng.integers(125, 128, (R, K // 32), np.uint8)
+        return q, s, M.decode(q, s)
     x = rng.standard_normal((R, K)) * np.exp2(rng.integers(-spread, spread + 1, (R, K // 32))).repeat(32, 1)
     q, s = M.quantize(x)
     return q, s, M.decode(q, s)
 
 
-def matrices_of(rng, E, N, K):
-    parts = [rows_of(rng, N, K) for _ in range(E)]
+def matrices_of(rng, E, N, K, random=False):
+    parts = [rows_of(rng, N, K, random=random) for _ in range(E)]
     return (cuda(np.stack([p[0] for p in parts])), cuda(np.stack([M.arrange(p[1]) for p in parts])),
             np.stack([p[2] for p in parts]))
 
@@ -194,13 +197,13 @@ def in_4_bits(h, peak):
     return (np.sign(blocks) * M.VALUES[M.codes_of(blocks / unit)] * unit).reshape(h.shape)
 
 
-def check_experts(T, d, f, E, k, seed=0, off=None):
+def check_experts(T, d, f, E, k, seed=0, off=None, random=False):
     rng = np.random.default_rng(seed + T + d + f + E)
     R = T * k
-    q, s, x = rows_of(rng, R, d, spread=1)
-    w1, s1, v1 = matrices_of(rng, E, f, d)
-    w3, s3, v3 = matrices_of(rng, E, f, d)
-    w2, s2, v2 = matrices_of(rng, E, d, f)
+    q, s, x = rows_of(rng, R, d, 1, random)
+    w1, s1, v1 = matrices_of(rng, E, f, d, random)
+    w3, s3, v3 = matrices_of(rng, E, f, d, random)
+    w2, s2, v2 = matrices_of(rng, E, d, f, random)
     off = offsets_of(rng, R, E) if off is None else off
     ctx = B.MoeContext(T, d, f, E, k)
     y = torch.empty((R, d), dtype=torch.bfloat16, device="cuda")
@@ -449,3 +452,50 @@ def test_refusals():
         B.moe_route_scored_from_logits(many, torch.zeros((4, 256), device="cuda"), None, B.MoeScoring("sigmoid", groups=128, top_groups=4),
                                        4, idx, w)
     many.close()
+
+
+# ---- every tile, at sizes too large for the host -----------------------------------------------------
+
+from mx4_sizes import GATEUP, PLAIN  # noqa: E402
+
+
+def random_rows(g, *lead):
+    """Codes at random and scales of five magnitudes, on the GPU: (codes, arranged scales, numbers in 64 bits)."""
+    *front, rows, K = lead
+    q = torch.randint(0, 256, (*front, rows, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    blocks = K // 32
+    s = torch.randint(125, 130, (*front, rows, blocks), generator=g, device="cuda", dtype=torch.uint8)
+    whole = torch.zeros((*front, rows, M.runs(K) * 8), dtype=torch.uint8, device="cuda")
+    whole[..., :blocks] = s
+    arranged = whole.view(*front, rows, -1, 2, 4).transpose(-1, -2).movedim(-4, -3).reshape(*front, -1, rows, 8).contiguous()
+    values = torch.tensor(np.concatenate([M.VALUES, -M.VALUES]), device="cuda")
+    v = values[torch.stack((q & 15, q >> 4), dim=-1).long()].flatten(-2)
+    return q, arranged, (v.view(*front, rows, blocks, 32) * torch.exp2(s.double() - 127)[..., None]).flatten(-2)
+
+
+@pytest.mark.parametrize("R,E,N,K", PLAIN)
+def test_product_of_every_tile(R, E, N, K):
+    g = torch.Generator(device="cuda").manual_seed(R + E + N + K)
+    rng = np.random.default_rng(R + E + N + K)
+    q, s, x = random_rows(g, R, K)
+    off = np.array([0, R], np.int32) if E == 1 else offsets_of(rng, R, E)
+    w = [random_rows(g, N, K) for _ in range(E)]
+    ctx = B.MoeContext(R, 512, 128, E, 1)
+    out = torch.full((R + 2, N), 9.0, device="cuda")
+    print(f"gemm R={R} E={E} N={N} K={K}", flush=True)
+    for _ in range(2):                               # the second call finds counters as the first one left them
+        out[:R] = 3.0
+        B.moe_gemm_mx4(ctx, q, s, None if E == 1 else cuda(off), R, E, N, K, torch.stack([m[0] for m in w]),
+                       torch.stack([m[1] for m in w]), out[:R])
+        assert (out[R:] == 9).all()
+        for e in range(E):
+            r = slice(int(off[e]), int(off[e + 1]))
+            want = x[r] @ w[e][2].t()
+            tol = sum_error(K) * (x[r].abs() @ w[e][2].abs().t()) + U * want.abs() * (1 + 1e-6)
+            assert ((out[r].double() - want).abs() <= tol).all(), (e, (out[r].double() - want).abs().max())
+    ctx.close()
+
+
+@pytest.mark.parametrize("R,E,f,d", GATEUP)
+def test_experts_of_every_tile(R, E, f, d):
+    check_experts(R, d, f, E, 1, seed=1, random=True)
