@@ -7,7 +7,9 @@
 // A token belongs to LPT lanes of a wavefront (16, or 64 where there are few tokens), and inside them every group of experts
 // to L lanes of its own, so that a group's best two are found by moves among those lanes and a group is kept or dropped by its
 // own lanes. Selection is k rounds of a maximum over the token's lanes, on integers of the scores' order (route_select.h).
-// The weights are formed from the selected experts' logits once more: a slot's lane reads its own.
+// The weights are formed from the selected experts' logits once more: a slot's lane reads its own. No result depends on the
+// number of lanes. Bound by the chain of the rounds (0.2 us each for one token) and, with many tokens, by their instructions: 8192 tokens
+// of 256 experts read 8.4 MB, 1.4 us of the 9.6.
 #include <algorithm>
 
 #include "route_select.h"
@@ -28,21 +30,65 @@ struct ScoredArgs {
     float* weight;                   // [T, k]
 };
 
-// Over the LPT lanes of a token, in all of them: butterflies by row moves (distances inside 16 lanes) and shuffles.
-template <int LPT, class Op>
-__device__ __forceinline__ uint32_t over_token(uint32_t v, Op&& op) {
-    v = over_16_lanes(v, op);
-    if constexpr (LPT == 64) {
-        v = op(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 16)));
-        v = op(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), 32)));
+// f(a, b) of a value and the one S lanes away for S = 1, 2, 4 .. 32, for symmetric f and values that the lanes of every S share
+// already (the partner at 4 and 8 is then any lane of the other half: the mirrored one).
+template <int S, class F>
+__device__ __forceinline__ auto with_partner(uint32_t v, F&& f) {
+    constexpr int CTRL = S == 1 ? 0xb1 : S == 2 ? 0x4e : S == 4 ? 0x141 : 0x140;      // quad_perm, row_half_mirror, row_mirror
+    if constexpr (S < 16) {
+        return f(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, 0xf, 0xf, false)));
+    } else if constexpr (S == 16) {
+        const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return f(p[0], p[1]);
+    } else {
+        const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return f(p[0], p[1]);
     }
-    return v;
 }
-template <int LPT, class T>
-__device__ __forceinline__ T sum_over_token(T v) {
-#pragma unroll
-    for (int s = LPT / 2; s > 0; s >>= 1) v += __shfl_xor(v, s);
-    return v;
+struct Pair { uint32_t lo, hi; };
+template <int S>
+__device__ __forceinline__ Pair partners(uint32_t v) {
+    return with_partner<S>(v, [](uint32_t x, uint32_t y) { return Pair{x, y}; });
+}
+template <int LPT, int S = 1>
+__device__ __forceinline__ uint32_t max_over_token(uint32_t v) {
+    if constexpr (S < LPT) return max_over_token<LPT, 2 * S>(with_partner<S>(v, [](uint32_t x, uint32_t y) { return max(x, y); }));
+    else return v;
+}
+template <int LPT, int S = 1>
+__device__ __forceinline__ uint32_t min_over_token(uint32_t v) {
+    if constexpr (S < LPT) return min_over_token<LPT, 2 * S>(with_partner<S>(v, [](uint32_t x, uint32_t y) { return min(x, y); }));
+    else return v;
+}
+// The sum in the order of the distances 1, 2, 4, ..
+template <int LPT, int S = 1>
+__device__ __forceinline__ float sum_over_token(float v) {
+    if constexpr (S < LPT) {
+        const Pair p = partners<S>(__float_as_uint(v));
+        return sum_over_token<LPT, 2 * S>(__uint_as_float(p.lo) + __uint_as_float(p.hi));
+    } else {
+        return v;
+    }
+}
+template <int LPT, int S = 1>
+__device__ __forceinline__ double sum_over_token(double v) {
+    if constexpr (S < LPT) {
+        const Pair lo = partners<S>(__double2loint(v)), hi = partners<S>(__double2hiint(v));
+        return sum_over_token<LPT, 2 * S>(__hiloint2double(hi.lo, lo.lo) + __hiloint2double(hi.hi, lo.hi));
+    } else {
+        return v;
+    }
+}
+// A group's two largest over its L lanes.
+template <int LPT, int S = 1>
+__device__ __forceinline__ void two_largest(uint32_t& first, uint32_t& second, int L) {
+    if constexpr (S < LPT) {
+        if (S >= L) return;
+        const Pair f = partners<S>(first), g = partners<S>(second);
+        second = max(min(f.lo, f.hi), max(g.lo, g.hi));
+        first = max(f.lo, f.hi);
+        two_largest<LPT, 2 * S>(first, second, L);
+    }
 }
 
 __device__ __forceinline__ float sigmoid(float l) { return 1.f / (1.f + expf(-l)); }
@@ -50,29 +96,53 @@ __device__ __forceinline__ float sigmoid(float l) { return 1.f / (1.f + expf(-l)
 __device__ __forceinline__ float exp_below(float l, float top) { return l == top ? 1.f : expf(l - top); }
 __device__ __forceinline__ float number(float l) { return l != l ? -INFINITY : l; }      // a NaN counts as -infinity
 
-template <int LPT, int EW>
+// A lane's EW experts of its group: every L-th one, or (QUADS) runs of four, every L-th of those, which it loads 16 bytes at a time.
+template <bool QUADS>
+__device__ __forceinline__ int in_group(int i, int j, int L) {
+    return QUADS ? ((i >> 2) * L + j) * 4 + (i & 3) : i * L + j;
+}
+template <int EW, bool QUADS>
+__device__ __forceinline__ void load_experts(float (&v)[EW], const bool (&has)[EW], const float* from, int j, int L, float none) {
+    if constexpr (QUADS) {
+#pragma unroll
+        for (int i = 0; i < EW; i += 4) {
+            float4 q = {none, none, none, none};
+            if (has[i]) q = *reinterpret_cast<const float4*>(from + in_group<true>(i, j, L));
+            v[i] = q.x;
+            v[i + 1] = q.y;
+            v[i + 2] = q.z;
+            v[i + 3] = q.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < EW; ++i) v[i] = has[i] ? from[in_group<false>(i, j, L)] : none;
+    }
+}
+
+template <int LPT, int EW, bool QUADS>
 __global__ __launch_bounds__(256) void route_scored_kernel(ScoredArgs a) {
     constexpr int PER = kWave / LPT, SLOTS = kWave / LPT;      // tokens of a wavefront; slots of a lane (k <= 64)
-    const int lane = threadIdx.x & (LPT - 1), base = threadIdx.x & (kWave - 1) & ~(LPT - 1);
+    const int lane = threadIdx.x & (LPT - 1);
     const int t_of = (blockIdx.x * 4 + threadIdx.x / kWave) * PER + (threadIdx.x & (kWave - 1)) / LPT;
+    if (LPT == kWave && t_of >= a.T) return;                   // a whole wavefront
     const int t = min(t_of, a.T - 1);                          // all lanes stay for the moves between them
     const float* row = a.logits + static_cast<size_t>(t) * a.E;
     const int L = 1 << a.lane_shift, g = lane >> a.lane_shift, j = lane & (L - 1);
 
-    float c[EW];
+    float c[EW], add[EW];
     bool has[EW];
 #pragma unroll
-    for (int i = 0; i < EW; ++i) {
-        const int at = i * L + j;
-        has[i] = g < a.groups && at < a.size;
-        c[i] = has[i] ? number(row[g * a.size + at]) : -INFINITY;
-    }
+    for (int i = 0; i < EW; ++i) has[i] = g < a.groups && in_group<QUADS>(i, j, L) < a.size;
+    load_experts<EW, QUADS>(c, has, row + g * a.size, j, L, -INFINITY);
+    if (a.correction != nullptr) load_experts<EW, QUADS>(add, has, a.correction + g * a.size, j, L, 0.f);
+#pragma unroll
+    for (int i = 0; i < EW; ++i) c[i] = number(c[i]);
     float top = 0.f, total = 1.f;
     if (!a.sigmoid) {
         uint32_t key = 0;
 #pragma unroll
         for (int i = 0; i < EW; ++i) key = max(key, logit_key(c[i]));
-        top = key_logit(over_token<LPT>(key, [](uint32_t x, uint32_t y) { return max(x, y); }));
+        top = key_logit(max_over_token<LPT>(key));
         // In multiples of 2^-44, to which a double near 256 rounds: the sum of up to 256 of them, each at most 1, is exact,
         // so its one rounding to fp32 is the same however the experts lie on the lanes.
         double sum = 0.0;
@@ -87,7 +157,7 @@ __global__ __launch_bounds__(256) void route_scored_kernel(ScoredArgs a) {
 #pragma unroll
     for (int i = 0; i < EW; ++i) {
         float s = a.sigmoid ? sigmoid(c[i]) : c[i] / total;
-        if (a.correction != nullptr && has[i]) s += a.correction[g * a.size + i * L + j];
+        if (a.correction != nullptr) s += add[i];
         key[i] = has[i] ? logit_key(s) : 0u;
     }
 
@@ -98,17 +168,14 @@ __global__ __launch_bounds__(256) void route_scored_kernel(ScoredArgs a) {
             second = max(second, min(first, key[i]));
             first = max(first, key[i]);
         }
-        for (int s = 1; s < L; s <<= 1) {
-            const uint32_t f = static_cast<uint32_t>(__shfl_xor(static_cast<int>(first), s));
-            const uint32_t h = static_cast<uint32_t>(__shfl_xor(static_cast<int>(second), s));
-            second = max(min(first, f), max(second, h));
-            first = max(first, f);
-        }
+        two_largest<LPT>(first, second, L);
         uint32_t value = first;
         if (a.two_best && a.size > 1) value = logit_key(key_logit(first) + key_logit(second));
+        const int base = threadIdx.x & (kWave - 1) & ~(LPT - 1);
         int better = 0;                                        // groups ahead of this one
         for (int o = 0; o < a.groups; ++o) {
-            const uint32_t v = static_cast<uint32_t>(__shfl(static_cast<int>(value), base + (o << a.lane_shift)));
+            const uint32_t v = LPT == kWave ? __builtin_amdgcn_readlane(value, o << a.lane_shift)
+                                            : static_cast<uint32_t>(__shfl(static_cast<int>(value), base + (o << a.lane_shift)));
             better += v > value || (v == value && o < g) ? 1 : 0;
         }
 #pragma unroll
@@ -117,21 +184,49 @@ __global__ __launch_bounds__(256) void route_scored_kernel(ScoredArgs a) {
 
     int slot_of[SLOTS] = {};                                   // lane l keeps slots l, l + LPT, ...
     for (int s = 0; s < a.k; ++s) {
-        uint32_t best = key[0];
+        uint32_t own = key[0];
 #pragma unroll
-        for (int i = 1; i < EW; ++i) best = max(best, key[i]);
-        best = over_token<LPT>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
-        uint32_t e = 0xffffffffu;                              // the lowest index that has it
+        for (int i = 1; i < EW; ++i) own = max(own, key[i]);
+        const uint32_t best = max_over_token<LPT>(own);
+        if constexpr (LPT == kWave) {
+            // The lowest index that has it, on the scalar unit: of the first group that has it the first i (with QUADS four of
+            // them), of those the first lane.
+            uint64_t in[EW], any = 0;
 #pragma unroll
-        for (int i = 0; i < EW; ++i)
-            e = min(e, key[i] == best ? static_cast<uint32_t>(g * a.size + i * L + j) : 0xffffffffu);
-        const uint32_t mine = e;
-        e = over_token<LPT>(e, [](uint32_t x, uint32_t y) { return min(x, y); });
+            for (int i = 0; i < EW; ++i) any |= in[i] = __ballot(key[i] == best);
+            const int found = __builtin_ctzll(any) >> a.lane_shift, first = found << a.lane_shift;
+            const uint64_t group = (L == kWave ? ~0ull : ((1ull << L) - 1)) << first;
+            constexpr int STEP = QUADS ? 4 : 1;
+            int which = 0, from = 0;
 #pragma unroll
-        for (int i = 0; i < EW; ++i)
-            key[i] = mine == e && e == static_cast<uint32_t>(g * a.size + i * L + j) ? 0u : key[i];
+            for (int i = EW - STEP; i >= 0; i -= STEP) {
+                uint64_t of = in[i];
 #pragma unroll
-        for (int q = 0; q < SLOTS; ++q) slot_of[q] = s == q * LPT + lane ? static_cast<int>(e) : slot_of[q];
+                for (int n = 1; n < STEP; ++n) of |= in[i + n];
+                of &= group;
+                if (of != 0) {
+                    from = __builtin_ctzll(of);
+                    which = i;
+#pragma unroll
+                    for (int n = STEP - 1; n >= 0; --n) which = (in[i + n] >> from) & 1 ? i + n : which;
+                }
+            }
+            const int e = found * a.size + in_group<QUADS>(which, from - first, L);
+#pragma unroll
+            for (int i = 0; i < EW; ++i) key[i] = i == which && lane == from ? 0u : key[i];
+            slot_of[0] = s == lane ? e : slot_of[0];
+        } else {
+            int at = 0;                                        // the lane's first one that has it
+#pragma unroll
+            for (int i = EW - 1; i >= 0; --i) at = key[i] == best ? i : at;
+            const uint32_t mine = own == best ? static_cast<uint32_t>(g * a.size + in_group<QUADS>(at, j, L)) : 0xffffffffu;
+            const uint32_t e = min_over_token<LPT>(mine);
+            at = e == mine ? at : -1;
+#pragma unroll
+            for (int i = 0; i < EW; ++i) key[i] = at == i ? 0u : key[i];
+#pragma unroll
+            for (int q = 0; q < SLOTS; ++q) slot_of[q] = s == q * LPT + lane ? static_cast<int>(e) : slot_of[q];
+        }
     }
 
     float w[SLOTS];
@@ -143,10 +238,11 @@ __global__ __launch_bounds__(256) void route_scored_kernel(ScoredArgs a) {
             w[q] = a.sigmoid ? sigmoid(l) : exp_below(l, top) / total;
         }
     }
-    if (a.renormalise) {                                       // slots 32 apart first, then 16, 8, 4, 2, 1
-        float sum = w[0];
-        if constexpr (SLOTS == 4) sum = (w[0] + w[2]) + (w[1] + w[3]);
-        sum = sum_over_token<LPT>(sum);
+    if (a.renormalise) {                                       // slots 1, 2, 4, 8 apart, then 16, then 32
+        float part[4] = {};
+#pragma unroll
+        for (int q = 0; q < SLOTS; ++q) part[q] = a.k > q * LPT ? sum_over_token<LPT>(w[q]) : 0.f;
+        const float sum = (part[0] + part[1]) + (part[2] + part[3]);
 #pragma unroll
         for (int q = 0; q < SLOTS; ++q) w[q] = sum > 0.f ? w[q] / sum : 0.f;
     }
@@ -161,10 +257,10 @@ __global__ __launch_bounds__(256) void route_scored_kernel(ScoredArgs a) {
     }
 }
 
-template <int LPT, int EW>
+template <int LPT, int EW, bool QUADS>
 int launch(const ScoredArgs& a, hipStream_t s) {
     constexpr int PER = 4 * kWave / LPT;
-    hipLaunchKernelGGL((route_scored_kernel<LPT, EW>), dim3(static_cast<unsigned>((a.T + PER - 1) / PER)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((route_scored_kernel<LPT, EW, QUADS>), dim3(static_cast<unsigned>((a.T + PER - 1) / PER)), dim3(256), 0, s, a);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
@@ -182,13 +278,31 @@ int launch_route_scored(const float* logits, const float* correction, const moe_
     if (T == 0) return MOE_OK;
     ScoredArgs a{logits, correction, T, E, k, sc.groups, E / sc.groups, 0, sc.top_groups, sc.group_best == 2,
                  sc.score == MOE_SCORE_SIGMOID, sc.renormalise != 0, sc.scale, topk_idx, topk_w};
-    const int lpt = T <= 2048 || group_lanes(a.groups, 16) == 0 ? 64 : 16;
+    // us, 16 | 64 lanes: 256 experts in 8 groups, one token 7.6 | 4.1, 2000 8.1 | 5.3, 4000 8.2 | 7.0, 8192 9.8 | 10.4, 16384 14.5 |
+    // 17.6; 64 experts, softmax, 5003 tokens 4.2 | 4.5, 16384 5.9 | 9.1. (32 lanes are between the two but for 8192 tokens: 9.1.)
+    const int lpt = T <= 4096 || group_lanes(a.groups, 16) == 0 ? 64 : 16;
     const int L = group_lanes(a.groups, lpt);
     while ((2 << a.lane_shift) <= L) ++a.lane_shift;
-    const int held = (a.size + L - 1) / L;           // of a lane
-    if (lpt == 64) return held <= 1 ? launch<64, 1>(a, s) : held <= 4 ? launch<64, 4>(a, s) : launch<64, 8>(a, s);
-    return held <= 4 ? launch<16, 4>(a, s) : held <= 8 ? launch<16, 8>(a, s) : held <= 16 ? launch<16, 16>(a, s)
-                                                                                        : launch<16, 32>(a, s);
+    const int held = (a.size + L - 1) / L;           // of a lane, where it takes every L-th expert
+    const bool quads = a.size % 4 == 0 && held > 2 && ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(correction)) & 15) == 0;
+    if (quads) {
+        const int runs = (a.size / 4 + L - 1) / L;   // of four
+        if (lpt == 64) return runs <= 1 ? launch<64, 4, true>(a, s) : launch<64, 8, true>(a, s);
+        return runs <= 1   ? launch<16, 4, true>(a, s)
+               : runs <= 2 ? launch<16, 8, true>(a, s)
+               : runs <= 4 ? launch<16, 16, true>(a, s)
+                           : launch<16, 32, true>(a, s);
+    }
+    if (lpt == 64)
+        return held <= 1   ? launch<64, 1, false>(a, s)
+               : held <= 2 ? launch<64, 2, false>(a, s)
+               : held <= 4 ? launch<64, 4, false>(a, s)
+                           : launch<64, 8, false>(a, s);
+    return held <= 1   ? launch<16, 1, false>(a, s)
+           : held <= 4 ? launch<16, 4, false>(a, s)
+           : held <= 8 ? launch<16, 8, false>(a, s)
+           : held <= 16 ? launch<16, 16, false>(a, s)
+                        : launch<16, 32, false>(a, s);
 }
 
 }  // namespace moe

@@ -61,13 +61,11 @@ def check(logits, correction, k, **kw):
 
 
 @pytest.mark.parametrize("score", ["sigmoid", "softmax"])
-@pytest.mark.parametrize("T", [1, 5, 64, 2048, 2049, 3001])
+@pytest.mark.parametrize("T", [1, 5, 64, 4096, 4099])
 @pytest.mark.parametrize("E,k,groups,top_groups,group_best", [
     (256, 8, 8, 4, 2), (64, 6, 1, 1, 1), (8, 2, 1, 1, 1), (160, 6, 8, 3, 1), (1, 1, 1, 1, 2), (96, 4, 3, 2, 2), (255, 5, 5, 4, 2),
     (252, 7, 9, 5, 2), (256, 4, 64, 9, 2), (128, 8, 32, 20, 1), (34, 3, 17, 8, 2), (256, 40, 2, 1, 2), (72, 64, 1, 1, 2)])
 def test_scores_and_groups(score, T, E, k, groups, top_groups, group_best):
-    if T > 64 and (E, k) in ((1, 1), (34, 3), (8, 2)) or T == 3001 and k > 8:
-        T = min(T, 300)
     rng = np.random.default_rng(E * 1000 + T + k)
     correction = (rng.standard_normal(E) * 0.05).astype(np.float32) if (E + T) % 2 else None
     logits = gapped_logits(rng, T, E, score, correction, groups, top_groups, group_best, k)
@@ -75,7 +73,7 @@ def test_scores_and_groups(score, T, E, k, groups, top_groups, group_best):
           renormalise=bool(T % 2), scale=2.5)
 
 
-@pytest.mark.parametrize("T", [3, 2100])
+@pytest.mark.parametrize("T", [3, 4200])
 @pytest.mark.parametrize("E,k,groups,top_groups", [(64, 6, 4, 2), (256, 8, 8, 4), (40, 5, 1, 1)])
 def test_ties_go_to_the_lowest_index(T, E, k, groups, top_groups):
     """Few different logits: equal ones have equal scores, and groups equal sums, whatever the rounding."""
@@ -86,7 +84,7 @@ def test_ties_go_to_the_lowest_index(T, E, k, groups, top_groups):
         check(np.zeros((T, E), np.float32), None, k, score=score, groups=groups, top_groups=top_groups, group_best=2)
 
 
-@pytest.mark.parametrize("T", [9, 2200])
+@pytest.mark.parametrize("T", [9, 4300])
 def test_nan_infinite_and_masked(T):
     rng = np.random.default_rng(T)
     E, k = 64, 6
@@ -116,7 +114,7 @@ def test_nan_infinite_and_masked(T):
 
 def test_results_do_not_depend_on_the_number_of_tokens():
     rng = np.random.default_rng(1)
-    logits = (rng.standard_normal((4096, 256)) * 2).astype(np.float32)
+    logits = (rng.standard_normal((5000, 256)) * 2).astype(np.float32)
     for score in ("sigmoid", "softmax"):
         kw = dict(score=score, groups=8, top_groups=4, group_best=2, renormalise=True, scale=1.5)
         for k in (8, 40):
