@@ -149,7 +149,7 @@ int large_of(const GemmEnv& env, const Operands& op, const Outputs& out, hipStre
 }
 template <class Cfg>
 int large(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
-    if (op.K <= 512 || op.N < Cfg::BN_OUT) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (op.K <= kMxRun || op.N < Cfg::BN_OUT) return MOE_ERR_UNSUPPORTED_SHAPE;
     return mx_runs(op.K) & 1 ? large_of<Cfg, true>(env, op, out, s) : large_of<Cfg, false>(env, op, out, s);
 }
 

@@ -35,6 +35,7 @@ constexpr MxTile kMxGateUpTiles[] = {{kMxGate32,      32,  64,  2,   0.44,   0.8
                                      {kMxGate128,     128, 128, 1,   1.25,   1.4,    7.0},
                                      {kMxGateLarge,   256, 128, 1,   1.0,    1.5,    8.0}};
 constexpr double kMxWeightBytesPerUs = 6.4e6;
+constexpr int kMxRunElements = 256;  // of a k-step
 // The large tiles draw on the board's power: up to this part of the compute units they run at the pace of one alone.
 constexpr double kMxLargeAlone = 0.6;
 
@@ -56,12 +57,12 @@ double mx_price(const MxTile& t, bool large, bool dual, int R, int E, int N, int
     return std::max(us, memory) + 0.2 * std::min(us, memory);
 }
 
-// The large tiles need three k-steps and as many columns as they have.
+// The large tiles need two k-steps and as many columns as they have.
 int mx_plain_tile(int R, int E, int N, int K, int cus) {
     int best = kMxFew;
     double least = 1e30;
     for (const MxTile& t : kMxPlainTiles) {
-        if (t.id == kMxLarge && (K <= 512 || N < t.columns)) continue;
+        if (t.id == kMxLarge && (K <= kMxRunElements || N < t.columns)) continue;
         const double p = mx_price(t, t.id == kMxLarge, false, R, E, N, K, cus);
         if (p < least) { least = p; best = t.id; }
     }
@@ -71,7 +72,7 @@ int mx_gateup_tile(int R, int E, int f, int d, int cus) {
     int best = kMxGate32;
     double least = 1e30;
     for (const MxTile& t : kMxGateUpTiles) {
-        if (t.id == kMxGateLarge && (d <= 512 || f < t.columns)) continue;
+        if (t.id == kMxGateLarge && (d <= kMxRunElements || f < t.columns)) continue;
         const double p = mx_price(t, t.id == kMxGateLarge, true, R, E, f, d, cus);
         if (p < least) { least = p; best = t.id; }
     }
