@@ -95,7 +95,7 @@ int moe_create(moe_ctx** out, const moe_shape* shape, int device_id);
 int moe_destroy(moe_ctx* ctx);
 
 /* Device bytes moe_create() allocates for `shape` (0 for an unsupported shape); what streamed experts, fp32 expert outputs and
- * the 8-bit path need beyond them is allocated by the first call that needs it. */
+ * the 8-bit path need beyond them (the 4-bit path needs nothing) is allocated by the first call that needs it. */
 size_t moe_workspace_bytes(const moe_shape* shape);
 
 /* Static, human-readable name of a status code. */
@@ -290,7 +290,7 @@ int moe_estimate_streamed_stage(const moe_shape* shape, const int32_t* rows, int
  * permutation. Adding 128 keeps the 256-row tiles of a last round that is less than half full
  * whole (by default each is run as two 128-row halves). Adding 256 / 512 runs the 256-row tiles
  * with eight wavefronts of 128 x 64 outputs / four of 128 x 128 (the default). Every setting produces identical bits (same accumulation chain per
- * output element); only speed differs. Returns MOE_ERR_INVALID_ARG for other values. */
+ * output element); only speed differs. 4-bit products do not look at it. Returns MOE_ERR_INVALID_ARG for other values. */
 int moe_set_gemm_config(moe_ctx* ctx, int config);
 
 /* Precision of the expert outputs Yp between the down projection and the combine inside
@@ -451,8 +451,8 @@ int moe_dequantize_mx4(const moe_mx4* q, const moe_e8m0* scale, int32_t T, int32
  * depends on R, E, N and K) and rounded to out's type. offsets [E+1] int32 (device), or NULL with E == 1: all R rows are one
  * group. x [R,K/2] with x_scale [ceil(K/256),R,8]; W [E,N,K/2] with w_scale [E,ceil(K/256),N,8]; out [R,N] of out_type
  * (MOE_OUT_*). x, W and out start at multiples of 16 bytes, the scales at multiples of 8 (else MOE_ERR_INVALID_ARG).
- * R <= T_max * k of the context, whose d_model, d_ff and E play no part here. E <= 256; K a multiple of 32 up to 2^22; N a
- * multiple of 16 up to 2^23; else MOE_ERR_UNSUPPORTED_SHAPE. Rows that no group holds are left as they were. */
+ * R <= T_max * k of the context, whose d_model, d_ff and E play no part here. E <= 256; K a multiple of 32 and N a
+ * multiple of 16, both up to 2^22; else MOE_ERR_UNSUPPORTED_SHAPE. Rows that no group holds are left as they were. */
 int moe_gemm_mx4(moe_ctx* ctx, const moe_mx4* x, const moe_e8m0* x_scale, const int32_t* offsets,
                  int32_t R, int32_t E, int32_t N, int32_t K, const moe_mx4* W, const moe_e8m0* w_scale,
                  void* out, int out_type, void* stream);

@@ -12,7 +12,7 @@ constexpr int kMaxExperts = 256; // four experts per lane in the permutation and
 constexpr int kMaxRowI8 = 65536; // a row in the registers of a workgroup (norm.hip)
 constexpr int kMaxSumI8 = 130944; // products of -128 .. 127 whose sum stays below 2^31, a multiple of 128
 constexpr int kMaxDimI8 = 1 << 23; // widths of outputs, for 32-bit offsets inside a tile
-constexpr int kMaxDimMx4 = 1 << 22; // lengths of rows in 4 bits: 256 rows of a tile stay below 2^30 bytes
+constexpr int kMaxDimMx4 = 1 << 22; // lengths of rows in 4 bits and of fp32 outputs: 128 rows of a tile stay below 2^32 bytes
 constexpr int kMaxGroups = 64;   // of experts: a lane each
 constexpr int kXcds = 8;         // workgroups are dealt round-robin to the 8 XCDs (own L2 each)
 

@@ -894,7 +894,7 @@ int moe_gemm_mx4(moe_ctx* c, const moe_mx4* x, const moe_e8m0* x_scale, const in
         return MOE_ERR_INVALID_ARG;
     if (!on_own_device(c) || E < 1 || N < 1 || K < 1 || (!offsets && E != 1)) return MOE_ERR_INVALID_ARG;
     if (out_type != MOE_OUT_BF16 && out_type != MOE_OUT_FP32) return MOE_ERR_INVALID_ARG;
-    if (E > kMaxExperts || N % 16 != 0 || N > kMaxDimI8 || K % 32 != 0 || K > kMaxDimMx4) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (E > kMaxExperts || N % 16 != 0 || N > kMaxDimMx4 || K % 32 != 0 || K > kMaxDimMx4) return MOE_ERR_UNSUPPORTED_SHAPE;
     if (R == 0) return MOE_OK;
     if (!x || !x_scale || !W || !w_scale || !out) return MOE_ERR_INVALID_ARG;
     if (!at_16_bytes(x, W, out) || !at_8_bytes(x_scale, w_scale)) return MOE_ERR_INVALID_ARG;

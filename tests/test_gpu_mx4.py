@@ -410,6 +410,59 @@ def test_another_stream_and_two_contexts_at_once():
 
 # ---- refusals that need a context -------------------------------------------------------------------
 
+def test_offsets_past_32_bits():
+    """540000 rows of 16384: more than 2^32 bytes of codes and 2^33 elements."""
+    T, d, N, last = 540000, 16384, 64, 300
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.zeros((T, d), dtype=torch.bfloat16, device="cuda")
+    tail = torch.randn((last, d), generator=g, device="cuda").to(torch.bfloat16)
+    x[-last:] = tail
+    q = torch.empty((T, d // 2), dtype=torch.uint8, device="cuda")
+    s = torch.empty((M.runs(d), T, 8), dtype=torch.uint8, device="cuda")
+    B.moe_quantize_mx4(x, q, s)
+    want_q, want_s = torch.empty_like(q[-last:]), torch.empty((M.runs(d), last, 8), dtype=torch.uint8, device="cuda")
+    B.moe_quantize_mx4(tail, want_q, want_s)
+    assert torch.equal(q[-last:], want_q) and torch.equal(s[:, -last:], want_s)
+    B.moe_dequantize_mx4(q, s, x)
+    y = torch.empty_like(tail)
+    B.moe_dequantize_mx4(want_q, want_s, y)
+    assert torch.equal(x[-last:], y) and not x[:-last].any()
+    del x
+    w, ws, wv = random_rows(g, N, d)
+    ctx = B.MoeContext(T, 512, 128, 2, 1)
+    out = torch.full((T, N), 5.0, device="cuda")
+    want = y.double() @ wv.t()
+    tol = sum_error(d) * (y.double().abs() @ wv.abs().t()) + U * want.abs() * (1 + 1e-6)
+    for off in (None, [0, T - last, T]):
+        E = 1 if off is None else 2
+        out.fill_(5.0)
+        B.moe_gemm_mx4(ctx, q, s, None if off is None else cuda(np.array(off, np.int32)), T, E, N, d, w.expand(E, -1, -1).contiguous(),
+                       ws.expand(E, -1, -1, -1).contiguous(), out)
+        assert ((out[-last:].double() - want).abs() <= tol).all() and not out[:-last].any()
+    ctx.close()
+
+
+def test_weights_past_32_bits():
+    """Three experts of 2^18 columns: the last one's weights lie behind 2^32 bytes."""
+    E, N, K, R = 3, 1 << 18, 16384, 50
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q, s, x = random_rows(g, R, K)
+    w = torch.randint(0, 256, (E, N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    ws = torch.full((E, M.runs(K), N, 8), 127, dtype=torch.uint8, device="cuda")
+    ctx = B.MoeContext(R, 512, 128, E, 1)
+    out = torch.empty((R, N), device="cuda")
+    values = torch.tensor(np.concatenate([M.VALUES, -M.VALUES]), device="cuda")
+    for rows in (R, 3):                              # of the last expert
+        B.moe_gemm_mx4(ctx, q, s, cuda(np.array([0, 0, R - rows, R], np.int32)), R, E, N, K, w, ws, out)
+        for e, r in ((1, slice(0, R - rows)), (2, slice(R - rows, R))):
+            cols = slice(N - 40, N)
+            wv = values[torch.stack((w[e, cols] & 15, w[e, cols] >> 4), dim=-1).long()].flatten(-2)
+            want = x[r] @ wv.t()
+            tol = sum_error(K) * (x[r].abs() @ wv.abs().t()) + U * want.abs() * (1 + 1e-6)
+            assert ((out[r, cols].double() - want).abs() <= tol).all()
+    ctx.close()
+
+
 def test_refusals():
     ctx = B.MoeContext(8, 512, 128, 4, 2)
     u8 = lambda *s: torch.zeros(s, dtype=torch.uint8, device="cuda")
