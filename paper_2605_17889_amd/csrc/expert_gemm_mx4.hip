@@ -32,62 +32,78 @@ template <bool F32> using Plain128x128 = Tile<128, 128, 2, 2, 4, false, false, F
 template <bool F32> using Plain128x128Pair = Tile<128, 128, 2, 2, 2, false, false, F32>;
 
 // ---- a few rows and few tiles: weights straight to registers, the reduction shared by the wavefronts of a workgroup ---------
-// A tile is 16 rows and 16 output columns, so that a projection of a few thousand columns has a workgroup for every compute unit.
-// Its eight wavefronts take contiguous parts of the reduction, two k-steps in flight each; the fp32 parts are added in LDS in
-// their order, which K alone decides. Bound by latency: one row, 14336 x 4096, weights from memory 8.8 us (31 MB, of which 4.8 at
-// 6.5 TB/s), with 16 x 64 tiles 15.3; four k-steps in flight or sixteen wavefronts 8.8 to 9.2, 32 columns 14.5.
+// A tile is 16 rows and 16 * CF output columns, so that a projection of a few thousand columns has a workgroup for every compute
+// unit. Its eight wavefronts take contiguous parts of the reduction, DEPTH k-steps in flight each; the fp32 parts are added in LDS
+// in their order, which K alone decides. Bound by latency: one row, 14336 x 4096, weights from memory 9.0 us (31 MB, of which 4.8 at
+// 6.5 TB/s), with two k-steps in flight 9.3, with 16 x 64 tiles 17.6. 32 columns read the rows half as often: 16 rows, 8192 x 8192 11.7
+// -> 10.9 us, 16384 x 6144 20.4 -> 17.4; one row, 14336 x 4096 (128 workgroups) 9.0 -> 13.8.
 constexpr int kFewWaves = 8, kFewRows = 16;
 
-template <bool F32>
+template <bool F32, int CF>
 __global__ __launch_bounds__(kFewWaves * kWave) void few_rows_kernel(Operands op, Outputs out) {
     using namespace mx4;
-    __shared__ f32x4 part[kFewWaves][kWave];
-    const int NT = op.N / 16;
+    constexpr int COLS = 16 * CF, DEPTH = CF == 1 ? 4 : 3;
+    __shared__ f32x4 part[kFewWaves][CF][kWave];
+    const int NT = op.N / COLS;
     const TileCoord tc =
         op.offsets ? gemm::locate_tile<kFewRows>(op.offsets, op.E, NT) : gemm::locate_tile_of_one<kFewRows>(op.R, NT);
     if (tc.expert < 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int frag_row = lane & 15, g = lane >> 4;
     const uint32_t pitch = static_cast<uint32_t>(op.K) / 2;
-    const int runs = mx_runs(op.K), col0 = tc.nt * 16;
+    const int runs = mx_runs(op.K), col0 = tc.nt * COLS;
     const int first = wave * runs / kFewWaves, last = (wave + 1) * runs / kFewWaves;
 
     const __amdgpu_buffer_rsrc_t a = resource(op.a + static_cast<size_t>(tc.row0) * pitch, tc.rows * pitch);
-    const __amdgpu_buffer_rsrc_t b = resource(op.b[0] + (static_cast<size_t>(tc.expert) * op.N + col0) * pitch, 16 * pitch);
+    const __amdgpu_buffer_rsrc_t b = resource(op.b[0] + (static_cast<size_t>(tc.expert) * op.N + col0) * pitch, COLS * pitch);
     const uint8_t* a_scale = op.a_scale + static_cast<size_t>(tc.row0) * kMxRunBytes;
     const uint8_t* b_scale = op.b_scale[0] + (static_cast<size_t>(tc.expert) * runs * op.N + col0) * kMxRunBytes;
     const uint32_t voff = frag_row * pitch + g * 16, soff = frag_row * kMxRunBytes + 2 * g;
     const bool row_in = frag_row < tc.rows;
 
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    struct Run { i32x4 a[2], b[2]; int as, bs; } held[2];
+    f32x4 acc[CF];
+#pragma unroll
+    for (int c = 0; c < CF; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    struct Run { i32x4 a[2], b[CF][2]; int as, bs[CF]; } held[DEPTH];
     auto load = [&](Run& r, int run) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) r.b[h] = __builtin_amdgcn_raw_buffer_load_b128(b, voff + h * 64, run * 128, 2);
-        r.bs = *reinterpret_cast<const uint16_t*>(b_scale + static_cast<size_t>(run) * op.N * kMxRunBytes + soff);
+        for (int c = 0; c < CF; ++c) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                r.b[c][h] = __builtin_amdgcn_raw_buffer_load_b128(b, voff + c * 16 * pitch + h * 64, run * 128, 2);
+            r.bs[c] = *reinterpret_cast<const uint16_t*>(b_scale + static_cast<size_t>(run) * op.N * kMxRunBytes + soff +
+                                                         c * 16 * kMxRunBytes);
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) r.a[h] = __builtin_amdgcn_raw_buffer_load_b128(a, voff + h * 64, run * 128, 0);
         r.as = row_in ? *reinterpret_cast<const uint16_t*>(a_scale + static_cast<size_t>(run) * op.R * kMxRunBytes + soff) : 0;
     };
     auto multiply = [&](const Run& r) {
-        acc = mma<0>(r.b[0], r.a[0], acc, r.bs, r.as);
-        acc = mma<1>(r.b[1], r.a[1], acc, r.bs, r.as);
-    };
-    if (first < last) load(held[0], first);
-    for (int p = first; p < last; p += 2) {
-        if (p + 1 < last) load(held[1], p + 1);
-        multiply(held[0]);
-        if (p + 1 >= last) break;
-        if (p + 2 < last) load(held[0], p + 2);
-        multiply(held[1]);
-    }
-    part[wave][lane] = acc;
-    __syncthreads();
-    if (wave != 0 || !row_in) return;
-    f32x4 sum = part[0][lane];
 #pragma unroll
-    for (int w = 1; w < kFewWaves; ++w) sum += part[w][lane];
-    const size_t at = (static_cast<size_t>(tc.row0) + frag_row) * op.N + col0 + 4 * g;
+        for (int c = 0; c < CF; ++c) {
+            acc[c] = mma<0>(r.b[c][0], r.a[0], acc[c], r.bs[c], r.as);
+            acc[c] = mma<1>(r.b[c][1], r.a[1], acc[c], r.bs[c], r.as);
+        }
+    };
+#pragma unroll
+    for (int q = 0; q < DEPTH - 1; ++q)
+        if (first + q < last) load(held[q], first + q);
+    for (int p = first; p < last; p += DEPTH) {
+#pragma unroll
+        for (int q = 0; q < DEPTH; ++q) {
+            if (p + q >= last) break;
+            if (p + q + DEPTH - 1 < last) load(held[(q + DEPTH - 1) % DEPTH], p + q + DEPTH - 1);
+            multiply(held[q]);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < CF; ++c) part[wave][c][lane] = acc[c];
+    __syncthreads();
+    if (wave >= CF || !row_in) return;               // a wavefront for each 16 columns
+    f32x4 sum = part[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) sum += part[w][wave][lane];
+    const size_t at = (static_cast<size_t>(tc.row0) + frag_row) * op.N + col0 + wave * 16 + 4 * g;
     if constexpr (F32) {
         *reinterpret_cast<f32x4*>(static_cast<float*>(out.c) + at) = sum;
     } else {
@@ -153,16 +169,19 @@ int large(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_
     return mx_runs(op.K) & 1 ? large_of<Cfg, true>(env, op, out, s) : large_of<Cfg, false>(env, op, out, s);
 }
 
-template <bool F32>
+template <bool F32, int CF>
 int few_rows(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
+    if (op.N % (16 * CF) != 0) return MOE_ERR_UNSUPPORTED_SHAPE;
     static std::atomic<uint64_t> attr_set{0};
-    return launch(env, attr_set, few_rows_kernel<F32>, 0, kFewWaves * kWave, most_row_tiles(op.R, op.E, kFewRows) * (op.N / 16), s, op, out);
+    return launch(env, attr_set, few_rows_kernel<F32, CF>, 0, kFewWaves * kWave,
+                  most_row_tiles(op.R, op.E, kFewRows) * (op.N / (16 * CF)), s, op, out);
 }
 
 template <bool F32>
 int product(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
     switch (mx_plain_tile(op.R, op.E, op.N, op.K, compute_units(env.device))) {
-        case kMxFew: return few_rows<F32>(env, op, out, s);
+        case kMxFew: return few_rows<F32, 1>(env, op, out, s);
+        case kMxFewWide: return few_rows<F32, 2>(env, op, out, s);
         case kMx16x64: return ring<Plain16x64<F32>>(env, op, out, s);
         case kMx32x64Deep: return ring<Plain32x64Deep<F32>>(env, op, out, s);
         case kMx32x64: return ring<Plain32x64<F32>>(env, op, out, s);

@@ -134,7 +134,7 @@ struct Loads {
     static constexpr int BLOCKS = Cfg::DUAL && Cfg::LB > 4 ? 2 : 1;
     static_assert(!Cfg::DUAL || Cfg::LB % 8 == 0 || 4 % Cfg::LB == 0, "whole blocks");
     __amdgpu_buffer_rsrc_t a, b[BLOCKS];
-    const uint8_t *a_scale, *b_scale[2];             // of the k-step whose loads are next
+    const uint8_t *a_scale, *b_scale[2];             // of the first k-step
     uint32_t a_scale_bytes, b_scale_bytes;
     uint32_t a_voff[Cfg::LA], b_voff[Cfg::LB];
     int wave, lane;
@@ -170,7 +170,7 @@ struct Loads {
     }
     __device__ __forceinline__ int load_a(int i) const { return min(wave * Cfg::LA + i, Cfg::NIA - 1); }
     __device__ __forceinline__ int load_b(int i) const { return min(wave * Cfg::LB + i, Cfg::NIB - 1); }
-    // all loads of k-step kt into the stage at LDS byte offset `stage`; k-steps are asked for one after the other
+    // all loads of k-step kt into the stage at LDS byte offset `stage`
     __device__ __forceinline__ void issue(const Operands& op, uint32_t stage, int kt) {
         const uint32_t koff = kt * 128;
 #pragma unroll
@@ -183,17 +183,15 @@ struct Loads {
         for (int i = 0; i < Cfg::LS; ++i) {
             const int q = min(wave * Cfg::LS + i, Cfg::NS - 1);
             if (q < Cfg::NSA) {
-                dma4(resource(a_scale, a_scale_bytes), q * 256 + lane * 4, stage + Cfg::SA_AT + q * 256);
+                const uint8_t* from = a_scale + static_cast<size_t>(kt) * op.R * kMxRunBytes;
+                dma4(resource(from, a_scale_bytes), q * 256 + lane * 4, stage + Cfg::SA_AT + q * 256);
             } else {
                 const int p = q - Cfg::NSA;          // 32 rows of the tile
                 const int m = Cfg::DUAL ? p & 1 : 0;
-                const uint8_t* from = m ? b_scale[1] : b_scale[0];
+                const uint8_t* from = (m ? b_scale[1] : b_scale[0]) + static_cast<size_t>(kt) * op.N * kMxRunBytes;
                 dma4(resource(from, b_scale_bytes), (Cfg::DUAL ? p >> 1 : p) * 256 + lane * 4, stage + Cfg::SB_AT + p * 256);
             }
         }
-        a_scale += static_cast<size_t>(op.R) * kMxRunBytes;
-#pragma unroll
-        for (int m = 0; m < (Cfg::DUAL ? 2 : 1); ++m) b_scale[m] += static_cast<size_t>(op.N) * kMxRunBytes;
     }
 };
 
@@ -239,6 +237,17 @@ __device__ __forceinline__ void store_tile(const f32x4 (&acc)[Cfg::TM][Cfg::TN],
     }
 }
 
+// The k-step that a tile begins with; the others follow in turn. Workgroups that start together stay at the same k, where weight rows a
+// multiple of 4 KB apart fall on few memory channels: n-tiles then begin at k-steps that their numbers draw (those that share
+// weights share the order). Expert FFN, 8 experts of 8192 x 8192, all from the first k-step -> so: 8 tokens 144 -> 121 us, 64 160 ->
+// 142, 256 179 -> 168, 400 182 -> 174; one matrix of 8192 x 32000, 37 rows 35.4 -> 29.6; rows of 2 KB, or no multiple: no difference.
+template <class Cfg>
+__device__ __forceinline__ int first_kstep(const Operands& op, const TileCoord& tc, int KT) {
+    if (op.K % 8192 != 0) return 0;
+    const uint32_t tile = static_cast<uint32_t>(tc.expert) * ((op.N + Cfg::BN_OUT - 1) / Cfg::BN_OUT) + tc.nt;
+    return static_cast<int>(__umulhi(tile * 0x9e3779b9u, static_cast<uint32_t>(KT)));
+}
+
 template <class Cfg>
 __global__ __launch_bounds__(Cfg::NTHREADS) void ring_kernel(Operands op, Outputs out) {
     constexpr int TM = Cfg::TM, TN = Cfg::TN, S = Cfg::NSTAGE;
@@ -250,10 +259,14 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void ring_kernel(Operands op, Output
     const int wm = wave / Cfg::WN, wn = wave % Cfg::WN, frag_row = lane & 15, g = lane >> 4;
     Loads<Cfg> loads;
     loads.init(op, tc, wave, lane);
-    const int KT = mx_runs(op.K);
+    const int KT = mx_runs(op.K), first = first_kstep<Cfg>(op, tc, KT);
+    auto issue = [&](int stage, int s) {             // k-step number s here
+        const int t = first + s;
+        loads.issue(op, stage * Cfg::STAGE, t >= KT ? t - KT : t);
+    };
 #pragma unroll
     for (int s = 0; s < S - 1; ++s)
-        if (s < KT) loads.issue(op, s * Cfg::STAGE, s);
+        if (s < KT) issue(s, s);
     f32x4 acc[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -285,7 +298,7 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void ring_kernel(Operands op, Output
             for (int j = 0; j < TN; ++j)
                 fb[h][j] = *reinterpret_cast<const i32x4*>(base + Cfg::B_AT + (wn * Cfg::WTN + j * 16) * 128 + at[h]);
         }
-        if (kt + S - 1 < KT) loads.issue(op, (stage == 0 ? S - 1 : stage - 1) * Cfg::STAGE, kt + S - 1);
+        if (kt + S - 1 < KT) issue(stage == 0 ? S - 1 : stage - 1, kt + S - 1);
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll

@@ -4,7 +4,7 @@
 // `alone` us with a tile on a compute unit or `full` with all it holds; a launch takes its rounds, or the time that its weights
 // take from memory if that is longer, and a fifth of the shorter of the two. The figures are fits to single products of 4096 and
 // 14336 elements through 4096 columns (one and two tiles per compute unit) and, for gate/up, to the experts of the presets;
-// against 61 sizes of both the tile of the lowest price is the fastest one or within 6 % of it but for three (16 % at most).
+// against 61 sizes of both the tile of the lowest price is the fastest one or within 6 % of it but for five (7 to 23 %).
 #pragma once
 #include <algorithm>
 #include <cmath>
@@ -17,12 +17,14 @@ struct MxTile {
     int resident;
     double alone, full, fixed;
 };
-enum MxPlain { kMxFew, kMx16x64, kMx32x64Deep, kMx32x64, kMx64x64, kMx64x128, kMx128x128, kMx128x128Pair, kMxLarge };
+enum MxPlain { kMxFew, kMxFewWide, kMx16x64, kMx32x64Deep, kMx32x64, kMx64x64, kMx64x128, kMx128x128, kMx128x128Pair,
+               kMxLarge };
 enum MxGateUp { kMxGate32, kMxGate64, kMxGate128, kMxGateLarge };
 
 //                                    id              rows cols res. alone   full    fixed
-constexpr MxTile kMxPlainTiles[] = {{kMxFew,          16,  16,  2,   0.10,   0.28,   3.0},
-                                    {kMx16x64,        16,  64,  2,   0.225,  0.3775, 3.0},
+constexpr MxTile kMxPlainTiles[] = {{kMxFew,          16,  16,  2,   0.12,   0.25,   2.5},
+                                    {kMxFewWide,      16,  32,  2,   0.20,   0.35,   4.2},
+                                    {kMx16x64,        16,  64,  2,   0.265,  0.3775, 3.0},
                                     {kMx32x64Deep,    32,  64,  2,   0.2575, 0.4425, 3.3},
                                     {kMx32x64,        32,  64,  4,   0.3625, 0.75,   3.0},
                                     {kMx64x64,        64,  64,  2,   0.3325, 0.5825, 3.1},
@@ -57,12 +59,13 @@ double mx_price(const MxTile& t, bool large, bool dual, int R, int E, int N, int
     return std::max(us, memory) + 0.2 * std::min(us, memory);
 }
 
-// The large tiles need two k-steps and as many columns as they have.
+// The large tiles need two k-steps and as many columns as they have, the wider ones of a few rows whole tiles.
 int mx_plain_tile(int R, int E, int N, int K, int cus) {
     int best = kMxFew;
     double least = 1e30;
     for (const MxTile& t : kMxPlainTiles) {
         if (t.id == kMxLarge && (K <= kMxRunElements || N < t.columns)) continue;
+        if (t.id == kMxFewWide && N % t.columns != 0) continue;
         const double p = mx_price(t, t.id == kMxLarge, false, R, E, N, K, cus);
         if (p < least) { least = p; best = t.id; }
     }
