@@ -20,6 +20,7 @@ using mx4::Outputs;
 using mx4::Tile;
 
 //                       BM   BN  WM WN NSTAGE DUAL STREAM_B
+using GateUpFew    = Tile<32, 64, 2, 1, 6, true, true>;
 using GateUp32     = Tile<32, 128, 2, 2, 3, true, true>;
 using GateUp64     = Tile<64, 128, 2, 2, 3, true, true>;
 using GateUp128    = Tile<128, 256, 2, 4, 3, true>;
@@ -201,6 +202,7 @@ int launch_gateup_mx4(const GemmEnv& env, const moe_mx4* x, const moe_e8m0* x_sc
     const Operands op{x, x_scale, {W1, W3}, {w1_scale, w3_scale}, offsets, R, E, f, d};
     const Outputs out{H, h_scale};
     switch (mx_gateup_tile(R, E, f, d, compute_units(env.device))) {
+        case kMxGateFew: return ring<GateUpFew>(env, op, out, s);
         case kMxGate32: return ring<GateUp32>(env, op, out, s);
         case kMxGate64: return ring<GateUp64>(env, op, out, s);
         case kMxGate128: return ring<GateUp128>(env, op, out, s);

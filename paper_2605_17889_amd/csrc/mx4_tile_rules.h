@@ -19,7 +19,7 @@ struct MxTile {
 };
 enum MxPlain { kMxFew, kMxFewWide, kMx16x64, kMx32x64Deep, kMx32x64, kMx64x64, kMx64x128, kMx128x128, kMx128x128Pair,
                kMxLarge };
-enum MxGateUp { kMxGate32, kMxGate64, kMxGate128, kMxGateLarge };
+enum MxGateUp { kMxGateFew, kMxGate32, kMxGate64, kMxGate128, kMxGateLarge };
 
 //                                    id              rows cols res. alone   full    fixed
 constexpr MxTile kMxPlainTiles[] = {{kMxFew,          16,  16,  2,   0.12,   0.25,   2.5},
@@ -32,7 +32,8 @@ constexpr MxTile kMxPlainTiles[] = {{kMxFew,          16,  16,  2,   0.12,   0.2
                                     {kMx128x128,      128, 128, 1,   0.7175, 0.7175, 6.0},
                                     {kMx128x128Pair,  128, 128, 2,   1.0,    1.2,    6.5},
                                     {kMxLarge,        256, 256, 1,   1.0,    1.5,    8.0}};
-constexpr MxTile kMxGateUpTiles[] = {{kMxGate32,      32,  64,  2,   0.44,   0.80,   4.0},
+constexpr MxTile kMxGateUpTiles[] = {{kMxGateFew,     32,  32,  2,   0.34,   0.60,   3.8},
+                                     {kMxGate32,      32,  64,  2,   0.44,   0.80,   4.0},
                                      {kMxGate64,      64,  64,  2,   0.52,   1.0,    5.0},
                                      {kMxGate128,     128, 128, 1,   1.25,   1.4,    7.0},
                                      {kMxGateLarge,   256, 128, 1,   1.0,    1.5,    8.0}};
@@ -43,7 +44,7 @@ constexpr double kMxLargeAlone = 0.6;
 
 // Experts that hold a row, and row tiles of `h` rows, under uniform routing: half of the groups a standard deviation below the mean
 // and half above it.
-double mx_touched(int R, int E) { return E == 1 ? 1.0 : E * (1.0 - std::exp(-static_cast<double>(R) / E)); }
+double mx_touched(int R, int E) { return E == 1 ? 1.0 : std::ceil(E * (1.0 - std::exp(-static_cast<double>(R) / E))); }
 double mx_row_tiles(int R, int E, int h) {
     if (E == 1) return std::ceil(static_cast<double>(R) / h);
     const double touched = mx_touched(R, E), avg = R / touched, sigma = touched > 1.5 ? std::sqrt(avg) : 0.0;

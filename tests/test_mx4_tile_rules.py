@@ -9,7 +9,7 @@ from mx4_sizes import GATEUP, PLAIN
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 FEW, FEW_WIDE, T16X64, T32X64_DEEP, T32X64, T64X64, T64X128, T128X128, T128X128_PAIR, LARGE = range(10)
-GATE32, GATE64, GATE128, GATE_LARGE = range(4)
+GATE_FEW, GATE32, GATE64, GATE128, GATE_LARGE = range(5)
 
 
 @pytest.fixture(scope="module")
@@ -36,7 +36,9 @@ def test_products(tile, R, E, N, K, want):
 
 
 @pytest.mark.parametrize("R,E,f,d,want", [
-    (32, 8, 14336, 4096, GATE32),              # us of the whole FFN: 129.4, 64 rows 129.0, 128 rows 156
+    (8, 128, 768, 2048, GATE_FEW),             # us of the whole FFN: 10.3, 64 columns 11.4
+    (16, 128, 768, 2048, GATE32),              # 13.1, 32 columns 13.5
+    (32, 8, 14336, 4096, GATE32),              # 129.4, 64 rows 129.0, 128 rows 156
     (256, 8, 14336, 4096, GATE64),             # 123.5, 32 rows 140.9, 128 rows 156.0
     (800, 8, 14336, 4096, GATE128),            # 162.8, large 166.1, 64 rows 192.3
     (1024, 8, 14336, 4096, GATE_LARGE),        # 181.2, 128 rows 210.5
@@ -47,7 +49,7 @@ def test_gate_and_up(tile, R, E, f, d, want):
 
 def test_sizes_of_the_numerical_tests_take_every_tile(tile):
     assert {tile("plain", R, E, N, K) for R, E, N, K in PLAIN} == set(range(10))
-    assert {tile("gateup", R, E, f, d) for R, E, f, d in GATEUP} == set(range(4))
+    assert {tile("gateup", R, E, f, d) for R, E, f, d in GATEUP} == set(range(5))
 
 
 def test_large_tiles_only_where_they_fit(tile):
