@@ -436,8 +436,8 @@ typedef uint8_t moe_e8m0;           /* a scale */
  * 2^max(m - 2, -127) and an element is brought to the nearest code of element / scale (ties to the even code), above 6 to 6.
  * A block of zeros has scale byte 0; a block that holds a NaN or an infinity has scale byte 255 and codes 0. Writes the
  * scales of blocks behind the row's end too.
- * x [T,d], rows x_stride >= d elements apart, d a multiple of 32 up to 2^22 (else MOE_ERR_UNSUPPORTED_SHAPE); q [T,d/2];
- * scale [ceil(d/256),T,8]. Tokens, or one matrix (T = N output channels of d = K). No context. */
+ * x [T,d], rows x_stride >= d elements apart, d a multiple of 32 up to 2^22, ceil(T/16) * ceil(d/256) below 2^24 - both ways,
+ * else MOE_ERR_UNSUPPORTED_SHAPE; q [T,d/2]; scale [ceil(d/256),T,8]. Tokens, or one matrix (T = N output channels of d = K). No context. */
 int moe_quantize_mx4(const moe_bf16* x, int64_t x_stride, int32_t T, int32_t d, moe_mx4* q,
                      moe_e8m0* scale, void* stream);
 

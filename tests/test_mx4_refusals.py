@@ -36,6 +36,13 @@ def test_widths_that_are_no_blocks_or_too_long(lib):  # noqa: F811
     assert quantize(lib, T=0, x=NULL, q=NULL, scale=NULL) == 0 and dequantize(lib, T=0, q=NULL, scale=NULL, y=NULL) == 0
 
 
+def test_more_rows_than_a_launch_holds(lib):  # noqa: F811
+    """A launch of 256 threads for 16 rows of one run holds fewer than 2^32 threads."""
+    for T, d in ((2**31 - 1, 32), (2**28 - 15, 32), (2**31 - 1, 512), (2**27 - 15, 512), (2**20, 1 << 17)):
+        assert quantize(lib, T=T, d=d, stride=d) == UNSUPPORTED
+        assert dequantize(lib, T=T, d=d) == UNSUPPORTED
+
+
 def test_calls_without_a_context_are_refused(lib):  # noqa: F811
     i = C.c_int32
     assert lib.moe_gemm_mx4(NULL, P, P, NULL, i(4), i(1), i(64), i(256), P, P, P, i(0), NULL) == INVALID
