@@ -116,9 +116,6 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_rows_kernel(Operands op
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------------
-// Upper bound on the number of row tiles of E groups with R rows in all.
-long long most_row_tiles(int R, int E, int BM) { return R / BM + std::min(E, R); }
-
 template <class Kernel, class... Args>
 int launch(const GemmEnv& env, std::atomic<uint64_t>& attr_set, Kernel kern, int smem, int threads, long long grid,
            hipStream_t s, Args... args) {
@@ -130,7 +127,7 @@ int launch(const GemmEnv& env, std::atomic<uint64_t>& attr_set, Kernel kern, int
         attr_set.fetch_or(bit, std::memory_order_release);
     }
     grid = (grid + kXcds - 1) / kXcds * kXcds;       // every XCD's range of tiles is as long
-    if (grid > 0x7fffffffLL) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (grid * threads >= 1ll << 32) return MOE_ERR_UNSUPPORTED_SHAPE;
     hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>(grid)), dim3(threads), smem, s, args...);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
@@ -139,7 +136,7 @@ template <class Cfg>
 int ring(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
     static std::atomic<uint64_t> attr_set{0};
     return launch(env, attr_set, mx4::ring_kernel<Cfg>, Cfg::SMEM, Cfg::NTHREADS,
-                  most_row_tiles(op.R, op.E, Cfg::BM) * ((op.N + Cfg::BN_OUT - 1) / Cfg::BN_OUT), s, op, out);
+                  mx_most_row_tiles(op.R, op.E, Cfg::BM) * ((op.N + Cfg::BN_OUT - 1) / Cfg::BN_OUT), s, op, out);
 }
 
 using GateUpLarge = mx4::Mx4<gemm::Config<256, 256, 64, 2, 2, 2, true>>;
@@ -156,7 +153,7 @@ int large_of(const GemmEnv& env, const Operands& op, const Outputs& out, hipStre
     static std::atomic<uint64_t> attr_set[2];
     const int cus = compute_units(env.device), nt = gemm::n_tiles<Cfg>(op.N);
     // tiles, and the halves that the last round's are cut into
-    const long long slots = most_row_tiles(op.R, op.E, 256) * nt + kXcds * ((cus / 2 + kXcds - 1) / kXcds + 1);
+    const long long slots = mx_most_row_tiles(op.R, op.E, 256) * nt + kXcds * ((cus / 2 + kXcds - 1) / kXcds + 1);
     const double tiles = static_cast<double>(op.R) / 256 * nt;
     if (tiles > 1.5 * cus)
         return launch(env, attr_set[0], mx4::large_kernel<Cfg, true, ODD>, mx4::Large<Cfg>::SMEM, 256, std::min<long long>(slots, cus), s,
@@ -175,7 +172,7 @@ int few_rows(const GemmEnv& env, const Operands& op, const Outputs& out, hipStre
     if (op.N % (16 * CF) != 0) return MOE_ERR_UNSUPPORTED_SHAPE;
     static std::atomic<uint64_t> attr_set{0};
     return launch(env, attr_set, few_rows_kernel<F32, CF>, 0, kFewWaves * kWave,
-                  most_row_tiles(op.R, op.E, kFewRows) * (op.N / (16 * CF)), s, op, out);
+                  mx_most_row_tiles(op.R, op.E, kFewRows) * (op.N / (16 * CF)), s, op, out);
 }
 
 template <bool F32>

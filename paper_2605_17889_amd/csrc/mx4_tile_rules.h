@@ -60,6 +60,15 @@ double mx_price(const MxTile& t, bool large, bool dual, int R, int E, int N, int
     return std::max(us, memory) + 0.2 * std::min(us, memory);
 }
 
+// Upper bound on the row tiles of E groups with R rows in all.
+long long mx_most_row_tiles(int R, int E, int rows) { return R / rows + std::min(E, R); }
+// A launch counts its threads in 32 bits: 512 for each tile of up to 32 columns, 256 for each of the others. Many groups and columns
+// (256 rows in 256 groups through 2^22 columns) take larger tiles for that; a large kernel's workgroup takes many.
+bool mx_launchable(const MxTile& t, int R, int E, int N) {
+    const long long tiles = mx_most_row_tiles(R, E, t.rows) * ((N + t.columns - 1) / t.columns);
+    return (tiles + 8) * (t.columns <= 32 ? 512 : 256) < 1ll << 32;
+}
+
 // The large tiles need two k-steps and as many columns as they have, the wider ones of a few rows whole tiles.
 int mx_plain_tile(int R, int E, int N, int K, int cus) {
     int best = kMxFew;
@@ -67,6 +76,7 @@ int mx_plain_tile(int R, int E, int N, int K, int cus) {
     for (const MxTile& t : kMxPlainTiles) {
         if (t.id == kMxLarge && (K <= kMxRunElements || N < t.columns)) continue;
         if (t.id == kMxFewWide && N % t.columns != 0) continue;
+        if (t.id != kMxLarge && !mx_launchable(t, R, E, N)) continue;
         const double p = mx_price(t, t.id == kMxLarge, false, R, E, N, K, cus);
         if (p < least) { least = p; best = t.id; }
     }

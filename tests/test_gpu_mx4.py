@@ -463,6 +463,28 @@ def test_weights_past_32_bits():
     ctx.close()
 
 
+def test_a_row_for_each_of_256_groups_and_the_most_columns():
+    """Small tiles would be more than a launch holds: 272 row tiles through 2^22 columns."""
+    E, N, K = 256, 1 << 22, 32
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, s, x = random_rows(g, E, K)
+    w = torch.empty((E, N, K // 2), dtype=torch.uint8, device="cuda")
+    for e in range(E):
+        w[e] = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    ws = torch.zeros((E, 1, N, 8), dtype=torch.uint8, device="cuda")
+    ws[..., 0] = 127
+    out = torch.full((E, N), 77.0, dtype=torch.bfloat16, device="cuda")
+    ctx = B.MoeContext(E, 512, 128, E, 1)
+    B.moe_gemm_mx4(ctx, q, s, torch.arange(E + 1, dtype=torch.int32, device="cuda"), E, E, N, K, w, ws, out)
+    values = torch.tensor(np.concatenate([M.VALUES, -M.VALUES]), device="cuda")
+    for cols in (slice(0, 100), slice(N // 2 - 50, N // 2 + 50), slice(N - 100, N)):
+        wv = values[torch.stack((w[:, cols] & 15, w[:, cols] >> 4), dim=-1).long()].flatten(-2)
+        want = (x[:, None] * wv).sum(-1)
+        tol = sum_error(K) * (x[:, None].abs() * wv.abs()).sum(-1) + BF16 * want.abs() * (1 + 1e-6)
+        assert ((out[:, cols].double() - want).abs() <= tol).all()
+    ctx.close()
+
+
 def test_refusals():
     ctx = B.MoeContext(8, 512, 128, 4, 2)
     u8 = lambda *s: torch.zeros(s, dtype=torch.uint8, device="cuda")

@@ -52,6 +52,22 @@ def test_sizes_of_the_numerical_tests_take_every_tile(tile):
     assert {tile("gateup", R, E, f, d) for R, E, f, d in GATEUP} == set(range(5))
 
 
+# rows, columns, threads of a workgroup
+SIZES = {FEW: (16, 16, 512), FEW_WIDE: (16, 32, 512), T16X64: (16, 64, 256), T32X64_DEEP: (32, 64, 256), T32X64: (32, 64, 256),
+         T64X64: (64, 64, 256), T64X128: (64, 128, 256), T128X128: (128, 128, 256), T128X128_PAIR: (128, 128, 256)}
+
+
+def test_launches_hold_fewer_than_2_32_threads(tile):
+    """A workgroup per possible tile: with many groups and columns the smaller tiles would be too many."""
+    for R in (1, 16, 100, 256, 1000, 4000, 16384):
+        for E in (1, 64, 256):
+            for N in (1 << 20, (1 << 21) + 16, 3 << 20, 1 << 22):
+                for K in (32, 128, 256):
+                    t = tile("plain", R, E, N, K)
+                    rows, columns, threads = SIZES[t]
+                    assert (R // rows + min(R, E)) * -(-N // columns) * threads < 2**32, (R, E, N, K, t)
+
+
 def test_large_tiles_only_where_they_fit(tile):
     for R in (1, 100, 5000, 100000):
         for N in (16, 128, 240):
