@@ -210,8 +210,8 @@ int moe_last_routing(moe_ctx* ctx, int32_t T, int32_t* topk_idx, float* topk_w, 
 
 /* Per-stage device timing for measurement. moe_profile_begin() arms up to `max_calls`
  * subsequent moe_layer_forward / moe_layer_forward_microbatched / moe_layer_forward_streamed / moe_layer_forward_i8 /
- * moe_layer_forward_mx4 / moe_expert_ffn / moe_expert_ffn_i8 / moe_expert_ffn_mx4 calls: each records HIP events on the caller's stream between stages (the
- * two GEMM stages for moe_expert_ffn). moe_profile_end() waits for those events and
+ * moe_layer_forward_mx4 / moe_expert_ffn / moe_expert_ffn_i8 / moe_expert_ffn_mx4 calls: each records HIP events on the
+ * caller's stream between stages (the two GEMM stages for moe_expert_ffn). moe_profile_end() waits for those events and
  * writes, per stage, the total milliseconds (stage_ms[MOE_NUM_STAGES], host), the number of
  * kernel launches (stage_launches[MOE_NUM_STAGES], host) and the number of layer calls
  * covered (*calls), then disarms. Costs two event records per stage while armed.
@@ -471,7 +471,8 @@ int moe_expert_ffn_mx4(moe_ctx* ctx, const moe_mx4* x_perm, const moe_e8m0* x_sc
 /* moe_layer_forward with its experts in 4 bits: the router reads the tokens x [T,d_model] in bf16, the experts the same tokens
  * as moe_quantize_mx4 brings them to 4 bits; route -> permute -> rows in 4 bits, grouped -> expert FFN as in
  * moe_expert_ffn_mx4 -> combine. scoring NULL: the router is moe_route's (correction is NULL then), else moe_route_scored's with
- * correction [E] or NULL. Weights as above; moe_set_expert_output_fp32 and moe_last_routing as for moe_layer_forward. */
+ * correction [E] or NULL. Weights as above; moe_set_expert_output_fp32 and moe_last_routing as for moe_layer_forward. The rows'
+ * conversion is the gather stage of moe_profile_begin. */
 int moe_layer_forward_mx4(moe_ctx* ctx, const moe_bf16* x, const float* w_router, const float* bias,
                           const float* correction, const moe_scoring* scoring, const moe_mx4* W1,
                           const moe_e8m0* w1_scale, const moe_mx4* W3, const moe_e8m0* w3_scale,

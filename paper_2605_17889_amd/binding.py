@@ -64,8 +64,8 @@ class MoeScoring(C.Structure):
         super().__init__(1 if score == "sigmoid" else 0, groups, top_groups, group_best, int(renormalise), scale)
 
 
-# Argument types of the calls with many arguments: ctypes then converts plain numbers by itself. Host time of a call, with an object for every
-# argument and for the stream -> so: moe_rmsnorm_i8 11.5 -> 7.4 us, moe_gemm_i8 10.3 -> 6.5, moe_expert_ffn_i8 18.5 -> 11.7.
+# Argument types of the calls with many arguments: ctypes then converts plain numbers by itself. Host time of a call, with an
+# object for every argument and for the stream -> so: moe_rmsnorm_i8 11.5 -> 7.4 us, moe_gemm_i8 10.3 -> 6.5, moe_expert_ffn_i8 18.5 -> 11.7.
 _P, _I, _L, _F = C.c_void_p, C.c_int32, C.c_int64, C.c_float
 _ARGUMENTS = {
     "moe_rmsnorm_i8": (_P, _L, _P, _I, _P, _F, _I, _I, _P, _P, _P, _P, _P),

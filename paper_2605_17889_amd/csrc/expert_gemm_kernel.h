@@ -509,8 +509,8 @@ template <class Cfg, class = void>
 struct any_width : operands_i8<Cfg> {};
 template <class Cfg>
 struct any_width<Cfg, std::void_t<decltype(Cfg::ANY_WIDTH)>> : std::bool_constant<Cfg::ANY_WIDTH> {};
-// The n-tiles of N output columns. With 8-bit operands (and with 4-bit ones) N need not be a multiple of a tile's columns (it has to hold one): the
-// last tile then starts further left, and the columns that two tiles share get the same bits from both.
+// The n-tiles of N output columns. With 8-bit operands, and 4-bit ones, N need not be a multiple of a tile's columns (it has to
+// hold one): the last tile then starts further left, and the columns that two tiles share get the same bits from both.
 template <class Cfg>
 __host__ __device__ __forceinline__ int n_tiles(int N) {
     return any_width<Cfg>::value ? (N + Cfg::BN_OUT - 1) / Cfg::BN_OUT : N / Cfg::BN_OUT;

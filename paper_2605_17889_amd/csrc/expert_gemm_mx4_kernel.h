@@ -237,8 +237,8 @@ __device__ __forceinline__ void store_tile(const f32x4 (&acc)[Cfg::TM][Cfg::TN],
     }
 }
 
-// The k-step that a tile begins with; the others follow in turn. Workgroups that start together stay at the same k, where weight rows a
-// multiple of 4 KB apart fall on few memory channels: n-tiles then begin at k-steps that their numbers draw (those that share
+// The k-step that a tile begins with; the others follow in turn. Workgroups that start together stay at the same k, where weight rows
+// a multiple of 4 KB apart fall on few memory channels: n-tiles then begin at k-steps that their numbers draw (those that share
 // weights share the order). Expert FFN, 8 experts of 8192 x 8192, all from the first k-step -> so: 8 tokens 144 -> 121 us, 64 160 ->
 // 142, 256 179 -> 168, 400 182 -> 174; one matrix of 8192 x 32000, 37 rows 35.4 -> 29.6; rows of 2 KB, or no multiple: no difference.
 template <class Cfg>
@@ -278,6 +278,7 @@ __global__ __launch_bounds__(Cfg::NTHREADS) void ring_kernel(Operands op, Output
     int stage = 0;
     for (int kt = 0; kt < KT; ++kt) {
         if (kt + S - 2 < KT) gemm::wait_vmcnt<(S - 2) * Cfg::LPW>(); else gemm::wait_vmcnt<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // own reads of the stage before, wherever their MFMAs are
         __builtin_amdgcn_s_barrier();                // stage `stage` is there, the one before is no longer read
         asm volatile("" ::: "memory");               // and is not read ahead of the barrier
         const unsigned char* base = smem + stage * Cfg::STAGE;
@@ -530,7 +531,7 @@ __device__ __forceinline__ void large_kstep(f32x4 (&acc)[Cfg::TM][8], i32x4 (&fa
 // and the neighbour's of one block), groups 0 and 2 of the first, 1 and 3 of the second, one of the upper and lower half
 // wavefronts brings 8 bytes of codes together; the maxima go the same way, and a third swap back. Stores go through resources
 // that end behind the wavefront's last row. What is left is bound by the exponentials and reciprocals of SiLU (16 cycles each,
-// 3.2 us of a tile's 4.7 at 1.9 GHz).
+// by count 3.2 us of a tile's 4.6 at 1.9 GHz).
 template <class Cfg, class Before>
 __device__ __forceinline__ void store_blocks(const f32x4 (&acc)[Cfg::TM][8], const Operands& op, const TileCoord& tc,
                                              const Outputs& out, int wm, int wn, int lane, Before&& before_stores) {
