@@ -9,7 +9,7 @@
 // own lanes. Selection is k rounds of a maximum over the token's lanes, on integers of the scores' order (route_select.h).
 // The weights are formed from the selected experts' logits once more: a slot's lane reads its own. No result depends on the
 // number of lanes. Bound by the chain of the rounds (0.2 us each for one token) and, with many tokens, by their instructions:
-// 8192 tokens of 256 experts read 8.4 MB, 1.3 us of the 9.6.
+// 8192 tokens of 256 experts read 8.4 MB, 1.3 us of the 8.9.
 #include <algorithm>
 
 #include "route_select.h"
@@ -55,10 +55,20 @@ __device__ __forceinline__ uint32_t max_over_token(uint32_t v) {
     if constexpr (S < LPT) return max_over_token<LPT, 2 * S>(with_partner<S>(v, [](uint32_t x, uint32_t y) { return max(x, y); }));
     else return v;
 }
+// Of numbers, without the quieting of signalling NaNs that a language's maximum has to do.
+__device__ __forceinline__ double larger(double x, double y) {
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(x), "v"(y));
+    return r;
+}
 template <int LPT, int S = 1>
-__device__ __forceinline__ uint32_t min_over_token(uint32_t v) {
-    if constexpr (S < LPT) return min_over_token<LPT, 2 * S>(with_partner<S>(v, [](uint32_t x, uint32_t y) { return min(x, y); }));
-    else return v;
+__device__ __forceinline__ double max_over_token(double v) {
+    if constexpr (S < LPT) {
+        const Pair lo = partners<S>(__double2loint(v)), hi = partners<S>(__double2hiint(v));
+        return max_over_token<LPT, 2 * S>(larger(__hiloint2double(hi.lo, lo.lo), __hiloint2double(hi.hi, lo.hi)));
+    } else {
+        return v;
+    }
 }
 // The sum in the order of the distances 1, 2, 4, ..
 template <int LPT, int S = 1>
@@ -183,12 +193,24 @@ __global__ __launch_bounds__(256) void route_scored_kernel(ScoredArgs a) {
     }
 
     int slot_of[SLOTS] = {};                                   // lane l keeps slots l, l + LPT, ...
-    for (int s = 0; s < a.k; ++s) {
-        uint32_t own = key[0];
+    // 16 lanes: c's order and the index (the lower one above) in the fraction of a double, so that a round is a maximum of numbers
+    // of which no two are equal, and needs no search for who has it. Maximum, then the lowest index that has it -> so: 8192 tokens
+    // of 256 experts, k = 8 9.8 -> 8.9 us, 16384, k = 16 18.2 -> 15.5, 128 experts 6.5 -> 6.0; of 64 and fewer 0 to 3 % slower.
+    // Its 8 bits of index are enough for all experts, and different in two low words.
+    double both[LPT == kWave ? 1 : EW];
+    if constexpr (LPT != kWave) {
 #pragma unroll
-        for (int i = 1; i < EW; ++i) own = max(own, key[i]);
-        const uint32_t best = max_over_token<LPT>(own);
+        for (int i = 0; i < EW; ++i) {
+            const uint32_t e = static_cast<uint32_t>(g * a.size + in_group<QUADS>(i, j, L));
+            both[i] = __hiloint2double(static_cast<int>(0x3ff00000u | key[i] >> 24), static_cast<int>(key[i] << 8 | ((255u - e) & 255u)));
+        }
+    }
+    for (int s = 0; s < a.k; ++s) {
         if constexpr (LPT == kWave) {
+            uint32_t own = key[0];
+#pragma unroll
+            for (int i = 1; i < EW; ++i) own = max(own, key[i]);
+            const uint32_t best = max_over_token<LPT>(own);
             // The lowest index that has it, on the scalar unit: of the first group that has it the first i (with QUADS four of
             // them), of those the first lane.
             uint64_t in[EW], any = 0;
@@ -216,16 +238,20 @@ __global__ __launch_bounds__(256) void route_scored_kernel(ScoredArgs a) {
             for (int i = 0; i < EW; ++i) key[i] = i == which && lane == from ? 0u : key[i];
             slot_of[0] = s == lane ? e : slot_of[0];
         } else {
-            int at = 0;                                        // the lane's first one that has it
+            double of[EW];
 #pragma unroll
-            for (int i = EW - 1; i >= 0; --i) at = key[i] == best ? i : at;
-            const uint32_t mine = own == best ? static_cast<uint32_t>(g * a.size + in_group<QUADS>(at, j, L)) : 0xffffffffu;
-            const uint32_t e = min_over_token<LPT>(mine);
-            at = e == mine ? at : -1;
+            for (int i = 0; i < EW; ++i) of[i] = both[i];
 #pragma unroll
-            for (int i = 0; i < EW; ++i) key[i] = at == i ? 0u : key[i];
+            for (int n = EW; n > 1; n = (n + 1) / 2)
 #pragma unroll
-            for (int q = 0; q < SLOTS; ++q) slot_of[q] = s == q * LPT + lane ? static_cast<int>(e) : slot_of[q];
+                for (int i = 0; i < n / 2; ++i) of[i] = larger(of[i], of[n - 1 - i]);
+            const double best = max_over_token<LPT>(of[0]);
+#pragma unroll
+            for (int i = 0; i < EW; ++i)
+                both[i] = __hiloint2double(__double2loint(both[i]) == __double2loint(best) ? 0 : __double2hiint(both[i]), __double2loint(both[i]));
+            const int e = 255 - (__double2loint(best) & 255);
+#pragma unroll
+            for (int q = 0; q < SLOTS; ++q) slot_of[q] = s == q * LPT + lane ? e : slot_of[q];
         }
     }
 
@@ -280,8 +306,8 @@ int launch_route_scored(const float* logits, const float* correction, const moe_
     if (T == 0) return MOE_OK;
     ScoredArgs a{logits, correction, T, E, k, sc.groups, E / sc.groups, 0, sc.top_groups, sc.group_best == 2,
                  sc.score == MOE_SCORE_SIGMOID, sc.renormalise != 0, sc.scale, topk_idx, topk_w};
-    // us, 16 | 64 lanes: 256 experts in 8 groups, one token 7.6 | 4.1, 2000 8.1 | 5.3, 4000 8.2 | 7.0, 8192 9.8 | 10.4, 16384 14.5 |
-    // 17.6; 64 experts, softmax, 5003 tokens 4.2 | 4.5, 16384 5.9 | 9.1. (32 lanes are between the two but for 8192 tokens: 9.1.)
+    // us, 16 | 64 lanes: 256 experts in 8 groups, one token 6.7 | 4.2, 2000 7.1 | 5.3, 4000 7.3 | 7.0, 5000 8.7 | 7.9, 8192 8.9 |
+    // 10.4, 16384 13.3 | 17.7; 128 experts, 4000 tokens 4.9 | 4.9; 64, softmax, 2000 3.8 | 3.6, 4000 3.9 | 4.3, 16384 6.0 | 9.2.
     const int lpt = T <= 4096 || group_lanes(a.groups, 16) == 0 ? 64 : 16;
     const int L = group_lanes(a.groups, lpt);
     while ((2 << a.lane_shift) <= L) ++a.lane_shift;
