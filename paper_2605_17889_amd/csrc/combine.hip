@@ -77,6 +77,8 @@ __global__ __launch_bounds__(256) void combine_kernel(const void* __restrict__ y
 
 }  // namespace
 
+bool combine_fits(int T) { return T * 256ll <= kMaxThreads; }
+
 int launch_combine(const void* y_perm, bool y_f32, const int32_t* inv_perm, const float* topk_w, int T,
                    int d, int k, moe_bf16* y, hipStream_t s) {
     if (T == 0) return MOE_OK;

@@ -15,6 +15,7 @@ constexpr int kMaxDimI8 = 1 << 23; // widths of outputs, for 32-bit offsets insi
 constexpr int kMaxDimMx4 = 1 << 22; // lengths of rows in 4 bits and of fp32 outputs: 128 rows of a tile stay below 2^32 bytes
 constexpr int kMaxGroups = 64;   // of experts: a lane each
 constexpr int kXcds = 8;         // workgroups are dealt round-robin to the 8 XCDs (own L2 each)
+constexpr long long kMaxThreads = (1ll << 32) - 1; // of a launch, which counts them in 32 bits
 
 __device__ __forceinline__ float bf16_to_f32(uint16_t b) {
     return __uint_as_float(static_cast<uint32_t>(b) << 16);
@@ -98,6 +99,7 @@ int launch_gateup_routed(const GemmEnv& env, const moe_bf16* x, const float* log
                          int E, int k, const moe_bf16* W1, const moe_bf16* W3, moe_bf16* H, hipStream_t s);
 int launch_down(const GemmEnv& env, const moe_bf16* H, const int32_t* offsets, int R, int R_hint,
                 int d, int f, int E, const moe_bf16* W2, void* y_perm, bool y_f32, hipStream_t s);
+bool combine_fits(int T);        // whether a launch holds the tokens
 int launch_combine(const void* y_perm, bool y_f32, const int32_t* inv_perm, const float* topk_w, int T,
                    int d, int k, moe_bf16* y, hipStream_t s);
 // Rows in 8 bits, of up to kMaxRowI8 elements: the norm in front of an 8-bit product, and bf16 rows as they are.
@@ -120,10 +122,12 @@ int launch_down_converting_i8(const GemmEnv& env, const moe_bf16* H, const int32
 constexpr int kNeedsSums = 1;
 int launch_product_i8(const GemmEnv& env, const moe_i8* x, const float* x_scale, const int32_t* offsets, int R, int N, int K,
                       int E, const moe_i8* W, const float* w_scale, void* out, bool out_f32, hipStream_t s);
-// Scores, groups and weights from logits; sc is checked.
+// Scores, groups and weights from logits; sc is checked. route_scored_fits: whether a launch holds the tokens.
+bool route_scored_fits(int T, int groups);
 int launch_route_scored(const float* logits, const float* correction, const moe_scoring& sc, int T, int E, int k,
                         int32_t* topk_idx, float* topk_w, hipStream_t s);
-// Rows in microscaled 4-bit floating point (mx4.h), d a multiple of 32.
+// Rows in microscaled 4-bit floating point (mx4.h), d a multiple of 32. rows_mx4_fit: whether a launch holds them.
+bool rows_mx4_fit(int T, int d);
 int launch_quantize_mx4(const moe_bf16* x, long long x_stride, int T, int d, moe_mx4* q, moe_e8m0* scale, hipStream_t s);
 // Token rows to their k places in the rows grouped by expert.
 int launch_quantize_grouped_mx4(const moe_bf16* x, const int32_t* inv_perm, int T, int d, int k, moe_mx4* q, moe_e8m0* scale,

@@ -268,12 +268,12 @@ int expert_ffn_i8(moe_ctx* c, const moe_i8* x, const float* x_scale, const int32
     });
 }
 
-int scoring_status(const moe_scoring* sc, const moe_shape& sh) {
+int scoring_status(const moe_scoring* sc, const moe_shape& sh, int T) {
     if (!sc || (sc->score != MOE_SCORE_SOFTMAX && sc->score != MOE_SCORE_SIGMOID)) return MOE_ERR_INVALID_ARG;
     if (sc->groups < 1 || sh.E % sc->groups != 0 || sc->top_groups < 1 || sc->top_groups > sc->groups) return MOE_ERR_INVALID_ARG;
     if (sc->group_best != 1 && sc->group_best != 2) return MOE_ERR_INVALID_ARG;
     if (sh.k > sc->top_groups * (sh.E / sc->groups) || !std::isfinite(sc->scale)) return MOE_ERR_INVALID_ARG;
-    return sc->groups > kMaxGroups ? MOE_ERR_UNSUPPORTED_SHAPE : MOE_OK;
+    return sc->groups > kMaxGroups || !route_scored_fits(T, sc->groups) ? MOE_ERR_UNSUPPORTED_SHAPE : MOE_OK;
 }
 
 // Logits, then the selection by scores. Without a caller's tensor the logits lie in the context's own or, where it has none (up to
@@ -853,7 +853,7 @@ int moe_route_scored(moe_ctx* c, const moe_bf16* x, const float* w_router, const
                      const moe_scoring* scoring, int32_t T, int32_t* topk_idx, float* topk_w, float* logits_out, void* stream) {
     if (!c || T < 0 || T > c->shape.T_max) return MOE_ERR_INVALID_ARG;
     if (!on_own_device(c)) return MOE_ERR_INVALID_ARG;
-    const int rc = scoring_status(scoring, c->shape);
+    const int rc = scoring_status(scoring, c->shape, T);
     if (rc != MOE_OK || T == 0) return rc;
     if (!x || !w_router || !topk_idx || !topk_w) return MOE_ERR_INVALID_ARG;
     return route_scored(c, x, w_router, bias, correction, *scoring, T, topk_idx, topk_w, logits_out,
@@ -864,7 +864,7 @@ int moe_route_scored_from_logits(moe_ctx* c, const float* logits, const float* c
                                  int32_t* topk_idx, float* topk_w, void* stream) {
     if (!c || T < 0 || T > c->shape.T_max) return MOE_ERR_INVALID_ARG;
     if (!on_own_device(c)) return MOE_ERR_INVALID_ARG;
-    const int rc = scoring_status(scoring, c->shape);
+    const int rc = scoring_status(scoring, c->shape, T);
     if (rc != MOE_OK || T == 0) return rc;
     if (!logits || !topk_idx || !topk_w) return MOE_ERR_INVALID_ARG;
     return launch_route_scored(logits, correction, *scoring, T, c->shape.E, c->shape.k, topk_idx, topk_w,
@@ -924,9 +924,10 @@ int moe_layer_forward_mx4(moe_ctx* c, const moe_bf16* x, const float* w_router, 
     if (!c || T < 0 || T > c->shape.T_max) return MOE_ERR_INVALID_ARG;
     if (!on_own_device(c)) return MOE_ERR_INVALID_ARG;
     const moe_shape& sh = c->shape;
-    int rc = scoring ? scoring_status(scoring, sh) : correction ? MOE_ERR_INVALID_ARG : MOE_OK;
+    int rc = scoring ? scoring_status(scoring, sh, T) : correction ? MOE_ERR_INVALID_ARG : MOE_OK;
     if (rc != MOE_OK) return rc;
-    if (sh.d_model > kMaxDimMx4 || sh.d_ff > kMaxDimMx4) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if (sh.d_model > kMaxDimMx4 || sh.d_ff > kMaxDimMx4 || !rows_mx4_fit(T, sh.d_model) || !combine_fits(T))
+        return MOE_ERR_UNSUPPORTED_SHAPE;
     if (T == 0) return MOE_OK;
     const ExpertsMx4 w{W1, W3, W2, w1_scale, w3_scale, w2_scale};
     if (!x || !w_router || !w.complete() || !y || !w.aligned()) return MOE_ERR_INVALID_ARG;

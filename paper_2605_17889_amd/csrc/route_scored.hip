@@ -129,8 +129,10 @@ __device__ __forceinline__ void load_experts(float (&v)[EW], const bool (&has)[E
     }
 }
 
+constexpr int kThreads = 256;
+
 template <int LPT, int EW, bool QUADS>
-__global__ __launch_bounds__(256) void route_scored_kernel(ScoredArgs a) {
+__global__ __launch_bounds__(kThreads) void route_scored_kernel(ScoredArgs a) {
     constexpr int PER = kWave / LPT, SLOTS = kWave / LPT;      // tokens of a wavefront; slots of a lane (k <= 64)
     const int lane = threadIdx.x & (LPT - 1);
     const int t_of = (blockIdx.x * 4 + threadIdx.x / kWave) * PER + (threadIdx.x & (kWave - 1)) / LPT;
@@ -283,12 +285,11 @@ __global__ __launch_bounds__(256) void route_scored_kernel(ScoredArgs a) {
     }
 }
 
+long long workgroups(int T, int lpt) { return (static_cast<long long>(T) * lpt + kThreads - 1) / kThreads; }
+
 template <int LPT, int EW, bool QUADS>
 int launch(const ScoredArgs& a, hipStream_t s) {
-    constexpr int PER = 4 * kWave / LPT;
-    const long long grid = (static_cast<long long>(a.T) + PER - 1) / PER;
-    if (grid * 256 >= 1ll << 32) return MOE_ERR_UNSUPPORTED_SHAPE;           // threads of a launch are counted in 32 bits
-    hipLaunchKernelGGL((route_scored_kernel<LPT, EW, QUADS>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((route_scored_kernel<LPT, EW, QUADS>), dim3(static_cast<unsigned>(workgroups(a.T, LPT))), dim3(kThreads), 0, s, a);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
@@ -298,17 +299,21 @@ int group_lanes(int groups, int lpt) {
     while (L > 0 && lpt / L < groups) L >>= 1;
     return L;
 }
+// Lanes of a token. us, 16 | 64 lanes: 256 experts in 8 groups, one token 6.7 | 4.2, 2000 7.1 | 5.3, 4000 7.3 | 7.0, 5000 8.7 | 7.9,
+// 8192 8.9 | 10.4, 16384 13.3 | 17.7; 128 experts, 4000 tokens 4.9 | 4.9; 64, softmax, 2000 3.8 | 3.6, 4000 3.9 | 4.3, 16384 6.0 | 9.2.
+int token_lanes(int T, int groups) { return T <= 4096 || group_lanes(groups, 16) == 0 ? 64 : 16; }
 
 }  // namespace
+
+bool route_scored_fits(int T, int groups) { return workgroups(T, token_lanes(T, groups)) * kThreads <= kMaxThreads; }
 
 int launch_route_scored(const float* logits, const float* correction, const moe_scoring& sc, int T, int E, int k,
                         int32_t* topk_idx, float* topk_w, hipStream_t s) {
     if (T == 0) return MOE_OK;
+    if (!route_scored_fits(T, sc.groups)) return MOE_ERR_UNSUPPORTED_SHAPE;
     ScoredArgs a{logits, correction, T, E, k, sc.groups, E / sc.groups, 0, sc.top_groups, sc.group_best == 2,
                  sc.score == MOE_SCORE_SIGMOID, sc.renormalise != 0, sc.scale, topk_idx, topk_w};
-    // us, 16 | 64 lanes: 256 experts in 8 groups, one token 6.7 | 4.2, 2000 7.1 | 5.3, 4000 7.3 | 7.0, 5000 8.7 | 7.9, 8192 8.9 |
-    // 10.4, 16384 13.3 | 17.7; 128 experts, 4000 tokens 4.9 | 4.9; 64, softmax, 2000 3.8 | 3.6, 4000 3.9 | 4.3, 16384 6.0 | 9.2.
-    const int lpt = T <= 4096 || group_lanes(a.groups, 16) == 0 ? 64 : 16;
+    const int lpt = token_lanes(T, a.groups);
     const int L = group_lanes(a.groups, lpt);
     while ((2 << a.lane_shift) <= L) ++a.lane_shift;
     const int held = (a.size + L - 1) / L;           // of a lane, where it takes every L-th expert

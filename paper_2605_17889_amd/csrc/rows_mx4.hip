@@ -93,18 +93,18 @@ int enqueue_error() { return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_
 long long row_groups(int T, int d) {
     return (static_cast<long long>(T) + kRowsPerGroup - 1) / kRowsPerGroup * mx_runs(d);
 }
-constexpr long long kMaxRowGroups = (1ll << 32) / kRowThreads - 1;       // threads of a launch are counted in 32 bits
 
 }  // namespace
+
+bool rows_mx4_fit(int T, int d) { return row_groups(T, d) * kRowThreads <= kMaxThreads; }
 
 template <bool GROUPED>
 static int quantize(const moe_bf16* x, long long x_stride, int T, int d, const int32_t* places, int k, moe_mx4* q, moe_e8m0* scale,
                     hipStream_t s) {
     if (T == 0) return MOE_OK;
-    const long long grid = row_groups(T, d);
-    if (grid > kMaxRowGroups) return MOE_ERR_UNSUPPORTED_SHAPE;
-    hipLaunchKernelGGL((quantize_mx4_kernel<GROUPED>), dim3(static_cast<unsigned>(grid)), dim3(kRowThreads), 0, s, x, x_stride, T, d,
-                       places, k, q, scale);
+    if (!rows_mx4_fit(T, d)) return MOE_ERR_UNSUPPORTED_SHAPE;
+    hipLaunchKernelGGL((quantize_mx4_kernel<GROUPED>), dim3(static_cast<unsigned>(row_groups(T, d))), dim3(kRowThreads), 0, s, x,
+                       x_stride, T, d, places, k, q, scale);
     return enqueue_error();
 }
 int launch_quantize_mx4(const moe_bf16* x, long long x_stride, int T, int d, moe_mx4* q, moe_e8m0* scale, hipStream_t s) {
@@ -117,9 +117,8 @@ int launch_quantize_grouped_mx4(const moe_bf16* x, const int32_t* inv_perm, int 
 
 int launch_dequantize_mx4(const moe_mx4* q, const moe_e8m0* scale, int T, int d, moe_bf16* y, hipStream_t s) {
     if (T == 0) return MOE_OK;
-    const long long grid = row_groups(T, d);
-    if (grid > kMaxRowGroups) return MOE_ERR_UNSUPPORTED_SHAPE;
-    hipLaunchKernelGGL(dequantize_mx4_kernel, dim3(static_cast<unsigned>(grid)), dim3(kRowThreads), 0, s, q, scale, T, d, y);
+    if (!rows_mx4_fit(T, d)) return MOE_ERR_UNSUPPORTED_SHAPE;
+    hipLaunchKernelGGL(dequantize_mx4_kernel, dim3(static_cast<unsigned>(row_groups(T, d))), dim3(kRowThreads), 0, s, q, scale, T, d, y);
     return enqueue_error();
 }
 
