@@ -163,8 +163,12 @@ int large_of(const GemmEnv& env, const Operands& op, const Outputs& out, hipStre
 }
 template <class Cfg>
 int large(const GemmEnv& env, const Operands& op, const Outputs& out, hipStream_t s) {
-    if (op.K <= kMxRun || op.N < Cfg::BN_OUT) return MOE_ERR_UNSUPPORTED_SHAPE;
-    return mx_runs(op.K) & 1 ? large_of<Cfg, true>(env, op, out, s) : large_of<Cfg, false>(env, op, out, s);
+    const bool odd = mx_runs(op.K) & 1;
+    if (op.K <= kMxRun || op.N < Cfg::BN_OUT || (Cfg::DUAL && odd)) return MOE_ERR_UNSUPPORTED_SHAPE;
+    if constexpr (!Cfg::DUAL) {                      // gate/up: K is d_model, a multiple of 512
+        if (odd) return large_of<Cfg, true>(env, op, out, s);
+    }
+    return large_of<Cfg, false>(env, op, out, s);
 }
 
 template <bool F32, int CF>

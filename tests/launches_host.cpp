@@ -134,6 +134,10 @@ int main() {
             int d;
             in >> T >> d;
             rc = moe_quantize_mx4(h(), d, T, d, b(), b(), nullptr);
+        } else if (what == "back") {                 // T d
+            int d;
+            in >> T >> d;
+            rc = moe_dequantize_mx4(b(), b(), T, d, h(), nullptr);
         }
         if (!in) rc = -101;
         std::printf("%d %zu\n", rc, launches.size());

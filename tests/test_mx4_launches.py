@@ -27,3 +27,34 @@ def test_more_tokens_than_a_launch_holds(program, call, tokens, experts):
     assert fits[0] == OK and fits[1]
     assert all(l.grid * l.threads < 2**32 for l in fits[1])
     assert refused == (UNSUPPORTED, []) and most == (UNSUPPORTED, [])
+
+
+def calls_of_every_kind():
+    """Sizes on both sides of every choice that the calls make."""
+    calls = ["context 64 512 128 8 1", "rows 5 64", "back 5 64"]
+    for d, f in ((512, 128), (512, 1408), (2048, 768), (4096, 14336)):
+        for E in (1, 8, 64):
+            for T in (1, 40, 300, 1000, 3000, 9000, 30000):
+                calls += [f"context {T} {d} {f} {E} 1", f"experts {T}"]
+    for R in (1, 40, 300, 1000, 3000, 9000, 30000):
+        calls.append(f"context {R} 512 128 256 1")
+        for E in (1, 8, 40, 256):
+            for N in (64, 80, 272, 2112, 4112, 8208, 16400):
+                for K in (96, 256, 512, 544, 800, 2080, 9248):
+                    calls += [f"product {R} {E} {N} {K} {fp32} {int(E > 1)}" for fp32 in (0, 1)]
+    for E in (8, 15, 32, 34, 63, 64, 128, 130, 252, 255, 256):
+        for groups in (1, 2, 3, 5, 8, 17, 32, 64):
+            if E % groups == 0:
+                for T in (5, 5000):
+                    calls += [f"context {T} 512 128 {E} 1", f"route {T} {SIGMOID} {groups} 1", f"layer {T} {SOFTMAX} {groups} 1"]
+    return calls
+
+
+def test_every_kernel_is_launched_by_some_call(program):
+    """The library holds no kernel of these paths that no call takes."""
+    taken = set()
+    for status, launches in run(program, calls_of_every_kind()):
+        assert status == OK
+        taken |= {l.kernel for l in launches}
+    ours = {k for k in kernels(program) if any(name in k for name in ("mx4", "few_rows_kernel", "route_scored"))}
+    assert len(ours) > 40 and not ours - taken, ours - taken
