@@ -1,0 +1,8 @@
+"""Sizes at which 4-bit products are compared with 64 bits besides those of mx4_sizes.py: what each stands for is checked by
+test_mx4_launches.py. Groups are named by the rows of each."""
+# tiles of every height, empty groups, groups of one row; 8 groups are looked up in another way than other numbers of them
+EIGHT = (0, 160, 185, 224, 256, 700, 1075, 1100)
+TWELVE = (0, 1, 33, 128, 160, 185, 224, 256, 257, 400, 700, 1356)
+# a tile for each workgroup; reductions of 16384 and more cut their tiles otherwise
+LARGE = [(EIGHT, 4112, 544), (EIGHT, 4112, 800), ((1000, 900, 1100), 4112, 544), ((1000, 900, 1100), 4112, 1024),
+         ((1100,), 4112, 16384), ((1100,), 4112, 16416), ((700, 0, 1400), 4112, 16416)]
