@@ -3,6 +3,12 @@ test_mx4_launches.py. Groups are named by the rows of each."""
 # tiles of every height, empty groups, groups of one row; 8 groups are looked up in another way than other numbers of them
 EIGHT = (0, 160, 185, 224, 256, 700, 1075, 1100)
 TWELVE = (0, 1, 33, 128, 160, 185, 224, 256, 257, 400, 700, 1356)
+# than half full. One group: without offsets.
+PERSISTENT = [(EIGHT, 16400, 544), (EIGHT, 16400, 1024), (TWELVE, 8720, 544), (TWELVE, 8720, 800),
+              ((3000,), 16400, 544), ((3000,), 16400, 800)]
 # a tile for each workgroup; reductions of 16384 and more cut their tiles otherwise
 LARGE = [(EIGHT, 4112, 544), (EIGHT, 4112, 800), ((1000, 900, 1100), 4112, 544), ((1000, 900, 1100), 4112, 1024),
          ((1100,), 4112, 16384), ((1100,), 4112, 16416), ((700, 0, 1400), 4112, 16416)]
+# the experts' FFN: groups, d_ff, d_model. d_ff = 128 modulo 256: rows of H that end in the middle of a run of scales
+GATEUP_PERSISTENT = [(EIGHT, 4224, 512), (TWELVE, 4224, 1024), ((3000,), 8320, 512), (TWELVE, 4096, 1536)]
+GATEUP_LARGE = [(EIGHT, 1408, 512), ((1000, 900, 1100), 2944, 1024), (EIGHT, 1408, 1536)]

@@ -1,7 +1,10 @@
 """What calls of the 4-bit path and of the routers by scores launch, and that calls which are refused launch nothing
 (launches_host.cpp: the library against a runtime that only takes notes)."""
+import re
+
 import pytest
 
+import mx4_large_sizes as S
 from mx4_launches import compile_program, kernels, run
 
 OK, INVALID, UNSUPPORTED = 0, -1, -2
@@ -58,3 +61,47 @@ def test_every_kernel_is_launched_by_some_call(program):
         taken |= {l.kernel for l in launches}
     ours = {k for k in kernels(program) if any(name in k for name in ("mx4", "few_rows_kernel", "route_scored"))}
     assert len(ours) > 40 and not ours - taken, ours - taken
+
+
+# ---- what the sizes of the numerical tests stand for ----------------------------------------------------
+
+def product_kernels(program, sizes, fp32):
+    """The kernel of each product; groups by their rows."""
+    calls = [call for counts, N, K in sizes
+             for call in (f"context {sum(counts)} 512 128 {len(counts)} 1",
+                          f"product {sum(counts)} {len(counts)} {N} {K} {int(fp32)} {int(len(counts) > 1)}")]
+    return [launches[0].kernel for status, launches in run(program, calls)[1::2]]
+
+
+def expert_kernels(program, sizes):
+    """The kernels of each FFN: gate/up, down."""
+    calls = [call for counts, f, d in sizes for call in (f"context {sum(counts)} {d} {f} {len(counts)} 1", f"experts {sum(counts)}")]
+    return [tuple(l.kernel for l in launches) for status, launches in run(program, calls)[1::2]]
+
+
+def tiles(counts, columns):
+    return sum(-(-rows // 256) for rows in counts) * columns
+
+
+LARGE_KERNEL = re.compile(r"large_kernel<.*>, (true|false), (true|false)>\(")
+
+
+def persistent_and_odd(kernel):
+    found = LARGE_KERNEL.search(kernel)
+    return found and tuple(word == "true" for word in found.groups())
+
+
+def test_sizes_of_persistent_workgroups(program):
+    """More than two rounds, so that workgroups draw tiles; last rounds more and less than half full, the latter in halves."""
+    for fp32 in (False, True):
+        forms = [persistent_and_odd(k) for k in product_kernels(program, S.PERSISTENT, fp32)]
+        assert all(f is not None and f[0] for f in forms)
+        for groups in (1, 8, 12):
+            assert {f[1] for f, (counts, _, _) in zip(forms, S.PERSISTENT) if len(counts) == groups} == {False, True}
+        assert {(f[0], f[1]) for f in map(persistent_and_odd, product_kernels(program, S.LARGE, fp32))} == {(False, False), (False, True)}
+    assert all(persistent_and_odd(gateup) == (True, False) for gateup, _ in expert_kernels(program, S.GATEUP_PERSISTENT))
+    assert all(persistent_and_odd(gateup) == (False, False) for gateup, _ in expert_kernels(program, S.GATEUP_LARGE))
+    plain = [tiles(counts, -(-N // 256)) for counts, N, _ in S.PERSISTENT]
+    gateup = [tiles(counts, f // 128) for counts, f, _ in S.GATEUP_PERSISTENT]
+    for totals in (plain, gateup):
+        assert min(totals) > 512 and {0 < t % 256 <= 128 for t in totals} == {False, True}
