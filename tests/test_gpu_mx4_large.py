@@ -1,5 +1,5 @@
-"""The 4-bit products on the GPU against 64 bits where tests of smaller sizes do not get: bf16 outputs of every tile, large
-tiles of every height, persistent workgroups.
+"""The 4-bit products on the GPU against 64 bits where tests of smaller sizes do not get: bf16 outputs of every tile, persistent
+workgroups, rows of H that end inside a run of scales, n-tiles that begin at k-steps of their own, NaN among the large tiles.
 
 Tolerances as in test_gpu_mx4.py: 8 units of 2^-24 of the sum of magnitudes for each matrix instruction of a sum (sum_error), half a
 step for each rounding.
@@ -9,7 +9,8 @@ import pytest
 import torch
 
 from paper_2605_17889_amd import binding as B
-from mx4_large_sizes import GATEUP_PERSISTENT, LARGE, PERSISTENT
+from mx4_large_sizes import (GATEUP_ENDS, GATEUP_LARGE, GATEUP_OWN_KSTEPS, GATEUP_PERSISTENT, LARGE, NAN, OWN_KSTEPS,
+                             PERSISTENT)
 from mx4_sizes import PLAIN
 from oracle import mx4 as M
 from test_gpu_mx4 import BF16, U, cuda, offsets_of, random_rows, sum_error
@@ -71,6 +72,38 @@ def test_large_tiles_of_every_height(counts, N, K, dtype):
 @pytest.mark.parametrize("counts,N,K", PERSISTENT)
 def test_persistent_workgroups(counts, N, K, dtype):
     check_product(offsets_from(counts), N, K, dtype)
+
+
+@pytest.mark.parametrize("counts,N,K", OWN_KSTEPS)
+def test_tiles_that_begin_at_ksteps_of_their_own(counts, N, K):
+    check_product(offsets_from(counts), N, K, torch.float32)
+
+
+@pytest.mark.parametrize("counts,N,K", NAN)
+def test_nan_of_a_row_and_of_a_column_and_no_others(counts, N, K):
+    """A block of a row, and a block of a weight row, that is NaN: that row and that column of its group, everything else as without."""
+    off, E = offsets_from(counts), len(counts)
+    R = int(off[-1])
+    g = generator(R, E, N, K)
+    q, s, _ = random_rows(g, R, K)
+    w = [random_rows(g, N, K)[:2] for _ in range(E)]
+    wq, ws = torch.stack([m[0] for m in w]), torch.stack([m[1] for m in w])
+    ctx = B.MoeContext(R, 512, 128, E, 1)
+    new = lambda: torch.empty((R, N), device="cuda")
+    call = lambda out: B.moe_gemm_mx4(ctx, q, s, None if E == 1 else cuda(off), R, E, N, K, wq, ws, out)
+    want, got = new(), new()
+    print(f"gemm with NaN R={R} E={E} N={N} K={K}", flush=True)
+    call(want)
+    assert torch.isfinite(want).all()
+    row, column, e = R // 2, N - 5, E - 1
+    s[K // 256, row, 0] = 255                        # the last run's first block
+    ws[e, 0, column, 2] = 255                        # block 1
+    call(got)
+    bad = torch.zeros((R, N), dtype=torch.bool, device="cuda")
+    bad[row] = True
+    bad[int(off[e]):int(off[e + 1]), column] = True
+    assert torch.equal(torch.isnan(got), bad) and torch.equal(got[~bad], want[~bad])
+    ctx.close()
 
 
 # ---- experts' FFN ------------------------------------------------------------------------------------
@@ -156,9 +189,24 @@ def check_experts(counts, f, d, nan_row=None):
     ctx.close()
 
 
+@pytest.mark.parametrize("counts,f,d", GATEUP_ENDS + GATEUP_LARGE)
+def test_rows_of_h_that_end_inside_a_run(counts, f, d):
+    check_experts(counts, f, d)
+
+
 @pytest.mark.parametrize("counts,f,d", GATEUP_PERSISTENT)
 def test_experts_of_persistent_workgroups(counts, f, d):
     check_experts(counts, f, d)
+
+
+@pytest.mark.parametrize("counts,f,d", GATEUP_OWN_KSTEPS)
+def test_experts_whose_tiles_begin_at_ksteps_of_their_own(counts, f, d):
+    check_experts(counts, f, d)
+
+
+@pytest.mark.parametrize("counts,f,d", [GATEUP_ENDS[1], GATEUP_LARGE[0], GATEUP_PERSISTENT[0]])
+def test_experts_of_a_row_with_nan(counts, f, d):
+    check_experts(counts, f, d, nan_row=sum(counts) // 2)
 
 
 # ---- persistent workgroups in graphs and on two streams ----------------------------------------------

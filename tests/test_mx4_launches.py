@@ -6,6 +6,7 @@ import pytest
 
 import mx4_large_sizes as S
 from mx4_launches import compile_program, kernels, run
+from mx4_sizes import PLAIN
 
 OK, INVALID, UNSUPPORTED = 0, -1, -2
 SOFTMAX, SIGMOID, NONE = 0, 1, -1
@@ -91,6 +92,15 @@ def persistent_and_odd(kernel):
     return found and tuple(word == "true" for word in found.groups())
 
 
+def test_every_product_kernel_is_compared_with_64_bits(program):
+    plain = [((R // E,) * (E - 1) + (R - R // E * (E - 1),), N, K) for R, E, N, K in PLAIN] + S.PERSISTENT + S.LARGE
+    tested = set(product_kernels(program, plain, False)) | set(product_kernels(program, plain, True))
+    experts = S.GATEUP_PERSISTENT + S.GATEUP_LARGE + S.GATEUP_ENDS + S.GATEUP_OWN_KSTEPS
+    tested |= {gateup for gateup, _ in expert_kernels(program, experts)}
+    ours = {k for k in kernels(program) if "mx4::Operands" in k}
+    assert len(ours) > 25 and not ours - tested, ours - tested
+
+
 def test_sizes_of_persistent_workgroups(program):
     """More than two rounds, so that workgroups draw tiles; last rounds more and less than half full, the latter in halves."""
     for fp32 in (False, True):
@@ -105,3 +115,26 @@ def test_sizes_of_persistent_workgroups(program):
     gateup = [tiles(counts, f // 128) for counts, f, _ in S.GATEUP_PERSISTENT]
     for totals in (plain, gateup):
         assert min(totals) > 512 and {0 < t % 256 <= 128 for t in totals} == {False, True}
+
+
+def test_sizes_whose_rows_of_h_end_inside_a_run(program):
+    gateup = [k[0] for k in expert_kernels(program, S.GATEUP_ENDS + S.GATEUP_LARGE + S.GATEUP_PERSISTENT[:3])]
+    assert all(f % 256 == 128 for _, f, _ in S.GATEUP_ENDS + S.GATEUP_LARGE + S.GATEUP_PERSISTENT[:3])
+    assert {persistent_and_odd(k) for k in gateup} == {None, (True, False), (False, False)}
+    assert len(set(gateup)) >= 5
+
+
+def test_sizes_of_ksteps_in_turn(program):
+    """Every tile whose k-steps may begin anywhere."""
+    for counts, _, K in S.OWN_KSTEPS + S.GATEUP_OWN_KSTEPS:
+        assert K % 8192 == 0
+    ring = {k for k in kernels(program) if "ring_kernel" in k}
+    plain = {k for k in ring if re.search(r", true>\s*>\(", k)}                           # of fp32 outputs
+    gateup = {k for k in ring if re.search(r", true, (true|false), false>\s*>\(", k)}     # DUAL
+    assert set(product_kernels(program, S.OWN_KSTEPS, True)) >= plain - {k for k in plain if "128, 128, 2, 2, 2" in k}
+    assert {k for k, _ in expert_kernels(program, S.GATEUP_OWN_KSTEPS)} >= gateup and len(gateup) == 4 and len(plain) == 7
+
+
+def test_sizes_with_nan_take_ring_and_large_tiles(program):
+    forms = {persistent_and_odd(k) for k in product_kernels(program, S.NAN, True)}
+    assert forms == {None, (False, True), (True, False)}
