@@ -472,8 +472,9 @@ int moe_expert_ffn_mx4(moe_ctx* ctx, const moe_mx4* x_perm, const moe_e8m0* x_sc
 /* moe_layer_forward with its experts in 4 bits: the router reads the tokens x [T,d_model] in bf16, the experts the same tokens
  * as moe_quantize_mx4 brings them to 4 bits; route -> permute -> rows in 4 bits, grouped -> expert FFN as in
  * moe_expert_ffn_mx4 -> combine. scoring NULL: the router is moe_route's (correction is NULL then), else moe_route_scored's with
- * correction [E] or NULL. T below 2^24, else MOE_ERR_UNSUPPORTED_SHAPE. Weights as above; moe_set_expert_output_fp32 and
- * moe_last_routing as for moe_layer_forward. The rows' conversion is the gather stage of moe_profile_begin. */
+ * correction [E] or NULL. T below 2^24 and tokens that moe_quantize_mx4 takes, else MOE_ERR_UNSUPPORTED_SHAPE. Weights as above;
+ * moe_set_expert_output_fp32 and moe_last_routing as for moe_layer_forward. The rows' conversion is the gather stage of
+ * moe_profile_begin. */
 int moe_layer_forward_mx4(moe_ctx* ctx, const moe_bf16* x, const float* w_router, const float* bias,
                           const float* correction, const moe_scoring* scoring, const moe_mx4* W1,
                           const moe_e8m0* w1_scale, const moe_mx4* W3, const moe_e8m0* w3_scale,
